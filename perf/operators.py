@@ -456,7 +456,7 @@ def _plain_adamw(st):
     m_top, v_top = m.abs().amax(1, True), v.amax(1, True)
     q = (m.abs() * torch.where(m_top > 0, 1.0 / m_top, 0.0)) * float(127 ** 2)
     k = (q.sqrt() + 0.5).floor()
-    k = k + ((k + 0.5) * (k + 0.5) <= q).float() - ((k - 0.5) * (k - 0.5) > q).float()
+    k = k + ((k + 0.5) * (k + 0.5) <= q).float() - (((k - 0.5) * (k - 0.5) > q) & (k > 0)).float()
     k = k.clamp(max=127.0) * torch.where(m < 0, -1.0, 1.0)
     st.m8.copy_(k.view(-1))
     st.m_top.copy_(m_top.view(-1))
