@@ -509,6 +509,120 @@ int32_t ddp_sync_static(int32_t R, int32_t device, void* stream, int32_t n,
                         const int64_t* numel, const int32_t* dtype,
                         void* const* grad_ptrs, uint64_t cap_bytes);
 
+/* ---- Around the synchronization: the optimizer ----------------------------
+ *
+ * What a training program does with the averages: their global norm, and the
+ * AdamW step over all parameter tensors at once.  A handle of its own (the
+ * gradients need not come from a context); its work is enqueued on the stream
+ * it is created with, which is backward_stream where it follows
+ * ddp_finalize_backward.  Like a context it is not thread-safe, borrows the
+ * memory it is given until ddp_opt_destroy, and is host-asynchronous once
+ * ddp_opt_set_state has returned.  Errors as for contexts, text in
+ * ddp_opt_last_error.  A handle made with DDP_DEVICE_NONE checks arguments
+ * and computes nothing (DDP_ERR_NO_DEVICE).
+ *
+ * Order of calls: create, register, optionally set_groups and set_copies,
+ * set_state; then per iteration grad_norm (optional) and adamw_step. */
+typedef struct ddp_opt ddp_opt;
+
+/* how the two moments of a parameter are held */
+#define DDP_STATE_FP32 0   /* binary32 each */
+#define DDP_STATE_8BIT 1   /* 8 bits each, and a binary32 scale for every 256 elements: with `top` the largest
+                              absolute value of the 256, m = top * sign(k) * (k / 127)^2 with a signed k and
+                              v = top * (k / 255)^4 with an unsigned one, the nearest k in the root's scale; k >= 1
+                              where v > 0.  A gradient that is not finite spoils the 256 elements it
+                              belongs to (skip_nonfinite below keeps it out).  Blocks whose largest value is below the smallest
+                              normal number count as zeros */
+
+/* A state is one region of device memory, which the caller owns, clears before
+ * the first step and saves with a checkpoint: the number of steps taken (int64)
+ * in its first 8 bytes, then where[0] first moments, where[1] second moments,
+ * and with DDP_STATE_8BIT where[2] and where[3] their scales.  Element j of
+ * tensor i is element elem_offset[i] + j (tensors start at multiples of 256).
+ *   elem_offset  host array of n, or NULL
+ *   where[6]     byte offsets of the four arrays, number of elements, total bytes */
+int32_t ddp_opt_state_layout(int32_t n, const int64_t* numel, int32_t kind, int64_t* elem_offset, int64_t* where);
+
+int32_t ddp_opt_create(ddp_opt** out, int32_t device, void* stream);
+int32_t ddp_opt_destroy(ddp_opt* opt);              /* waits for the handle's outstanding work */
+const char* ddp_opt_last_error(const ddp_opt* opt);
+
+/* n tensors: element counts (0 allowed), types and device addresses of the
+ * parameters (param_ptrs NULL: for ddp_opt_grad_norm alone) and of their
+ * gradients; contiguous, aligned to their element size, all regions apart.
+ * Types may differ from tensor to tensor and between a parameter and its
+ * gradient (binary32 averages of ddp_set_outputs for bfloat16 parameters, or
+ * bfloat16 gradients for binary32 parameters). */
+int32_t ddp_opt_register(ddp_opt* opt, int32_t n, const int64_t* numel, const int32_t* param_dtype, void* const* param_ptrs,
+                         const int32_t* grad_dtype, void* const* grad_ptrs);
+
+/* Factors of a step's lr and weight_decay for every tensor (host arrays of n, or
+ * NULL: all 1).  decay_scale 0 exempts vectors and biases. */
+int32_t ddp_opt_set_groups(ddp_opt* opt, const float* lr_scale, const float* decay_scale);
+
+/* 16-bit copies of binary32 parameters, which a step writes as well (the next
+ * forward pass's weights); a NULL address: this tensor has none. */
+int32_t ddp_opt_set_copies(ddp_opt* opt, const int32_t* copy_dtype, void* const* copy_ptrs);
+
+/* The state, aligned to 16 bytes; allocates the handle's tables. */
+int32_t ddp_opt_set_state(ddp_opt* opt, int32_t kind, void* state, int64_t bytes);
+
+/* The 2-norm over all gradients, summed in 64 bits in a fixed order: |grad_scale|
+ * times it is written to norm_out (device, may be NULL), and the next step can
+ * clip by it.  used[n] (host, NULL = all ones): parameters with 0 are left out;
+ * what ddp_get_global_used gives suits. */
+int32_t ddp_opt_grad_norm(ddp_opt* opt, double grad_scale, const uint8_t* used, float* norm_out);
+
+/* One step, with g' = g * grad_scale * min(1, max_norm / (norm + 1e-6)):
+ *   m = beta1 m + (1 - beta1) g'      v = beta2 v + (1 - beta2) g'^2
+ *   p = p - lr weight_decay p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * t counts the steps in the state, this one included.  All in binary32 and rounded
+ * once to a parameter's type; the moments of DDP_STATE_8BIT are rounded after they
+ * have served.  max_norm <= 0: no clipping; norm is |grad_scale| times
+ * that of the latest ddp_opt_grad_norm, which max_norm > 0 and skip_nonfinite need since the step
+ * before (DDP_ERR_STATE otherwise).  skip_nonfinite != 0: where the norm is not finite nothing changes and
+ * no step is counted.  Parameters with used[i] == 0 keep their values and moments.
+ * May be captured into a HIP graph, with ddp_opt_grad_norm in front of it (the
+ * hyperparameters and flags are those of the capture, the count of steps goes on). */
+int32_t ddp_opt_adamw_step(ddp_opt* opt, double lr, double beta1, double beta2, double eps, double weight_decay,
+                           double grad_scale, double max_norm, int32_t skip_nonfinite, const uint8_t* used);
+
+/* DDP_STATE_8BIT: the moments as the binary32 values that the codes stand for, in the
+ * order of the state (where[4] elements each; either may be NULL). */
+int32_t ddp_opt_read_state(ddp_opt* opt, float* m_out, float* v_out);
+
+/* ---- Around the synchronization: the embedding -----------------------------
+ *
+ * The table that opens a language model's forward pass is usually the first
+ * parameter, so its gradient closes the backward pass: the last to be marked ready.
+ * A handle holds a table's sizes and the workspace of the gradient; conventions as for
+ * ddp_opt.  All calls on a handle share the workspace and run on its stream. */
+typedef struct ddp_embedding ddp_embedding;
+
+/* A table of `rows` (up to 2^23) rows of `width` (up to 2^20) elements; max_tokens (up to 2^26): of a
+ * ddp_embedding_grad call (0: lookups only).  The workspace takes 12 bytes and a
+ * sixteenth of a binary32 row per token, and 4 bytes per row. */
+int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, int64_t rows, int64_t width, int64_t max_tokens);
+int32_t ddp_embedding_destroy(ddp_embedding* emb);   /* waits for the handle's outstanding work */
+const char* ddp_embedding_last_error(const ddp_embedding* emb);
+
+/* out[t, :] = scale * table[ids[t], :], in binary32, rounded once to the type of out.
+ * ids: device array of 32- or 64-bit integers (id_bits); an id outside
+ * [0, rows) reads nothing and gives zeros.  Strides in elements, at least the width;
+ * any alignment to the element size.  table and out must not overlap. */
+int32_t ddp_embedding_lookup(ddp_embedding* emb, int64_t tokens, const void* ids, int32_t id_bits, const void* table, int32_t table_dtype,
+                             int64_t table_stride, float scale, void* out, int32_t out_dtype, int64_t out_stride);
+
+/* grad[r, :] = scale * sum of dout[t, :] over the tokens with ids[t] == r, for every row r of
+ * the table (zeros where there are none); accumulate != 0: added to what grad holds,
+ * rows without tokens are not touched.  Tokens whose id is padding_row (-1: none) or outside
+ * [0, rows) take no part and their rows of dout are not read.  Sums are in binary32 in an
+ * order that depends on the ids alone (repeated calls give the same bits), rounded once
+ * to the type of grad. */
+int32_t ddp_embedding_grad(ddp_embedding* emb, int64_t tokens, const void* ids, int32_t id_bits, const void* dout, int32_t dout_dtype,
+                           int64_t dout_stride, float scale, int64_t padding_row, int32_t accumulate, void* grad, int32_t grad_dtype,
+                           int64_t grad_stride);
+
 /* Library version string. */
 const char* ddp_version(void);
 

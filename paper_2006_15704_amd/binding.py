@@ -43,6 +43,7 @@ DDP_OPT_FLAG_ORDER, DDP_OPT_GATE_WAIT_US, DDP_OPT_LAUNCH_HOLD, DDP_OPT_CHAIN_LAU
 DDP_STAT_REPAIRED_LAUNCHES, DDP_STAT_EARLY_LAUNCHES = 100, 101
 DDP_PIPELINE_STAGED, DDP_PIPELINE_FUSED = 0, 1
 DDP_STATIC_SCRATCH_BYTES = 32 << 20
+DDP_STATE_FP32, DDP_STATE_8BIT = 0, 1
 DDP_K_PACK, DDP_K_REDUCE, DDP_K_UNPACK, DDP_K_ACCUMULATE, DDP_K_ITERATION = 0, 1, 2, 3, 4
 
 EXPORTS = [
@@ -54,6 +55,11 @@ EXPORTS = [
     "ddp_mark_ready_many", "ddp_finalize_backward", "ddp_synchronize",
     "ddp_get_launch_log", "ddp_no_sync_accumulate", "ddp_get_used_map",
     "ddp_synth_backward", "ddp_get_kernel_times", "ddp_sync_static",
+    "ddp_opt_state_layout", "ddp_opt_create", "ddp_opt_destroy", "ddp_opt_last_error", "ddp_opt_register",
+    "ddp_opt_set_groups", "ddp_opt_set_copies", "ddp_opt_set_state", "ddp_opt_grad_norm", "ddp_opt_adamw_step",
+    "ddp_opt_read_state",
+    "ddp_embedding_create", "ddp_embedding_destroy", "ddp_embedding_last_error", "ddp_embedding_lookup",
+    "ddp_embedding_grad",
 ]
 
 
@@ -115,8 +121,28 @@ _lib.ddp_get_used_map.argtypes = [_vp, _i32, C.POINTER(C.c_uint8)]
 _lib.ddp_synth_backward.argtypes = [_vp, C.POINTER(_i32), _i32, C.POINTER(_i64), C.POINTER(_vp), _i32]
 _lib.ddp_get_kernel_times.argtypes = [_vp, _i32, C.POINTER(C.c_float), C.POINTER(_i32), _i32, C.POINTER(_i32)]
 _lib.ddp_sync_static.argtypes = [_i32, _i32, _vp, _i32, C.POINTER(_i64), C.POINTER(_i32), C.POINTER(_vp), _u64]
+_f32, _f64 = C.c_float, C.c_double
+_lib.ddp_opt_last_error.restype = C.c_char_p
+_lib.ddp_opt_last_error.argtypes = [_vp]
+_lib.ddp_opt_state_layout.argtypes = [_i32, C.POINTER(_i64), _i32, C.POINTER(_i64), C.POINTER(_i64)]
+_lib.ddp_opt_create.argtypes = [C.POINTER(_vp), _i32, _vp]
+_lib.ddp_opt_destroy.argtypes = [_vp]
+_lib.ddp_opt_register.argtypes = [_vp, _i32, C.POINTER(_i64), C.POINTER(_i32), C.POINTER(_vp), C.POINTER(_i32),
+                                  C.POINTER(_vp)]
+_lib.ddp_opt_set_groups.argtypes = [_vp, C.POINTER(_f32), C.POINTER(_f32)]
+_lib.ddp_opt_set_copies.argtypes = [_vp, C.POINTER(_i32), C.POINTER(_vp)]
+_lib.ddp_opt_set_state.argtypes = [_vp, _i32, _vp, _i64]
+_lib.ddp_opt_grad_norm.argtypes = [_vp, _f64, C.POINTER(C.c_uint8), _vp]
+_lib.ddp_opt_adamw_step.argtypes = [_vp] + [_f64] * 7 + [_i32, C.POINTER(C.c_uint8)]
+_lib.ddp_opt_read_state.argtypes = [_vp, _vp, _vp]
+_lib.ddp_embedding_last_error.restype = C.c_char_p
+_lib.ddp_embedding_last_error.argtypes = [_vp]
+_lib.ddp_embedding_create.argtypes = [C.POINTER(_vp), _i32, _vp, _i64, _i64, _i64]
+_lib.ddp_embedding_destroy.argtypes = [_vp]
+_lib.ddp_embedding_lookup.argtypes = [_vp, _i64, _vp, _i32, _vp, _i32, _i64, _f32, _vp, _i32, _i64]
+_lib.ddp_embedding_grad.argtypes = [_vp, _i64, _vp, _i32, _vp, _i32, _i64, _f32, _i64, _i32, _vp, _i32, _i64]
 for _name in EXPORTS:
-    if _name not in ("ddp_version", "ddp_last_error"):
+    if not _name.endswith("_last_error") and _name != "ddp_version":
         getattr(_lib, _name).restype = _i32
 
 
@@ -370,3 +396,153 @@ def ddp_sync_static(R: int, device: int, stream: int, numel: Sequence[int], dtyp
         raise ValueError(f"grad_ptrs has {len(gp)} entries, expected R*n = {R * len(ne)}")
     return _check(None, _lib.ddp_sync_static(R, device, _vp(stream or None), len(ne), _as(ne, _i64),
                                              _as(dt, _i32), _as(gp, _vp), cap_bytes))
+
+
+# ---- around the synchronization: the optimizer ----
+
+_opt_n = {}      # handle address -> number of tensors, for checking array lengths before they cross the C ABI
+
+
+def _check_opt(opt, status: int) -> int:
+    if status < 0:
+        raise DdpError(status, ddp_opt_last_error(opt))
+    return status
+
+
+def _sized(values, n: int, what: str, convert):
+    """An array of exactly n entries (the library reads that many), or None."""
+    if values is None:
+        return None
+    arr = convert(values)
+    if arr.ndim != 1 or len(arr) != n:
+        raise ValueError(f"{what} has {arr.size} entries, expected {n}")
+    return arr
+
+
+def _f32_array(values) -> np.ndarray:
+    return np.ascontiguousarray(values, dtype=np.float32)
+
+
+def _flags(used, opt):
+    if used is None:
+        return None
+    return _sized(used, _opt_n.get(opt.value, 0), "used", lambda u: np.ascontiguousarray(np.asarray(u) != 0, dtype=np.uint8))
+
+
+def _or_null(arr, ctype):
+    return None if arr is None else _as(arr, ctype)
+
+
+def ddp_opt_last_error(opt) -> str:
+    msg = _lib.ddp_opt_last_error(opt)
+    return msg.decode() if msg else ""
+
+
+def ddp_opt_state_layout(numel: Sequence[int], kind: int):
+    """(element offset of every tensor, {"m", "v", "m_top", "v_top": byte offsets, "elems", "bytes"})."""
+    ne = _i64_array(numel)
+    offset, where = np.zeros(len(ne), dtype=np.int64), np.zeros(6, dtype=np.int64)
+    _check_opt(None, _lib.ddp_opt_state_layout(len(ne), _as(ne, _i64), kind, _as(offset, _i64), _as(where, _i64)))
+    return offset, dict(zip(("m", "v", "m_top", "v_top", "elems", "bytes"), (int(x) for x in where)))
+
+
+def ddp_opt_create(device: int, stream: int = 0):
+    """Returns the opaque handle.  stream: a raw hipStream_t value."""
+    handle = _vp()
+    _check_opt(None, _lib.ddp_opt_create(C.byref(handle), device, _vp(stream or None)))
+    return handle
+
+
+def ddp_opt_destroy(opt) -> None:
+    _opt_n.pop(opt.value, None)
+    _check_opt(None, _lib.ddp_opt_destroy(opt))
+
+
+def ddp_opt_register(opt, numel: Sequence[int], param_dtype: Sequence[int], param_ptrs: Optional[Sequence[int]],
+                     grad_dtype: Sequence[int], grad_ptrs: Optional[Sequence[int]]) -> None:
+    ne = _i64_array(numel)
+    n = len(ne)
+    pt, gt = _sized(param_dtype, n, "param_dtype", _i32_array), _sized(grad_dtype, n, "grad_dtype", _i32_array)
+    pp, gp = _sized(param_ptrs, n, "param_ptrs", _ptr_array), _sized(grad_ptrs, n, "grad_ptrs", _ptr_array)
+    _check_opt(opt, _lib.ddp_opt_register(opt, n, _as(ne, _i64), _as(pt, _i32), _or_null(pp, _vp), _as(gt, _i32),
+                                          _or_null(gp, _vp)))
+    _opt_n[opt.value] = n
+
+
+def ddp_opt_set_groups(opt, lr_scale: Optional[Sequence[float]] = None,
+                       decay_scale: Optional[Sequence[float]] = None) -> None:
+    n = _opt_n.get(opt.value, 0)
+    lr, decay = _sized(lr_scale, n, "lr_scale", _f32_array), _sized(decay_scale, n, "decay_scale", _f32_array)
+    _check_opt(opt, _lib.ddp_opt_set_groups(opt, _or_null(lr, _f32), _or_null(decay, _f32)))
+
+
+def ddp_opt_set_copies(opt, copy_dtype: Sequence[int], copy_ptrs: Sequence[Optional[int]]) -> None:
+    n = _opt_n.get(opt.value, 0)
+    ct, cp = _sized(copy_dtype, n, "copy_dtype", _i32_array), _sized(copy_ptrs, n, "copy_ptrs", _ptr_array)
+    _check_opt(opt, _lib.ddp_opt_set_copies(opt, _or_null(ct, _i32), _or_null(cp, _vp)))
+
+
+def ddp_opt_set_state(opt, kind: int, state: int, nbytes: int) -> None:
+    _check_opt(opt, _lib.ddp_opt_set_state(opt, kind, _vp(state or None), nbytes))
+
+
+def ddp_opt_grad_norm(opt, grad_scale: float = 1.0, norm_out: int = 0, used=None) -> None:
+    flags = _flags(used, opt)
+    status = _lib.ddp_opt_grad_norm(opt, grad_scale, _or_null(flags, C.c_uint8), norm_out or None)
+    if status < 0:
+        _check_opt(opt, status)
+
+
+def ddp_opt_adamw_step(opt, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                       weight_decay: float = 0.0, grad_scale: float = 1.0, max_norm: float = 0.0,
+                       skip_nonfinite: bool = False, used=None) -> None:
+    flags = _flags(used, opt)
+    status = _lib.ddp_opt_adamw_step(opt, lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm,
+                                     1 if skip_nonfinite else 0, _or_null(flags, C.c_uint8))
+    if status < 0:
+        _check_opt(opt, status)
+
+
+def ddp_opt_read_state(opt, m_out: int, v_out: int) -> None:
+    _check_opt(opt, _lib.ddp_opt_read_state(opt, m_out or None, v_out or None))
+
+
+# ---- around the synchronization: the embedding ----
+
+def _check_embedding(emb, status: int) -> int:
+    if status < 0:
+        raise DdpError(status, ddp_embedding_last_error(emb))
+    return status
+
+
+def ddp_embedding_last_error(emb) -> str:
+    msg = _lib.ddp_embedding_last_error(emb)
+    return msg.decode() if msg else ""
+
+
+def ddp_embedding_create(device: int, stream: int, rows: int, width: int, max_tokens: int):
+    """Returns the opaque handle.  max_tokens: of a ddp_embedding_grad call (0: lookups only)."""
+    handle = _vp()
+    _check_embedding(None, _lib.ddp_embedding_create(C.byref(handle), device, _vp(stream or None), rows, width, max_tokens))
+    return handle
+
+
+def ddp_embedding_destroy(emb) -> None:
+    _check_embedding(None, _lib.ddp_embedding_destroy(emb))
+
+
+def ddp_embedding_lookup(emb, tokens: int, ids: int, id_bits: int, table: int, table_dtype: int, table_stride: int,
+                         scale: float, out: int, out_dtype: int, out_stride: int) -> None:
+    status = _lib.ddp_embedding_lookup(emb, tokens, ids, id_bits, table, table_dtype, table_stride, scale, out,
+                                       out_dtype, out_stride)
+    if status < 0:
+        _check_embedding(emb, status)
+
+
+def ddp_embedding_grad(emb, tokens: int, ids: int, id_bits: int, dout: int, dout_dtype: int, dout_stride: int,
+                       scale: float, padding_row: int, accumulate: bool, grad: int, grad_dtype: int,
+                       grad_stride: int) -> None:
+    status = _lib.ddp_embedding_grad(emb, tokens, ids, id_bits, dout, dout_dtype, dout_stride, scale, padding_row,
+                                     1 if accumulate else 0, grad, grad_dtype, grad_stride)
+    if status < 0:
+        _check_embedding(emb, status)

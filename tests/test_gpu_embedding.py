@@ -1,0 +1,305 @@
+"""The embedding lookup and its gradient, through the C ABI, against the 64-bit oracle.
+
+A lookup is one binary32 product, rounded to the type of the output: compared bit for bit.  A row of the
+gradient is a binary32 sum of n terms, scaled (and added to what is there): its error is at most (n + 3) u times the
+sum of the terms' magnitudes, u = 2^-24, plus one rounding to the gradient's type."""
+import numpy as np
+import pytest
+
+from oracle import operators as ops
+
+pytestmark = pytest.mark.gpu
+
+FP32, FP16, BF16 = 0, 1, 2
+U = 2.0 ** -24
+UNIT = {FP32: 0.0, FP16: 2.0 ** -11, BF16: 2.0 ** -8}
+TINY = {FP32: 2.0 ** -149, FP16: 2.0 ** -25, BF16: 2.0 ** -134}
+
+
+def lib():
+    import torch
+    import paper_2006_15704_amd as d
+    return torch, d
+
+
+def torch_type(torch, dt):
+    return {FP32: torch.float32, FP16: torch.float16, BF16: torch.bfloat16}[dt]
+
+
+def rows_of(values, dt, stride, shift=0, guard=7.0):
+    """values[T, D] in a buffer with `stride` elements from row to row, `shift` elements in: (buffer, view)."""
+    torch, _ = lib()
+    T, D = values.shape
+    buf = torch.full((shift + T * stride + 16,), guard, dtype=torch_type(torch, dt), device="cuda")
+    view = buf[shift:shift + T * stride].view(T, stride)[:, :D]
+    view.copy_(torch.from_numpy(np.ascontiguousarray(values, dtype=np.float64)))
+    return buf, view
+
+
+def ids_on(ids, bits, shift=0):
+    torch, _ = lib()
+    buf = torch.zeros(len(ids) + shift, dtype=torch.int64 if bits == 64 else torch.int32, device="cuda")
+    buf[shift:].copy_(torch.from_numpy(np.asarray(ids, dtype=np.int64)))
+    return buf[shift:]
+
+
+def check_lookup(rows, width, ids, table_dt, out_dt, bits=64, gaps=(0, 0), shifts=(0, 0), scale=1.5, seed=0):
+    torch, d = lib()
+    rng = np.random.default_rng(seed)
+    T = len(ids)
+    _, table = rows_of(rng.standard_normal((rows, width)), table_dt, width + gaps[0], shifts[0])
+    out_buf, out = rows_of(np.full((T, width), 7.0), out_dt, width + gaps[1], shifts[1])
+    on = ids_on(ids, bits)
+    emb = d.ddp_embedding_create(0, 0, rows, width, 0)
+    torch.cuda.synchronize()
+    d.ddp_embedding_lookup(emb, T, on.data_ptr(), bits, table.data_ptr(), table_dt, width + gaps[0], scale, out.data_ptr(),
+                           out_dt, width + gaps[1])
+    torch.cuda.synchronize()
+    held = table.double().cpu().numpy()
+    want = torch.from_numpy(ops.lookup(held, np.asarray(ids), np.float32(scale)).astype(np.float32)).to(torch_type(torch, out_dt))
+    assert torch.equal(out.cpu(), want)
+    keep = out_buf.clone()
+    keep[shifts[1]:shifts[1] + T * (width + gaps[1])].view(T, width + gaps[1])[:, :width] = 7.0
+    assert (keep == 7.0).all(), "wrote outside its rows"
+    d.ddp_embedding_destroy(emb)
+
+
+@pytest.mark.parametrize("table_dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("out_dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("width,tokens", [(1, 1), (7, 5), (64, 3), (513, 9), (1024, 1), (2050, 6)])
+def test_lookup(table_dt, out_dt, width, tokens):
+    rng = np.random.default_rng(width)
+    check_lookup(37, width, rng.integers(0, 37, tokens), table_dt, out_dt)
+
+
+@pytest.mark.parametrize("bits", [32, 64])
+def test_lookup_outside_the_table(bits):
+    far = 2 ** 31 - 1 if bits == 32 else 2 ** 40
+    check_lookup(5, 100, [0, -1, 4, 5, far, -far, 2], FP32, BF16, bits)
+
+
+@pytest.mark.parametrize("gaps,shifts", [((3, 0), (0, 1)), ((0, 5), (1, 3)), ((1, 1), (1, 0)), ((8, 8), (4, 4))])
+@pytest.mark.parametrize("dt", [FP32, BF16])
+def test_lookup_strides_and_alignments(gaps, shifts, dt):
+    check_lookup(19, 130, np.arange(40) % 19, dt, dt, gaps=gaps, shifts=shifts)
+
+
+def test_lookup_past_32_bits():
+    """A table of 4.3 GB: the offset of its last rows needs more than 32 bits."""
+    torch, d = lib()
+    rows, width = 1 << 21, 1040
+    table = torch.zeros((rows, width), dtype=torch.bfloat16, device="cuda")
+    table[-1], table[rows // 2 + 1] = 3.0, 5.0
+    ids = ids_on([rows - 1, rows // 2 + 1, 0], 64)
+    out = torch.full((3, width), 7.0, device="cuda")
+    emb = d.ddp_embedding_create(0, 0, rows, width, 0)
+    torch.cuda.synchronize()
+    d.ddp_embedding_lookup(emb, 3, ids.data_ptr(), 64, table.data_ptr(), BF16, width, 2.0, out.data_ptr(), FP32, width)
+    torch.cuda.synchronize()
+    assert (out[0] == 6.0).all() and (out[1] == 10.0).all() and (out[2] == 0.0).all()
+    d.ddp_embedding_destroy(emb)
+
+
+class Table:
+    def __init__(self, rows, width, max_tokens, stream=0):
+        _, d = lib()
+        self.rows, self.width = rows, width
+        self.emb = d.ddp_embedding_create(0, stream, rows, width, max_tokens)
+
+    def grad(self, ids, dout, dout_dt, grad, grad_dt, scale=1.5, padding=-1, add=False, bits=64, gaps=(0, 0)):
+        _, d = lib()
+        d.ddp_embedding_grad(self.emb, len(ids), ids.data_ptr(), bits, dout.data_ptr(), dout_dt, self.width + gaps[0], scale,
+                             padding, add, grad.data_ptr(), grad_dt, self.width + gaps[1])
+
+    def close(self):
+        _, d = lib()
+        d.ddp_embedding_destroy(self.emb)
+
+
+def check_grad(rows, width, ids, dout_dt, grad_dt, padding=-1, add=False, bits=64, gaps=(0, 0), shifts=(0, 0), seed=0, table=None,
+               poison=False, scale=1.5):
+    torch, _ = lib()
+    rng = np.random.default_rng(seed)
+    ids = np.asarray(ids, dtype=np.int64)
+    T = len(ids)
+    unused = (ids < 0) | (ids >= rows) | (ids == padding)
+    _, dout = rows_of(rng.standard_normal((T, width)) if T else np.zeros((0, width)), dout_dt, width + gaps[0], shifts[0])
+    if poison:
+        dout[torch.from_numpy(unused).cuda()] = float("nan")
+    buf, grad = rows_of(rng.standard_normal((rows, width)), grad_dt, width + gaps[1], shifts[1])
+    if poison and not add:
+        grad.fill_(float("nan"))
+    old = grad.double().cpu().numpy() if add else None
+    mine = table or Table(rows, width, max(T, 1))
+    on = ids_on(ids, bits)
+    torch.cuda.synchronize()
+    mine.grad(on, dout, dout_dt, grad, grad_dt, scale, padding, add, bits, gaps)
+    torch.cuda.synchronize()
+    held = np.nan_to_num(dout.double().cpu().numpy())
+    want, size = ops.embedding_grad(rows, ids, held, float(np.float32(scale)), padding, old)
+    count = np.bincount(ids[~unused], minlength=rows)[:, None]
+    got = grad.double().cpu().numpy()
+    assert (np.abs(got - want) <= (count + 3) * U * size + UNIT[grad_dt] * np.abs(want) + TINY[grad_dt]).all()
+    if add:
+        assert (got[count[:, 0] == 0] == old[count[:, 0] == 0]).all(), "a row without tokens was touched"
+    keep = buf.clone()
+    keep[shifts[1]:shifts[1] + rows * (width + gaps[1])].view(rows, width + gaps[1])[:, :width] = 7.0
+    assert (keep == 7.0).all(), "wrote outside its rows"
+    if table is None:
+        mine.close()
+    return got
+
+
+def zipf(rng, rows, tokens):
+    return np.minimum(np.exp(rng.random(tokens) * np.log(rows + 1.0)).astype(np.int64) - 1, rows - 1)
+
+
+@pytest.mark.parametrize("dout_dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("grad_dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("add", [False, True])
+def test_grad_types(dout_dt, grad_dt, add):
+    rng = np.random.default_rng(1)
+    check_grad(50, 130, zipf(rng, 50, 333), dout_dt, grad_dt, add=add)
+
+
+@pytest.mark.parametrize("rows,width,tokens", [
+    (1, 1, 1), (1, 5, 1000), (2, 64, 512), (3, 1024, 2), (16, 8, 17), (17, 520, 33), (1000, 3, 1023), (1024, 16, 1024),
+    (1025, 16, 1025), (2049, 4, 5000), (5000, 40, 100), (40000, 12, 20000), (513, 1030, 600)])
+@pytest.mark.parametrize("spread", ["zipf", "even", "one"])
+def test_grad_sizes(rows, width, tokens, spread):
+    rng = np.random.default_rng(rows + tokens)
+    ids = zipf(rng, rows, tokens) if spread == "zipf" else rng.integers(0, rows, tokens) if spread == "even" else np.full(tokens, rows - 1)
+    check_grad(rows, width, ids, BF16, FP32)
+
+
+@pytest.mark.parametrize("tokens", [0, 1, 31, 32, 33, 63, 64, 65, 96, 97, 4095, 4096, 4097])
+def test_grad_of_one_row(tokens):
+    """Every length at which a row's tokens are split or end a part, next to rows with one token."""
+    ids = np.concatenate([[0], np.full(tokens, 1), [3]])
+    check_grad(5, 20, ids, FP32, FP32)
+
+
+@pytest.mark.parametrize("lengths", [(33, 33, 33), (40, 1, 40), (32, 33, 31, 64), (1, 100, 1, 100), (33, 31, 33, 31, 1)])
+def test_grad_rows_that_meet_in_a_window(lengths):
+    ids = np.concatenate([np.full(n, r) for r, n in enumerate(lengths)])
+    for seed in range(2):
+        check_grad(len(lengths), 24, np.random.default_rng(seed).permutation(ids), BF16, BF16, seed=seed)
+
+
+@pytest.mark.parametrize("padding", [-1, 0, 6])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("bits", [32, 64])
+def test_grad_padding_is_not_read(padding, add, bits):
+    """Rows of dout whose token takes no part hold NaN, and so does the gradient that is overwritten."""
+    rng = np.random.default_rng(3)
+    ids = rng.integers(-3, 12, 500)
+    ids[7], ids[8] = (2 ** 31 - 1, -2 ** 31) if bits == 32 else (2 ** 40, -2 ** 50)
+    check_grad(9, 77, ids, BF16, FP32, padding=padding, add=add, bits=bits, poison=True)
+
+
+def test_grad_without_a_token_that_counts():
+    got = check_grad(9, 33, np.full(700, 4), FP32, FP16, padding=4, poison=True)
+    assert (got == 0).all()
+    check_grad(9, 33, np.full(700, -1), FP32, FP16, add=True)
+    check_grad(9, 33, [], FP32, FP16, poison=True)
+    check_grad(9, 33, [], FP32, FP16, add=True)
+
+
+@pytest.mark.parametrize("gaps,shifts", [((3, 0), (0, 1)), ((0, 5), (1, 3)), ((1, 1), (1, 0)), ((8, 8), (4, 4))])
+@pytest.mark.parametrize("dt", [FP32, FP16])
+def test_grad_strides_and_alignments(gaps, shifts, dt):
+    rng = np.random.default_rng(4)
+    check_grad(61, 131, zipf(rng, 61, 400), dt, dt, gaps=gaps, shifts=shifts)
+    check_grad(61, 131, zipf(rng, 61, 400), dt, dt, gaps=gaps, shifts=shifts, add=True)
+
+
+def test_grad_values_that_are_not_finite_stay_in_their_row():
+    torch, _ = lib()
+    dout = torch.ones((40, 16), device="cuda")
+    dout[3, 5], dout[9, 2] = float("inf"), float("nan")
+    grad = torch.empty((6, 16), device="cuda")
+    ids = ids_on([i % 4 for i in range(40)], 64)
+    t = Table(6, 16, 40)
+    t.grad(ids, dout, FP32, grad, FP32, 1.0)
+    torch.cuda.synchronize()
+    bad = (~torch.isfinite(grad)).nonzero().cpu().tolist()
+    assert bad == [[1, 2], [3, 5]]
+    t.close()
+
+
+def test_grad_calls_do_not_see_each_other():
+    """One handle, calls of different lengths and spreads in turn: nothing of a longer call is left."""
+    rng = np.random.default_rng(5)
+    t = Table(3000, 48, 30000)
+    for k, tokens in enumerate((30000, 10, 0, 5000, 1, 29999, 1024)):
+        ids = zipf(rng, 3000, tokens) if k % 2 else rng.integers(-5, 3000, tokens)
+        check_grad(3000, 48, ids, BF16, FP32, seed=k, table=t)
+    t.close()
+
+
+def test_grad_same_bits_every_time():
+    torch, _ = lib()
+    rng = np.random.default_rng(6)
+    ids = ids_on(zipf(rng, 2000, 20000), 64)
+    dout = torch.randn((20000, 136), device="cuda")
+    t = Table(2000, 136, 20000)
+    out = []
+    for _ in range(3):
+        grad = torch.empty((2000, 136), device="cuda")
+        t.grad(ids, dout, FP32, grad, FP32)
+        torch.cuda.synchronize()
+        out.append(grad)
+    assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+    t.close()
+
+
+def test_grad_against_differences():
+    """The gradient of sum(w * lookup(table)) against differences of the library's own lookup.  Small whole numbers
+    and a step of 1 make every value exact, so the two are equal."""
+    torch, d = lib()
+    rng = np.random.default_rng(7)
+    rows, width, T = 7, 5, 60
+    ids = ids_on(rng.integers(-1, rows + 1, T), 64)
+    w = torch.from_numpy(rng.integers(-4, 5, (T, width)).astype(np.float32)).cuda()
+    table = torch.from_numpy(rng.integers(-4, 5, (rows, width)).astype(np.float32)).cuda()
+    grad = torch.empty_like(table)
+    t = Table(rows, width, T)
+    t.grad(ids, w, FP32, grad, FP32, 2.0)
+
+    def loss(x):
+        out = torch.empty((T, width), device="cuda")
+        d.ddp_embedding_lookup(t.emb, T, ids.data_ptr(), 64, x.data_ptr(), FP32, width, 2.0, out.data_ptr(), FP32, width)
+        return (out.double() * w.double()).sum().item()
+    base = loss(table)
+    for r in range(rows):
+        for c in range(width):
+            up = table.clone()
+            up[r, c] += 1.0
+            assert loss(up) - base == grad[r, c].item()
+    t.close()
+
+
+def test_grad_captured():
+    """Replays of a captured call, with other tokens and eager work in between."""
+    torch, _ = lib()
+    stream = torch.cuda.Stream()
+    rng = np.random.default_rng(8)
+    a, b = Table(300, 64, 3000, stream.cuda_stream), Table(300, 64, 3000)
+    ids = ids_on(zipf(rng, 300, 3000), 64)
+    dout = torch.randn((3000, 64), device="cuda", dtype=torch.bfloat16)
+    one, two = torch.empty((300, 64), device="cuda"), torch.empty((300, 64), device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        a.grad(ids, dout, BF16, one, FP32)
+    for k in range(4):
+        ids.copy_(torch.from_numpy(zipf(rng, 300, 3000)))
+        dout.normal_()
+        one.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        b.grad(ids, dout, BF16, two, FP32)
+        torch.cuda.synchronize()
+        assert torch.equal(one, two), k
+    a.close()
+    b.close()

@@ -1,0 +1,503 @@
+"""The global gradient norm and the AdamW step, through the C ABI, against the 64-bit oracle on
+the same inputs.  Tolerances come from counting roundings: u = 2^-24 is one of binary32, a 16-bit
+result adds one of its own type.  After a step the moments may be off by 6 u (first) and 8 u (second) of the
+magnitudes that were added, the update by 24 u of its magnitude (moments 6 + 4, root 2, bias correction 2, eps 2,
+reciprocal 2, product 1, rate 2, sum 1, and what is left over), and a parameter by 4 u of itself."""
+import numpy as np
+import pytest
+
+from oracle import operators as ops
+
+pytestmark = pytest.mark.gpu
+
+FP32, FP16, BF16 = 0, 1, 2
+U = 2.0 ** -24
+UNIT = {FP32: 0.0, FP16: 2.0 ** -11, BF16: 2.0 ** -8}      # one rounding to the type (a binary32 result's are counted)
+TINY = {FP32: 0.0, FP16: 2.0 ** -25, BF16: 0.0}            # half the smallest subnormal
+NUMEL = [1, 3, 255, 256, 257, 0, 4096, 4097, 10000, 70]
+HYPER = dict(lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.1)
+
+
+def lib():
+    import torch
+    import paper_2006_15704_amd as d
+    return torch, d
+
+
+def torch_type(torch, dt):
+    return {FP32: torch.float32, FP16: torch.float16, BF16: torch.bfloat16}[dt]
+
+
+class Flat:
+    """Tensors of one buffer, `skew` elements between them, with guard values around each."""
+
+    def __init__(self, numel, dt, values=None, skew=1):
+        torch, _ = lib()
+        self.numel, self.dt = list(numel), dt
+        self.at, off = [], 8
+        for n in numel:
+            self.at.append(off)
+            off += n + skew
+        self.buf = torch.full((off + 64,), 7.0, dtype=torch_type(torch, dt), device="cuda")
+        if values is not None:
+            for i, x in enumerate(values):
+                self.view(i).copy_(torch.from_numpy(np.asarray(x, dtype=np.float64)))
+
+    def view(self, i):
+        return self.buf[self.at[i]:self.at[i] + self.numel[i]]
+
+    def ptrs(self):
+        return [self.buf.data_ptr() + o * self.buf.element_size() for o in self.at]
+
+    def host(self):
+        return [self.view(i).double().cpu().numpy() for i in range(len(self.numel))]
+
+    def guards_hold(self):
+        keep = self.buf.double().cpu().numpy().copy()
+        for i, n in enumerate(self.numel):
+            keep[self.at[i]:self.at[i] + n] = 7.0
+        return (keep == 7.0).all()
+
+
+class Program:
+    """Parameters, gradients, copies and a state, as a training program has them."""
+
+    def __init__(self, numel=NUMEL, param=FP32, grad=FP32, copy=None, bits=32, skew=1, seed=0, sigma=1e-2, lr_scale=None,
+                 decay_scale=None, steps=0, stream=0):
+        torch, d = lib()
+        rng = np.random.default_rng(seed)
+        self.numel, self.bits, self.n = list(numel), bits, len(numel)
+        self.p = Flat(numel, param, [rng.standard_normal(k) * 0.1 for k in numel], skew)
+        self.g = Flat(numel, grad, [rng.standard_normal(k) * sigma for k in numel], skew)
+        self.c = None if copy is None else Flat(numel, copy, None, skew)
+        self.lr_scale = [1.0] * self.n if lr_scale is None else lr_scale
+        self.decay_scale = [1.0] * self.n if decay_scale is None else decay_scale
+        kind = d.DDP_STATE_FP32 if bits == 32 else d.DDP_STATE_8BIT
+        self.offset, self.where = d.ddp_opt_state_layout(self.numel, kind)
+        self.state = torch.zeros(self.where["bytes"] + 256, dtype=torch.uint8, device="cuda")
+        self.state[self.where["bytes"]:] = 0xA5
+        self.state[:8].view(torch.int64).fill_(steps)
+        self.opt = d.ddp_opt_create(0, stream)
+        d.ddp_opt_register(self.opt, self.numel, [param] * self.n, self.p.ptrs(), [grad] * self.n, self.g.ptrs())
+        d.ddp_opt_set_groups(self.opt, lr_scale, decay_scale)
+        if copy is not None:
+            d.ddp_opt_set_copies(self.opt, [copy] * self.n, self.c.ptrs())
+        d.ddp_opt_set_state(self.opt, kind, self.state.data_ptr(), self.where["bytes"])
+        torch.cuda.synchronize()
+
+    def steps(self):
+        torch, _ = lib()
+        return int(self.state[:8].view(torch.int64).item())
+
+    def part(self, name, dtype, count):
+        size = np.dtype(dtype).itemsize
+        a = self.where[name]
+        return self.state[a:a + count * size].cpu().numpy().view(dtype)
+
+    def codes(self):
+        """8-bit state: (first codes, second codes, first tops, second tops), whole."""
+        e = self.where["elems"]
+        return (self.part("m", np.int8, e), self.part("v", np.uint8, e), self.part("m_top", np.float32, e // 256),
+                self.part("v_top", np.float32, e // 256))
+
+    def moments(self):
+        """Per tensor (m, v) in 64 bits, as the state stands for them."""
+        e = self.where["elems"]
+        if self.bits == 32:
+            m, v = self.part("m", np.float32, e).astype(np.float64), self.part("v", np.float32, e).astype(np.float64)
+        else:
+            mc, vc, mt, vt = self.codes()
+            m, v = ops.held_first(mc, mt), ops.held_second(vc, vt)
+        return [(m[o:o + n], v[o:o + n]) for o, n in zip(self.offset, self.numel)]
+
+    def close(self):
+        _, d = lib()
+        d.ddp_opt_destroy(self.opt)
+
+    def guards_hold(self):
+        tail = self.state[self.where["bytes"]:].cpu().numpy()
+        return (self.p.guards_hold() and self.g.guards_hold() and (self.c is None or self.c.guards_hold()) and (tail == 0xA5).all())
+
+
+def check_step(prog, do_step, hyper=HYPER, grad_scale=1.0, max_norm=0.0, used=None, what=""):
+    """Runs do_step() and compares every parameter, copy and moment with the oracle."""
+    torch, _ = lib()
+    p0, g0, s0 = prog.p.host(), prog.g.host(), prog.moments()
+    norm = ops.grad_norm([g for i, g in enumerate(g0) if used is None or used[i]])
+    t = prog.steps() + 1
+    do_step()
+    torch.cuda.synchronize()
+    assert prog.steps() == t, what
+    p1, s1 = prog.p.host(), prog.moments()
+    codes = prog.codes() if prog.bits == 8 else None
+    clip = min(1.0, max_norm / (abs(grad_scale) * norm + 1e-6)) if max_norm > 0 else 1.0
+    dt = prog.p.dt
+    for i, n in enumerate(prog.numel):
+        tag = f"{what} tensor {i} of {n}"
+        (m0, v0), (m1, v1) = s0[i], s1[i]
+        if used is not None and not used[i]:
+            assert (p1[i] == p0[i]).all() and (m1 == m0).all() and (v1 == v0).all(), tag
+            continue
+        lr, decay = hyper["lr"] * prog.lr_scale[i], hyper["weight_decay"] * prog.decay_scale[i]
+        b1, b2, eps = hyper["beta1"], hyper["beta2"], hyper["eps"]
+        p, m, v = ops.adamw(p0[i], g0[i], m0, v0, t, lr, b1, b2, eps, decay, grad_scale, max_norm, norm)
+        added = np.abs(b1 * m0) + np.abs((1 - b1) * g0[i] * grad_scale * clip)
+        denom = np.sqrt(v / (1 - b2 ** t)) + eps
+        extra = 8 if prog.bits == 8 else 0                   # decoding: 3 roundings of the first, 4 of the second moment
+        tol = (24 + extra) * U * abs(lr) / (1 - b1 ** t) * added / denom + 4 * U * (np.abs(p0[i]) + np.abs(p))
+        assert (np.abs(p1[i] - p) <= tol + UNIT[dt] * np.abs(p) + TINY[dt]).all(), tag
+        if prog.c is not None:
+            c1 = prog.c.view(i).double().cpu().numpy()
+            assert (np.abs(c1 - p) <= tol + UNIT[prog.c.dt] * np.abs(p) + TINY[prog.c.dt]).all(), tag
+            assert (c1 == prog.p.view(i).to(prog.c.buf.dtype).double().cpu().numpy()).all(), tag + ": the copy is the parameter, rounded once"
+        if prog.bits == 32:
+            assert (np.abs(m1 - m) <= 6 * U * added).all(), tag
+            assert (np.abs(v1 - v) <= 8 * U * v + 2.0 ** -149).all(), tag
+            continue
+        o, blocks = prog.offset[i], slice(prog.offset[i] // 256, (prog.offset[i] + n + 255) // 256)
+        mc, vc, mt, vt = codes[0][o:o + n], codes[1][o:o + n], codes[2][blocks], codes[3][blocks]
+        want, tops, root = ops.nearest_first(m)
+        most = ops._tops(added)
+        assert (np.abs(mt - tops) <= 9 * U * most).all(), tag
+        top = np.repeat(tops, 256)[:n]
+        # how far 9 u of what was added (and of the top) moves the root, and 4 roundings on the way
+        off = np.where(top > 0, 127 * (9 * U * np.repeat(most, 256)[:n] / np.maximum(top, 1e-300)) / np.maximum(root / 127, 0.5 / 127), 0) + 127 * 4 * U
+        low, high = np.floor(np.maximum(root - off, 0) + 0.5), np.floor(root + off + 0.5)
+        assert ((np.abs(mc) >= np.minimum(low, 127)) & (np.abs(mc) <= np.minimum(high, 127))).all(), tag
+        sure = np.abs(m) > 9 * U * np.repeat(most, 256)[:n]
+        assert ((np.sign(mc) == np.sign(m)) | (mc == 0))[sure].all(), tag
+        want, tops, root = ops.nearest_second(v)
+        assert (np.abs(vt - tops) <= 12 * U * tops).all(), tag
+        off = 255 * 16 * U
+        low, high = np.maximum(np.floor(root - off + 0.5), 1), np.maximum(np.floor(root + off + 0.5), 1)
+        assert (np.where(v > 0, (vc >= low) & (vc <= np.minimum(high, 255)), vc == 0)).all(), tag
+
+
+def step(prog, hyper=HYPER, **more):
+    _, d = lib()
+    d.ddp_opt_adamw_step(prog.opt, hyper["lr"], hyper["beta1"], hyper["beta2"], hyper["eps"], hyper["weight_decay"], **more)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,grad,copy", [(FP32, FP32, None), (FP32, FP16, FP16), (FP32, BF16, BF16), (FP32, FP32, BF16),
+                                             (FP16, FP16, None), (BF16, BF16, None), (BF16, FP32, None), (FP16, BF16, None)])
+def test_steps_over_types(param, grad, copy, bits):
+    prog = Program(param=param, grad=grad, copy=copy, bits=bits, seed=param * 9 + grad * 3)
+    for k in range(3):
+        check_step(prog, lambda: step(prog), what=f"step {k}")
+    assert prog.guards_hold()
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("skew", [0, 1, 2, 3, 8])
+def test_alignments(skew, bits):
+    prog = Program(numel=[5, 4096 + 3, 8192, 1, 777], grad=FP16, copy=BF16, bits=bits, skew=skew, seed=skew)
+    for k in range(2):
+        check_step(prog, lambda: step(prog), what=f"skew {skew} step {k}")
+    assert prog.guards_hold()
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_groups_and_later_steps(bits):
+    n = len(NUMEL)
+    prog = Program(bits=bits, lr_scale=[0.5 if i % 3 else 2.0 for i in range(n)], decay_scale=[float(i % 2) for i in range(n)],
+                   steps=100000)
+    for k in range(2):
+        check_step(prog, lambda: step(prog), what=f"step {k}")
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("beta1,beta2,eps,decay", [(0.0, 0.0, 1e-6, 0.0), (0.95, 0.9999, 1e-12, 0.0), (0.5, 0.5, 1.0, 1.0)])
+def test_hyperparameters(beta1, beta2, eps, decay, bits):
+    hyper = dict(lr=3e-3, beta1=beta1, beta2=beta2, eps=eps, weight_decay=decay)
+    prog = Program(bits=bits, seed=5)
+    for k in range(2):
+        check_step(prog, lambda: step(prog, hyper), hyper, what=f"step {k}")
+    prog.close()
+
+
+def test_types_that_differ_from_tensor_to_tensor():
+    """Parameters of all types in one list, some with copies: each has a launch of its own, the step counts once."""
+    torch, d = lib()
+    rng = np.random.default_rng(8)
+    numel = [300, 5000, 7, 4096, 513, 1]
+    pt, gt = [FP32, BF16, FP32, FP16, FP32, BF16], [FP32, BF16, BF16, FP16, FP16, FP32]
+    ps = [Flat([n], t, [rng.standard_normal(n)]) for n, t in zip(numel, pt)]
+    gs = [Flat([n], t, [rng.standard_normal(n)]) for n, t in zip(numel, gt)]
+    copies = [Flat([n], BF16) if t == FP32 and n != 7 else None for n, t in zip(numel, pt)]
+    p0, g0 = [x.host()[0] for x in ps], [x.host()[0] for x in gs]
+    offset, where = d.ddp_opt_state_layout(numel, d.DDP_STATE_FP32)
+    state = torch.zeros(where["bytes"], dtype=torch.uint8, device="cuda")
+    opt = d.ddp_opt_create(0)
+    d.ddp_opt_register(opt, numel, pt, [x.ptrs()[0] for x in ps], gt, [x.ptrs()[0] for x in gs])
+    d.ddp_opt_set_copies(opt, [BF16] * 6, [None if c is None else c.ptrs()[0] for c in copies])
+    d.ddp_opt_set_state(opt, d.DDP_STATE_FP32, state.data_ptr(), where["bytes"])
+    torch.cuda.synchronize()
+    d.ddp_opt_adamw_step(opt, 1e-2, weight_decay=0.1)
+    torch.cuda.synchronize()
+    assert int(state[:8].view(torch.int64).item()) == 1
+    for i in range(6):
+        p, _, _ = ops.adamw(p0[i], g0[i], 0 * p0[i], 0 * p0[i], 1, 1e-2, 0.9, 0.999, 1e-8, 0.1)
+        got = ps[i].host()[0]
+        tol = 24 * U * 1e-2 * 1.01 + 4 * U * (np.abs(p0[i]) + np.abs(p))
+        assert (np.abs(got - p) <= tol + UNIT[pt[i]] * np.abs(p) + TINY[pt[i]]).all(), i
+        if copies[i] is not None:
+            assert (copies[i].host()[0] == ps[i].view(0).bfloat16().double().cpu().numpy()).all(), i
+    d.ddp_opt_destroy(opt)
+
+
+@pytest.mark.parametrize("grad", [FP32, FP16, BF16])
+@pytest.mark.parametrize("sigma", [1e-3, 1.0])
+def test_norm(grad, sigma):
+    """Squares are summed in 64 bits; the result is rounded once."""
+    torch, d = lib()
+    prog = Program(numel=[1, 70001, 0, 4096, 333], grad=grad, sigma=sigma, seed=grad)
+    out = torch.zeros(1, dtype=torch.float32, device="cuda")
+    for scale in (1.0, -0.25):
+        d.ddp_opt_grad_norm(prog.opt, scale, out.data_ptr())
+        torch.cuda.synchronize()
+        want = abs(scale) * ops.grad_norm(prog.g.host())
+        assert abs(out.item() - want) <= 2 * U * want
+    used = [0, 1, 1, 0, 1]
+    d.ddp_opt_grad_norm(prog.opt, 1.0, out.data_ptr(), used)
+    torch.cuda.synchronize()
+    want = ops.grad_norm([g for g, u in zip(prog.g.host(), used) if u])
+    assert abs(out.item() - want) <= 2 * U * want
+    prog.close()
+
+
+def test_norm_of_large_and_small_gradients():
+    """1e30 squared is no binary32, 1e-30 squared is 0 in it."""
+    torch, d = lib()
+    out = torch.zeros(1, dtype=torch.float32, device="cuda")
+    for value in (1e30, 1e-30):
+        prog = Program(numel=[1000], grad=BF16)
+        prog.g.view(0).fill_(value)
+        held = float(prog.g.view(0)[0].double().item())
+        d.ddp_opt_grad_norm(prog.opt, 1.0, out.data_ptr())
+        torch.cuda.synchronize()
+        want = held * np.sqrt(1000.0)
+        assert abs(out.item() - want) <= 2 * U * want
+        prog.close()
+
+
+def test_norm_without_parameters():
+    """A program with a step of its own registers gradients alone."""
+    torch, d = lib()
+    g = Flat([100, 5000], FP16, [np.ones(100), np.full(5000, 2.0)])
+    opt = d.ddp_opt_create(0)
+    d.ddp_opt_register(opt, [100, 5000], [FP16, FP16], None, [FP16, FP16], g.ptrs())
+    out = torch.zeros(1, dtype=torch.float32, device="cuda")
+    torch.cuda.synchronize()
+    d.ddp_opt_grad_norm(opt, 1.0, out.data_ptr())
+    torch.cuda.synchronize()
+    assert abs(out.item() - np.sqrt(20100.0)) <= 2 * U * np.sqrt(20100.0)
+    with pytest.raises(d.DdpError) as e:
+        d.ddp_opt_set_state(opt, d.DDP_STATE_FP32, 256, 1 << 20)
+    assert e.value.code == d.DDP_ERR_STATE
+    d.ddp_opt_destroy(opt)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad_scale,max_norm", [(1.0, 0.05), (1.0, 1e6), (1.0 / 1024, 1e-4), (-2.0, 0.1)])
+def test_clipping(grad_scale, max_norm, bits):
+    _, d = lib()
+    prog = Program(bits=bits, seed=2)
+
+    def both():
+        d.ddp_opt_grad_norm(prog.opt, grad_scale)
+        step(prog, grad_scale=grad_scale, max_norm=max_norm)
+    for k in range(2):
+        check_step(prog, both, grad_scale=grad_scale, max_norm=max_norm, what=f"step {k}")
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_unused_parameters(bits):
+    _, d = lib()
+    prog = Program(bits=bits, seed=4)
+    check_step(prog, lambda: step(prog))
+    used = [i % 3 != 1 for i in range(prog.n)]
+
+    def both():
+        d.ddp_opt_grad_norm(prog.opt, 1.0, 0, used)
+        step(prog, max_norm=0.1, used=used)
+    check_step(prog, both, max_norm=0.1, used=used)
+    check_step(prog, lambda: step(prog, used=[1] * prog.n))
+    prog.close()
+
+
+def test_many_small_tensors_and_a_mask():
+    """More tensors than one launch's mask words hold."""
+    _, d = lib()
+    n = 768 * 32 + 100
+    prog = Program(numel=[1] * n, skew=0)
+    used = (np.arange(n) % 7 != 0).astype(np.uint8)
+    before = prog.p.buf.clone()
+    step(prog, used=used)
+    moved = (prog.p.buf != before).cpu().numpy()[8:8 + n]
+    assert (moved == (used != 0)).all()
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_skipping_what_is_not_finite(bits, bad):
+    torch, d = lib()
+    prog = Program(bits=bits, seed=6, copy=BF16)
+    check_step(prog, lambda: step(prog))
+    keep = prog.g.view(7)[4000].clone()
+    prog.g.view(7)[4000] = bad
+    held = [x.clone() for x in (prog.p.buf, prog.c.buf, prog.state)]
+    d.ddp_opt_grad_norm(prog.opt)
+    step(prog, skip_nonfinite=True, max_norm=1.0)
+    torch.cuda.synchronize()
+    for x, y in zip(held, (prog.p.buf, prog.c.buf, prog.state)):
+        assert torch.equal(x, y)
+    prog.g.view(7)[4000] = keep
+
+    def both():
+        d.ddp_opt_grad_norm(prog.opt)
+        step(prog, skip_nonfinite=True, max_norm=1.0)
+    check_step(prog, both, max_norm=1.0)
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_what_is_not_finite_stays_where_it_is(bits):
+    """Without skipping: its element (8 bits: its block of 256) and nothing else."""
+    torch, _ = lib()
+    prog = Program(numel=[2000], bits=bits, seed=6)
+    prog.g.view(0)[600] = float("nan")
+    step(prog)
+    p = prog.p.host()[0]
+    bad = np.flatnonzero(~np.isfinite(p))
+    assert 600 in bad and (bad.tolist() == [600] if bits == 32 else ((bad >= 512) & (bad < 768)).all())
+    step(prog)
+    bad = np.flatnonzero(~np.isfinite(prog.p.host()[0]))
+    assert 600 in bad and (bad.tolist() == [600] if bits == 32 else ((bad >= 512) & (bad < 768)).all())
+    prog.close()
+
+
+def test_tiny_and_empty_blocks():
+    """Gradients of zero and below the normal range: nothing blows up, and blocks of zeros stay zeros."""
+    prog = Program(numel=[1024], bits=8)
+    prog.g.view(0).zero_()
+    prog.g.view(0)[256:512] = 1e-25          # v about 1e-53: no binary32
+    prog.g.view(0)[512:768] = 1e-40
+    p0 = prog.p.host()[0]
+    hyper = dict(HYPER, weight_decay=0.0)
+    step(prog, hyper)
+    p1 = prog.p.host()[0]
+    mc, vc, mt, vt = prog.codes()
+    assert np.isfinite(p1).all() and (p1[:256] == p0[:256]).all()
+    assert (mc[:256] == 0).all() and (vc[:256] == 0).all() and mt[0] == 0 and vt[0] == 0
+    assert (mc[256:512] == 127).all() and vt[1] == 0 and (vc[256:512] == 0).all()
+    assert mt[2] == 0 and (mc[512:768] == 0).all()
+    prog.close()
+
+
+def test_small_second_moments_are_kept():
+    """One large gradient in a block must not make the others' second moments vanish: a step later they
+    would be divided by next to nothing."""
+    prog = Program(numel=[256], bits=8)
+    prog.g.view(0).fill_(1e-6)
+    prog.g.view(0)[0] = 1e3
+    step(prog)
+    _, vc, _, _ = prog.codes()
+    assert vc[0] == 255 and (vc[1:] == 1).all()
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_same_bits_every_time(bits):
+    torch, d = lib()
+    results = []
+    for _ in range(2):
+        prog = Program(numel=[300000, 17, 5000], grad=BF16, copy=BF16, bits=bits, seed=11)
+        for _ in range(3):
+            d.ddp_opt_grad_norm(prog.opt)
+            step(prog, max_norm=0.5)
+        torch.cuda.synchronize()
+        results.append((prog.p.buf.clone(), prog.c.buf.clone(), prog.state.clone()))
+        prog.close()
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
+
+
+def test_launches_of_more_blocks_than_count_themselves():
+    """Above some thousand blocks another launch counts the step; a large tensor between small ones."""
+    prog = Program(numel=[9, 5 * 1024 * 1024 + 1, 3000], seed=12, skew=0)
+    for k in range(2):
+        check_step(prog, lambda: step(prog), what=f"step {k}")
+    prog.close()
+
+
+def test_read_state():
+    torch, d = lib()
+    prog = Program(bits=8, seed=13)
+    for _ in range(2):
+        step(prog)
+    e = prog.where["elems"]
+    m, v = torch.full((e,), 9.0, device="cuda"), torch.full((e,), 9.0, device="cuda")
+    d.ddp_opt_read_state(prog.opt, m.data_ptr(), v.data_ptr())
+    torch.cuda.synchronize()
+    mc, vc, mt, vt = prog.codes()
+    np.testing.assert_allclose(m.cpu().numpy(), ops.held_first(mc, mt), rtol=4 * U)
+    np.testing.assert_allclose(v.cpu().numpy(), ops.held_second(vc, vt), rtol=5 * U)
+    m.fill_(9.0)
+    d.ddp_opt_read_state(prog.opt, m.data_ptr(), 0)
+    torch.cuda.synchronize()
+    np.testing.assert_allclose(m.cpu().numpy(), ops.held_first(mc, mt), rtol=4 * U)
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_steps(bits):
+    """A graph of norm and step, replayed several times with eager work in between: the count of steps goes on and
+    every replay does what the eager calls do."""
+    torch, d = lib()
+    stream = torch.cuda.Stream()
+    progs = [Program(numel=[5000, 300, 1], grad=BF16, copy=BF16, bits=bits, seed=14, stream=stream.cuda_stream) for _ in range(2)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        d.ddp_opt_grad_norm(progs[0].opt)
+        step(progs[0], max_norm=0.1, skip_nonfinite=True)
+    for k in range(5):
+        for prog in progs:
+            gen = torch.Generator("cuda").manual_seed(k)
+            for i in range(3):
+                prog.g.view(i).normal_(0.0, 0.01, generator=gen)
+        torch.cuda.synchronize()
+        graph.replay()
+        d.ddp_opt_grad_norm(progs[1].opt)
+        step(progs[1], max_norm=0.1, skip_nonfinite=True)
+        torch.cuda.synchronize()
+        for x, y in zip(*[(q.p.buf, q.c.buf, q.state) for q in progs]):
+            assert torch.equal(x, y), k
+        assert progs[0].steps() == k + 1
+    for prog in progs:
+        prog.close()
+
+
+def test_moments_in_8_bits_follow_those_in_32():
+    """300 steps on noisy gradients of a fixed mean: the updates of the two stay together.  A code is off by at most 1.2 %
+    of a first moment near its block's top; summed over steps the parameters agree to a few per cent of the way they went."""
+    torch, d = lib()
+    a, b = (Program(numel=[4096], bits=bits, seed=15) for bits in (32, 8))
+    start = a.p.host()[0]
+    gen = torch.Generator("cuda").manual_seed(1)
+    mean = torch.empty(4096, device="cuda").normal_(0.0, 0.02, generator=gen)
+    hyper = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0)
+    for _ in range(300):
+        g = mean + torch.empty(4096, device="cuda").normal_(0.0, 0.01, generator=gen)
+        for prog in (a, b):
+            prog.g.view(0).copy_(g)
+            step(prog, hyper)
+    way, off = a.p.host()[0] - start, b.p.host()[0] - a.p.host()[0]
+    assert np.linalg.norm(off) <= 0.05 * np.linalg.norm(way)
+    for prog in (a, b):
+        prog.close()

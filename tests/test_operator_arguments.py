@@ -1,0 +1,159 @@
+"""What the optimizer and embedding calls refuse, on handles without a device: arguments, order of calls, and the
+binding's own checks of lengths."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+FP32, FP16, BF16 = 0, 1, 2
+
+
+@pytest.fixture(scope="module")
+def d():
+    import paper_2006_15704_amd as lib
+    return lib
+
+
+def refused(d, code, call, *args, **more):
+    with pytest.raises(d.DdpError) as e:
+        call(*args, **more)
+    assert e.value.code == code, e.value
+    assert len(str(e.value)) > len(f"ddp error {code}: "), "no text"
+
+
+@pytest.fixture
+def opt(d):
+    h = d.ddp_opt_create(d.DDP_DEVICE_NONE)
+    yield h
+    d.ddp_opt_destroy(h)
+
+
+@pytest.fixture
+def emb(d):
+    h = d.ddp_embedding_create(d.DDP_DEVICE_NONE, 0, 100, 16, 1000)
+    yield h
+    d.ddp_embedding_destroy(h)
+
+
+def test_state_layout(d):
+    offset, where = d.ddp_opt_state_layout([1, 0, 256, 257, 5], d.DDP_STATE_FP32)
+    assert offset.tolist() == [0, 256, 256, 512, 1024]
+    assert where == {"m": 256, "v": 256 + 4 * 1280, "m_top": 0, "v_top": 0, "elems": 1280, "bytes": 256 + 8 * 1280}
+    offset, where = d.ddp_opt_state_layout([1, 0, 256, 257, 5], d.DDP_STATE_8BIT)
+    assert where == {"m": 256, "v": 256 + 1280, "m_top": 256 + 2560, "v_top": 512 + 2560, "elems": 1280, "bytes": 768 + 2560}
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_state_layout, [1, -1], 0)
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_state_layout, [1], 2)
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_state_layout, [], 0)
+
+
+def test_optimizer_order(d, opt):
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_set_groups, opt)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_set_copies, opt, [], [])
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_set_state, opt, 0, 256, 1 << 20)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_grad_norm, opt)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_adamw_step, opt, 1e-3)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_read_state, opt, 256, 256)
+    d.ddp_opt_register(opt, [10, 300], [FP32, FP32], None, [BF16, FP32], None)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_register, opt, [10], [FP32], None, [FP32], None)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_adamw_step, opt, 1e-3)
+    d.ddp_opt_set_groups(opt, [1.0, 2.0], None)
+    d.ddp_opt_set_copies(opt, [BF16, BF16], [256, None])
+    d.ddp_opt_set_state(opt, d.DDP_STATE_8BIT, 0, 1 << 20)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_set_state, opt, d.DDP_STATE_8BIT, 0, 1 << 20)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_set_groups, opt)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_set_copies, opt, [BF16, BF16], [256, None])
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_opt_grad_norm, opt)
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_opt_adamw_step, opt, 1e-3)
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_opt_read_state, opt, 256, 256)
+
+
+@pytest.mark.parametrize("numel,pt,pp,gt,gp", [
+    ([], [], None, [], None),
+    ([-1], [FP32], None, [FP32], None),
+    ([1 << 50], [FP32], None, [FP32], None),
+    ([1 << 47, 1 << 47, 1 << 47], [FP32] * 3, None, [FP32] * 3, None),
+    ([5], [3], None, [FP32], None),
+    ([5], [FP32], None, [-1], None),
+    ([5], [FP32], [0], [FP32], None),
+    ([5], [FP32], [258], [FP32], None),
+    ([5], [FP32], None, [BF16], [257]),
+    ([5], [FP32], None, [BF16], [0]),
+])
+def test_registration(d, opt, numel, pt, pp, gt, gp):
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_register, opt, numel, pt, pp, gt, gp)
+
+
+def test_empty_tensors_need_no_address(d, opt):
+    d.ddp_opt_register(opt, [0, 4], [FP32, FP16], [0, 256], [FP32, FP16], [0, 256])
+
+
+def test_options_of_the_optimizer(d, opt):
+    d.ddp_opt_register(opt, [10, 300], [FP32, BF16], None, [FP32, BF16], None)
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_set_groups, opt, [1.0, float("nan")], None)
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_set_groups, opt, None, [float("inf"), 1.0])
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_set_copies, opt, [FP32, BF16], [256, None])
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_set_copies, opt, [BF16, BF16], [None, 256])     # of a 16-bit parameter
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_set_copies, opt, [BF16, BF16], [257, None])
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_set_state, opt, 2, 256, 1 << 20)
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_set_state, opt, 0, 256, 100)
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_set_state, opt, 0, 264, 1 << 20)
+    d.ddp_opt_set_state(opt, d.DDP_STATE_FP32, 256, 1 << 20)
+    refused(d, d.DDP_ERR_STATE, d.ddp_opt_read_state, opt, 256, 256)
+    inf, nan = float("inf"), float("nan")
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_grad_norm, opt, nan)
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_grad_norm, opt, 1.0, 258)
+    for bad in (dict(lr=nan), dict(lr=1.0, beta1=1.0), dict(lr=1.0, beta1=-0.1), dict(lr=1.0, beta2=1.0), dict(lr=1.0, beta2=nan),
+                dict(lr=1.0, eps=-1e-9), dict(lr=1.0, eps=inf), dict(lr=1.0, weight_decay=inf), dict(lr=1.0, grad_scale=nan),
+                dict(lr=1.0, max_norm=inf)):
+        refused(d, d.DDP_ERR_ARG, d.ddp_opt_adamw_step, opt, **bad)
+
+
+def test_lengths_are_checked_before_the_call(d, opt):
+    with pytest.raises(ValueError):
+        d.ddp_opt_register(opt, [1, 2], [FP32], None, [FP32, FP32], None)
+    with pytest.raises(ValueError):
+        d.ddp_opt_register(opt, [1, 2], [FP32, FP32], [256], [FP32, FP32], None)
+    d.ddp_opt_register(opt, [1, 2], [FP32, FP32], None, [FP32, FP32], None)
+    with pytest.raises(ValueError):
+        d.ddp_opt_set_groups(opt, [1.0], None)
+    with pytest.raises(ValueError):
+        d.ddp_opt_set_copies(opt, [BF16, BF16], [256])
+    with pytest.raises(ValueError):
+        d.ddp_opt_grad_norm(opt, 1.0, 0, [1])
+    with pytest.raises(ValueError):
+        d.ddp_opt_adamw_step(opt, 1e-3, used=np.ones(3))
+
+
+def test_null_handles(d):
+    lib = C.CDLL(d.binding.LIB_PATH)
+    for name in ("ddp_opt_destroy", "ddp_embedding_destroy"):
+        assert getattr(lib, name)(None) == d.DDP_ERR_ARG
+    assert lib.ddp_opt_create(None, -1, None) == d.DDP_ERR_ARG
+    assert lib.ddp_opt_register(None, 1, None, None, None, None, None) == d.DDP_ERR_ARG
+    lib.ddp_embedding_create.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int64]
+    assert lib.ddp_embedding_create(None, -1, None, 1, 1, 1) == d.DDP_ERR_ARG
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_create, -2)
+
+
+@pytest.mark.parametrize("rows,width,tokens,code", [(0, 1, 1, "ARG"), (1, 0, 1, "ARG"), (1, 1, -1, "ARG"), (2 ** 23 + 1, 1, 1, "UNSUPPORTED"),
+                                                    (1, 2 ** 20 + 1, 1, "UNSUPPORTED"), (1, 1, 2 ** 26 + 1, "UNSUPPORTED")])
+def test_embedding_sizes(d, rows, width, tokens, code):
+    refused(d, getattr(d, "DDP_ERR_" + code), d.ddp_embedding_create, -1, 0, rows, width, tokens)
+
+
+def test_lookup_arguments(d, emb):
+    def call(tokens=5, ids=256, bits=64, table=256, table_dt=FP32, table_stride=16, out=256, out_dt=FP32, out_stride=16):
+        return d.ddp_embedding_lookup(emb, tokens, ids, bits, table, table_dt, table_stride, 1.0, out, out_dt, out_stride)
+    refused(d, d.DDP_ERR_NO_DEVICE, call)
+    for bad in (dict(tokens=-1), dict(tokens=2 ** 27), dict(bits=16), dict(table_dt=3), dict(out_dt=-1), dict(table_stride=15),
+                dict(out_stride=0), dict(table_stride=2 ** 31)):
+        refused(d, d.DDP_ERR_ARG, call, **bad)
+
+
+def test_grad_arguments(d, emb):
+    def call(tokens=5, ids=256, bits=64, dout=256, dout_dt=FP32, dout_stride=16, padding=-1, grad=256, grad_dt=FP32, grad_stride=16):
+        return d.ddp_embedding_grad(emb, tokens, ids, bits, dout, dout_dt, dout_stride, 1.0, padding, False, grad, grad_dt, grad_stride)
+    refused(d, d.DDP_ERR_NO_DEVICE, call)
+    for bad in (dict(tokens=-1), dict(tokens=1001), dict(bits=8), dict(dout_dt=3), dict(grad_dt=-1), dict(dout_stride=15),
+                dict(grad_stride=15), dict(padding=100), dict(padding=-2)):
+        refused(d, d.DDP_ERR_ARG, call, **bad)
