@@ -599,9 +599,9 @@ int32_t ddp_opt_read_state(ddp_opt* opt, float* m_out, float* v_out);
  * ddp_opt.  All calls on a handle share the workspace and run on its stream. */
 typedef struct ddp_embedding ddp_embedding;
 
-/* A table of `rows` (up to 2^23) rows of `width` (up to 2^20) elements; max_tokens (up to 2^24): of a
- * ddp_embedding_grad call (0: lookups only).  The workspace takes 16 bytes and a
- * sixteenth of a binary32 row per token, and 4 bytes per row. */
+/* A table of `rows` (up to 2^23) rows of `width` (up to 2^20) elements; max_tokens (up to 2^22): of a
+ * ddp_embedding_grad call (0: lookups only).  The workspace takes 12 bytes and a
+ * sixteenth of a binary32 row per token, and 4 to 8 bytes per row. */
 int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, int64_t rows, int64_t width, int64_t max_tokens);
 int32_t ddp_embedding_destroy(ddp_embedding* emb);   /* waits for the handle's outstanding work */
 const char* ddp_embedding_last_error(const ddp_embedding* emb);

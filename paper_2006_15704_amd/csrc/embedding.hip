@@ -27,7 +27,7 @@ namespace {
 using namespace ddp;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int64_t kMaxRows = int64_t(1) << 23, kMaxTokens = int64_t(1) << 24, kMaxWidth = int64_t(1) << 20;
+constexpr int64_t kMaxRows = int64_t(1) << 23, kMaxTokens = int64_t(1) << 22, kMaxWidth = int64_t(1) << 20;
 
 template <typename Id>
 __device__ __forceinline__ int64_t row_of(const Id* ids, int64_t t) { return static_cast<int64_t>(*(DDP_GLOBAL_MEM const Id*)(ids + t)); }
@@ -49,11 +49,11 @@ struct Columns {
     }
 };
 
-template <int DT, int N>
+template <int DT, bool NT, int N>
 __device__ __forceinline__ void store_own(char* row, int at, int own, const float (&x)[N]) {
     char* to = row + at * ElemBytes<DT>::value;
     if (own == 0) {
-        store_some<DT, N>(to, N, x);
+        store_some<DT, N, NT>(to, N, x);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -63,24 +63,30 @@ __device__ __forceinline__ void store_own(char* row, int at, int own, const floa
 // N = 1 of a 16-bit type is half a dword: no vector access.
 template <int DT, int N> struct Vector {
     Parts<DT, N> raw;
-    __device__ __forceinline__ void load(const char* p) { raw = load_parts<DT, N>(p); }
+    template <bool NT = false>
+    __device__ __forceinline__ void load(const char* p) { raw = load_parts<DT, N, NT>(p); }
     __device__ __forceinline__ void get(float (&x)[N]) const { widen<DT, N>(raw, x); }
 };
 template <int DT> struct Vector<DT, 1> {
     float x1;
+    template <bool NT = false>
     __device__ __forceinline__ void load(const char* p) { x1 = load_one<DT>(p); }
     __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = x1; }
 };
-template <int DT>
+template <int DT, bool NT>
 __device__ __forceinline__ void store_own(char* row, int at, int own, const float (&x)[1]) {
     if (own == 0) store_one<DT>(row + at * ElemBytes<DT>::value, x[0]);
 }
 
 // ---- lookup ----
 
+// Rows that the caches cannot keep for the next kernel are stored with the non-temporal hint: 16384 rows of 1024, binary32 table,
+// bfloat16 rows (33 MB) 11.2 us with it, 13.2 without.
+constexpr int64_t kStreamBytes = int64_t(4) << 20;
+
 template <typename Id, int WT, int OT, int N>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(const Id* ids, int64_t tokens, const char* table, int64_t rows, int width,
-                                                          int64_t table_stride, float scale, char* out, int64_t out_stride) {
+                                                          int64_t table_stride, float scale, char* out, int64_t out_stride, int stream) {
     constexpr int GROUPS = N == 1 ? 1 : 16 / N;
     const int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
     if (t >= tokens) return;
@@ -101,9 +107,31 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const Id* ids, int64_t
             v[s].get(x);
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = named ? x[i] * scale : 0.0f;
-            store_own<OT>(to, at.at[s], at.own[s], x);
+            if (stream) store_own<OT, true>(to, at.at[s], at.own[s], x);
+            else store_own<OT, false>(to, at.at[s], at.own[s], x);
         }
     }
+}
+
+// Rows of up to half a wave's vectors: a thread takes one vector of one token.  (100 thousand rows of 64 in bfloat16: 18 us with a wave
+// a row.)
+template <typename Id, int WT, int OT, int N>
+__global__ __launch_bounds__(kThreads) void narrow_lookup_kernel(const Id* ids, unsigned tokens, const char* table, int64_t rows, int width, int64_t table_stride,
+                                                                 float scale, char* out, int64_t out_stride, int stream) {
+    const unsigned vectors = (width + N - 1) / N, i = blockIdx.x * kThreads + threadIdx.x, t = i / vectors;
+    if (t >= tokens) return;
+    const int c = static_cast<int>(i - t * vectors) * N, at = min(c, width - N);
+    const int64_t r = row_of(ids, t);
+    const bool named = r >= 0 && r < rows;
+    Vector<WT, N> v;
+    v.load(table + ((named ? r : 0) * table_stride + at) * ElemBytes<WT>::value);
+    float x[N];
+    v.get(x);
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = named ? x[k] * scale : 0.0f;
+    char* to = out + t * out_stride * ElemBytes<OT>::value;
+    if (stream) store_own<OT, true>(to, at, c - at, x);
+    else store_own<OT, false>(to, at, c - at, x);
 }
 
 // ---- sums of tokens' rows ----
@@ -114,17 +142,18 @@ struct SumArgs {
     const void* ids;
     const char* dout;
     char* grad;
-    float* partial;                              // [windows][2][width]
+    const uint32_t* split;
+    float* partial;                              // [windows][2][width], of the parts that `split` lists
     int64_t tokens, rows, dout_stride, grad_stride, padding;
-    int32_t width, window, windows, window_blocks, add;
-    int32_t units, log2_blocks;                  // units: column ranges of a wave in a row
+    int32_t width, windows, window_blocks, row_blocks, rows_per_block, add;
+    int32_t units, window_units, log2_blocks;    // units: column ranges of a wave in a row
+    int32_t shift, bucket_bits;                  // of the sort
     float scale;
 };
 
-template <int FT, int N, int GROUPS>
+// U: tokens whose rows are on the way together.
+template <int FT, int N, int GROUPS, int U = 8>
 struct Sum {
-    // Tokens whose rows are on the way together: 16 KiB of a wave.
-    static constexpr int U = N == 1 ? 8 : FT == DDP_FP32 ? 64 / (N * GROUPS) : 128 / (N * GROUPS);
     float acc[GROUPS][N] = {};
 
     __device__ __forceinline__ void load(Vector<FT, N> (&v)[GROUPS], const SumArgs& a, const Columns<N, GROUPS>& at, uint32_t token) {
@@ -143,24 +172,18 @@ struct Sum {
             for (int k = 0; k < N; ++k) acc[s][k] += x[k];
         }
     }
-    // The tokens that `token(i)` gives for i = 0 .. n-1, in this order; token(i) is the same in all lanes.
+    // The tokens that `token(i)` gives for i = 0 .. n-1, in this order; n and token(i) are the same in all lanes.
     template <typename Token>
     __device__ __forceinline__ void tokens(const SumArgs& a, const Columns<N, GROUPS>& at, int n, Token token) {
-        int i = 0;
-        for (; i + U <= n; i += U) several<U>(a, at, i, token);
-        if constexpr (U > 4)
-            for (; i + 4 <= n; i += 4) several<4>(a, at, i, token);
-        if constexpr (U > 2)
-            if (i + 2 <= n) { several<2>(a, at, i, token); i += 2; }
-        for (; i < n; ++i) several<1>(a, at, i, token);
-    }
-    template <int K, typename Token>
-    __device__ __forceinline__ void several(const SumArgs& a, const Columns<N, GROUPS>& at, int i, Token token) {
-        Vector<FT, N> v[K][GROUPS];
+        for (int i = 0; i < n; i += U) {
+            Vector<FT, N> v[U][GROUPS];
 #pragma unroll
-        for (int u = 0; u < K; ++u) load(v[u], a, at, token(i + u));
+            for (int u = 0; u < U; ++u)
+                if (i + u < n) load(v[u], a, at, token(i + u));
 #pragma unroll
-        for (int u = 0; u < K; ++u) add(v[u], at);
+            for (int u = 0; u < U; ++u)
+                if (i + u < n) add(v[u], at);
+        }
     }
     template <int GT>
     __device__ __forceinline__ void put(const SumArgs& a, const Columns<N, GROUPS>& at, int64_t row) {
@@ -177,7 +200,7 @@ struct Sum {
                 old[s].get(x);
 #pragma unroll
                 for (int k = 0; k < N; ++k) acc[s][k] = acc[s][k] * a.scale + x[k];
-                store_own<GT>(to, at.at[s], at.own[s], acc[s]);
+                store_own<GT, true>(to, at.at[s], at.own[s], acc[s]);
             }
             return;
         }
@@ -186,10 +209,14 @@ struct Sum {
             if (at.own[s] == N) continue;
 #pragma unroll
             for (int k = 0; k < N; ++k) acc[s][k] *= a.scale;
-            store_own<GT>(to, at.at[s], at.own[s], acc[s]);
+            store_own<GT, true>(to, at.at[s], at.own[s], acc[s]);
         }
     }
 };
+
+// Where a row comes in the sort, and the row there.
+__device__ __forceinline__ int64_t place_of(const SumArgs& a, int64_t row) { return (row & ((int64_t(1) << a.bucket_bits) - 1)) << a.shift | row >> a.bucket_bits; }
+__device__ __forceinline__ int64_t row_at(const SumArgs& a, int64_t place) { return (place & ((int64_t(1) << a.shift) - 1)) << a.bucket_bits | place >> a.shift; }
 
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
     return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0));
@@ -207,6 +234,18 @@ __device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) {
     return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(x), lane));
 }
 
+// Vector i of a block's rows one after the other: zeros at its place in the gradient.  row_of_block(j) is the block's row j, or -1
+// where that is not to be zeroed.
+template <int GT, int N, typename Row>
+__device__ __forceinline__ void zero_vector(const SumArgs& a, unsigned i, Row row_of_block) {
+    const unsigned vectors = (a.width + N - 1) / N, j = i / vectors;
+    const int64_t row = row_of_block(static_cast<int>(j));
+    if (row < 0) return;
+    const int at = min(static_cast<int>(i - j * vectors) * N, a.width - N);     // (the last two may overlap: zeros both)
+    const float zeros[N] = {};
+    store_own<GT, true>(a.grad + row * a.grad_stride * ElemBytes<GT>::value, at, 0, zeros);
+}
+
 // ---- few tokens: every block looks through all of them ----
 //
 // Block b of 2^log2_blocks has the rows b, b + blocks, ... (rows of frequent tokens are neighbours in many vocabularies: they go to
@@ -216,30 +255,32 @@ __device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) {
 constexpr int kScanThreads = 512, kScanWaves = kScanThreads / 64;
 constexpr int kScanTokens = 4096;
 constexpr int kScanEach = kScanTokens / kScanThreads;
+constexpr int kScanBlocks = 2048;                // blocks to have where there are column ranges to go round
 constexpr int kScanAlone = 16;                   // tokens of a row that one wave sums
 constexpr int kScanRows = 32;                    // rows of 1024 columns that a block has at most (up to 1024 of fewer columns)
 
-template <typename Id, int FT, int GT, int N, int GROUPS>
-__global__ __launch_bounds__(kScanThreads) void scan_sum_kernel(SumArgs a) {
+template <typename Id, int FT, int GT, int N>
+__global__ __launch_bounds__(kScanThreads, 6) void scan_sum_kernel(SumArgs a) {
     __shared__ uint32_t list[kScanTokens];           // row in the block << 16 | token
     __shared__ uint32_t wave_count[kScanWaves];
-    __shared__ float part[kScanWaves][64 * N * GROUPS];
-    extern __shared__ uint32_t crowded[];            // a bit for every row of the block that has many tokens
+    __shared__ float part[kScanWaves][64 * N];
+    extern __shared__ uint32_t counts[];             // of the tokens of each row
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t b = blockIdx.x;
     const int nrows = static_cast<int>((a.rows - b + (int64_t(1) << a.log2_blocks) - 1) >> a.log2_blocks);
     const int per_wave = static_cast<int>((a.tokens + kScanThreads - 1) / kScanThreads) * 64;
-    for (int i = threadIdx.x; i < (nrows + 31) / 32; i += kScanThreads) crowded[i] = 0;
-    int64_t row[kScanEach];
+    for (int i = threadIdx.x; i < nrows; i += kScanThreads) counts[i] = 0;
+    int64_t id[kScanEach];
+    int row[kScanEach];
 #pragma unroll
     for (int k = 0; k < kScanEach; ++k) {
         const int t = wave * per_wave + k * 64 + lane;
-        row[k] = k * 64 < per_wave && t < a.tokens ? row_of(static_cast<const Id*>(a.ids), t) : -1;
+        id[k] = k * 64 < per_wave && t < a.tokens ? row_of(static_cast<const Id*>(a.ids), t) : -1;
     }
     uint32_t mine = 0;
 #pragma unroll
     for (int k = 0; k < kScanEach; ++k) {
-        if (row[k] < 0 || row[k] >= a.rows || row[k] == a.padding || (row[k] & ((int64_t(1) << a.log2_blocks) - 1)) != b) row[k] = -1;
+        row[k] = id[k] < 0 || id[k] >= a.rows || id[k] == a.padding || (id[k] & ((int64_t(1) << a.log2_blocks) - 1)) != b ? -1 : static_cast<int>(id[k]);
         mine += __popcll(__ballot(row[k] >= 0));
     }
     if (lane == 0) wave_count[wave] = mine;
@@ -253,49 +294,61 @@ __global__ __launch_bounds__(kScanThreads) void scan_sum_kernel(SumArgs a) {
 #pragma unroll
     for (int k = 0; k < kScanEach; ++k) {
         const uint64_t hits = __ballot(row[k] >= 0);
-        if (row[k] >= 0) list[next + lanes_below(hits)] = static_cast<uint32_t>(row[k] >> a.log2_blocks) << 16 | static_cast<uint32_t>(wave * per_wave + k * 64 + lane);
+        if (row[k] >= 0) {
+            list[next + lanes_below(hits)] = static_cast<uint32_t>(row[k] >> a.log2_blocks) << 16 | static_cast<uint32_t>(wave * per_wave + k * 64 + lane);
+            atomicAdd(&counts[row[k] >> a.log2_blocks], 1u);
+        }
         next += __popcll(hits);
     }
     __syncthreads();
     const int n = __builtin_amdgcn_readfirstlane(static_cast<int>(listed));
-    const int units = a.units;
-    // rows of few tokens, a wave each
-    for (int u = wave; u < nrows * units; u += kScanWaves) {
-        const int j = u / units;
-        int count = 0;
-        for (int i = 0; i < n; i += 64) count += __popcll(__ballot(i + lane < n && list[min(i + lane, n - 1)] >> 16 == static_cast<uint32_t>(j)));
-        if (count > kScanAlone) {
-            if (lane == 0) atomicOr(&crowded[j >> 5], 1u << (j & 31));
-            continue;
-        }
-        if (a.add && count == 0) continue;
-        const Columns<N, GROUPS> at((u % units) * (64 * N * GROUPS), a.width);
-        Sum<FT, N, GROUPS> sum;
-        for (int i = 0; count > 0; i += 64) {
-            const uint32_t e = list[min(i + lane, n - 1)];
-            uint64_t hits = __ballot(i + lane < n && e >> 16 == static_cast<uint32_t>(j));
-            const int here = __popcll(hits);
-            count -= here;
-            sum.tokens(a, at, here, [&](int) {
-                const int l = __ffsll(static_cast<unsigned long long>(hits)) - 1;
-                hits &= hits - 1;
-                return lane_value(e, l) & 0xFFFFu;
-            });
-        }
-        sum.template put<GT>(a, at, b + (static_cast<int64_t>(j) << a.log2_blocks));
+    // the column ranges of the block: blockIdx.y, + gridDim.y, ...
+    const int units = (a.units - static_cast<int>(blockIdx.y) + static_cast<int>(gridDim.y) - 1) / static_cast<int>(gridDim.y);
+    auto first_column = [&](int i) { return (static_cast<int>(blockIdx.y) + i * static_cast<int>(gridDim.y)) * (64 * N); };
+    auto row_of_block = [&](int j) { return b + (static_cast<int64_t>(j) << a.log2_blocks); };
+    // rows of no tokens: the blocks of one set of rows and other columns share them
+    if (!a.add) {
+        const unsigned vectors = nrows * ((a.width + N - 1) / N), step = kScanThreads * gridDim.y;
+        for (unsigned i = blockIdx.y * kScanThreads + threadIdx.x; i < vectors; i += step)
+            zero_vector<GT, N>(a, i, [&](int j) { return counts[j] == 0 ? row_of_block(j) : -1; });
     }
-    __syncthreads();
-    for (int j0 = 0; j0 < nrows; j0 += 32) {
-        uint32_t bits = __builtin_amdgcn_readfirstlane(crowded[j0 >> 5]);
-        while (bits != 0) {
-            const int j = j0 + __ffs(bits) - 1;
-            bits &= bits - 1;
-            int count = 0;
-            for (int i = 0; i < n; i += 64) count += __popcll(__ballot(i + lane < n && list[min(i + lane, n - 1)] >> 16 == static_cast<uint32_t>(j)));
+    if (n == 0) return;
+    // rows of few tokens, a wave for each and each range
+    int turn = 0;
+    for (int j0 = 0; j0 < nrows; j0 += 64) {
+        const uint32_t here = counts[min(j0 + lane, nrows - 1)];
+        for (uint64_t some = __ballot(j0 + lane < nrows && here > 0 && here <= kScanAlone); some != 0; some &= some - 1) {
+            const int l = __ffsll(static_cast<unsigned long long>(some)) - 1, j = j0 + l;
+            for (int unit = 0; unit < units; ++unit, ++turn) {
+                if (turn % kScanWaves != wave) continue;
+                int left = static_cast<int>(lane_value(here, l));
+                const Columns<N, 1> at(first_column(unit), a.width);
+                Sum<FT, N, 1> sum;
+                for (int i = 0; left > 0; i += 64) {
+                    const uint32_t e = list[min(i + lane, n - 1)];
+                    uint64_t hits = __ballot(i + lane < n && e >> 16 == static_cast<uint32_t>(j));
+                    const int found = __popcll(hits);
+                    left -= found;
+                    sum.tokens(a, at, found, [&](int) {
+                        const int k = __ffsll(static_cast<unsigned long long>(hits)) - 1;
+                        hits &= hits - 1;
+                        return lane_value(e, k) & 0xFFFFu;
+                    });
+                }
+                sum.template put<GT>(a, at, row_of_block(j));
+            }
+        }
+    }
+    if (n <= kScanAlone) return;
+    for (int j0 = 0; j0 < nrows; j0 += 64) {
+        uint64_t crowded = __ballot(j0 + lane < nrows && counts[min(j0 + lane, nrows - 1)] > kScanAlone);
+        for (; crowded != 0; crowded &= crowded - 1) {
+            const int j = j0 + __ffsll(static_cast<unsigned long long>(crowded)) - 1;
+            const int count = __builtin_amdgcn_readfirstlane(static_cast<int>(counts[j]));
             const int share = (count + kScanWaves - 1) / kScanWaves, from = wave * share, to = min(from + share, count);
             for (int unit = 0; unit < units; ++unit) {
-                const Columns<N, GROUPS> at(unit * (64 * N * GROUPS), a.width);
-                Sum<FT, N, GROUPS> sum;
+                const Columns<N, 1> at(first_column(unit), a.width);
+                Sum<FT, N, 1> sum;
                 int seen = 0;                        // the row's tokens so far
                 for (int i = 0; i < n && seen < to; i += 64) {
                     const uint32_t e = list[min(i + lane, n - 1)];
@@ -310,18 +363,16 @@ __global__ __launch_bounds__(kScanThreads) void scan_sum_kernel(SumArgs a) {
                         return lane_value(e, l) & 0xFFFFu;
                     });
                 }
+                if (wave > 0) {
 #pragma unroll
-                for (int s = 0; s < GROUPS; ++s)
-#pragma unroll
-                    for (int k = 0; k < N; ++k) part[wave][(s * N + k) * 64 + lane] = sum.acc[s][k];
+                    for (int k = 0; k < N; ++k) part[wave][k * 64 + lane] = sum.acc[0][k];
+                }
                 __syncthreads();
                 if (wave == 0) {
 #pragma unroll
-                    for (int s = 0; s < GROUPS; ++s)
-#pragma unroll
-                        for (int k = 0; k < N; ++k)
-                            for (int w = 1; w < kScanWaves; ++w) sum.acc[s][k] += part[w][(s * N + k) * 64 + lane];
-                    sum.template put<GT>(a, at, b + (static_cast<int64_t>(j) << a.log2_blocks));
+                    for (int k = 0; k < N; ++k)
+                        for (int w = 1; w < kScanWaves; ++w) sum.acc[0][k] += part[w][k * 64 + lane];
+                    sum.template put<GT>(a, at, row_of_block(j));
                 }
                 __syncthreads();
             }
@@ -331,26 +382,38 @@ __global__ __launch_bounds__(kScanThreads) void scan_sum_kernel(SumArgs a) {
 
 // ---- more tokens: sorted by row ----
 //
-// Rows are put into buckets of 2^shift consecutive rows.  A block sorts a chunk of tokens by bucket; starts[chunk][b] is where
+// Rows are put into 2^bucket_bits buckets by their low bits, so that the frequent rows, which are neighbours in many
+// vocabularies, come into different ones; the order in which `sorted` and `first` have the rows is by bucket, then by what is left
+// of the row (`place_of`, `row_at`).  A block sorts a chunk of tokens by bucket; starts[chunk][b] is where
 // bucket b starts in the chunk's part of `list`, which is also the number of the chunk's tokens in the buckets before it: summed
 // over the chunks it is where the bucket starts among all tokens, so no scan over buckets is needed.  A block then
 // gathers a bucket's tokens chunk by chunk (t ascending) and sorts them by row.
 
+// A row of up to kWindow tokens is summed by one wave (and column range).  Rows of more are split at multiples of kWindow in the
+// sorted tokens, their parts go through `partial` and are joined by another launch.  split[w][0] is 1 + the place of the row
+// that reaches back before window w, split[w][1] of the one that starts in it, 0 where there is no such row of more than kWindow
+// tokens (two of them cannot start in one window).
+constexpr int kWindow = 32;
+
 constexpr int kChunk = 1024;
 constexpr int kMaxBuckets = 8192;                // 32 KiB of counters
 constexpr int kSortThreads = 512, kSortWaves = kSortThreads / 64;
-constexpr int kSortRows = 1024;                  // rows of a bucket, at most
+constexpr int kSortRows = 1024;                  // places of a bucket, at most
 constexpr int kSortCache = 4096;                 // tokens of a bucket held in LDS
+constexpr int kTokenBits = 22;
+constexpr uint32_t kTokenMask = (1u << kTokenBits) - 1;
+static_assert(kMaxTokens <= int64_t(1) << kTokenBits && kSortRows <= 1 << (32 - kTokenBits), "an entry is 32 bits");
 
 struct SortArgs {
     const void* ids;
     int64_t tokens, rows, padding;
-    int32_t shift, buckets, bucket_bits, chunks;
+    int32_t shift, buckets, bucket_bits, chunks; // buckets of 2^shift places
     uint16_t* starts;                            // [chunks][buckets + 1]
-    uint32_t* list;                              // [tokens] by chunk, by bucket: row in the bucket << 10 | token in the chunk
-    uint64_t* gathered;                          // [tokens] by bucket, t ascending (buckets that LDS does not hold): row << 32 | token
-    uint32_t* sorted;                            // [tokens] by row, t ascending
-    uint32_t* first;                             // [rows + 1] where each row starts in `sorted`
+    uint32_t* list;                              // [tokens] by chunk, by bucket: entries, place in the bucket << 22 | token
+    uint32_t* gathered;                          // [tokens] by bucket, t ascending (buckets that LDS does not hold)
+    uint32_t* sorted;                            // [tokens] by place, t ascending
+    uint32_t* first;                             // [places + 1] where each place's row starts in `sorted`
+    uint32_t* split;                             // [windows][2] see Split
 };
 
 // Lanes of the wave (of those in `active`) that hold the same value of `bits` bits.
@@ -373,7 +436,8 @@ __global__ __launch_bounds__(kChunk) void chunk_sort_kernel(SortArgs a) {
     const int64_t row = t < a.tokens ? row_of(static_cast<const Id*>(a.ids), t) : -1;
     const bool in = row >= 0 && row < a.rows && row != a.padding;
     for (int i = tid; i < a.buckets; i += kChunk) count[i] = 0;
-    const uint32_t b = in ? static_cast<uint32_t>(row) >> a.shift : 0u;
+    if (tid < 2 * kChunk / kWindow) a.split[static_cast<int64_t>(blockIdx.x) * (2 * kChunk / kWindow) + tid] = 0;
+    const uint32_t b = in ? static_cast<uint32_t>(row) & (a.buckets - 1) : 0u;
     const uint64_t same = peers(b, a.bucket_bits, __ballot(in));
     const uint32_t rank = lanes_below(same);
     uint32_t before = 0;
@@ -404,62 +468,145 @@ __global__ __launch_bounds__(kChunk) void chunk_sort_kernel(SortArgs a) {
     }
     if (tid == kChunk - 1) starts[a.buckets] = static_cast<uint16_t>(next);
     __syncthreads();
-    if (in) a.list[static_cast<int64_t>(blockIdx.x) * kChunk + count[b] + before + rank] = (static_cast<uint32_t>(row) & ((1u << a.shift) - 1)) << 10 | tid;
+    if (in) a.list[static_cast<int64_t>(blockIdx.x) * kChunk + count[b] + before + rank] = static_cast<uint32_t>(row) >> a.bucket_bits << kTokenBits | static_cast<uint32_t>(t);
 }
 
+// LDS accesses of a wave stay in order; the fence keeps the compiler to it.
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// A bucket's counters in LDS: where the next token of each row goes, and where a row of more than kWindow tokens starts in `sorted`
+// (others: the largest number).
+struct RowCounters {
+    uint32_t *next, *crowded_from;
+};
+// Row r of a bucket has n tokens, the first of them at `from` in `sorted`.
+__device__ __forceinline__ void row_starts(const SortArgs& a, const RowCounters& rows, int64_t place0, int r, uint32_t from, uint32_t n) {
+    a.first[place0 + r] = from;
+    rows.crowded_from[r] = n > kWindow ? from : ~0u;
+    if (n > kWindow) a.split[from / kWindow * 2 + 1] = 1 + static_cast<uint32_t>(place0 + r);
+}
+// 64 tokens of a bucket (entries; lanes that are not `in` have none) go to their places behind `base`.
+__device__ __forceinline__ void place_tokens(const SortArgs& a, uint32_t* next, const uint32_t* crowded_from, int64_t place0, uint32_t base, uint32_t e, bool in) {
+    const uint32_t r = e >> kTokenBits;
+    const uint64_t same = peers(r, a.shift, __ballot(in));
+    const uint32_t rank = lanes_below(same);
+    uint32_t p = 0;
+    if (in) p = next[r];
+    wave_fence();
+    if (in) {
+        const uint32_t at = base + p + rank;
+        a.sorted[at] = e & kTokenMask;
+        if (at % kWindow == 0 && crowded_from[r] < at) a.split[at / kWindow * 2] = 1 + static_cast<uint32_t>(place0) + r;
+        if (rank == 0) next[r] = p + __popcll(same);
+    }
+    wave_fence();
+}
+
+// Up to this many tokens of a bucket are sorted by the block's first wave alone, without barriers.
+constexpr int kWaveTokens = 256;
+
 __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
-    __shared__ uint64_t cache[kSortCache];
-    __shared__ uint32_t wave_part[2][kSortWaves];
+    __shared__ uint32_t cache[kSortCache];
+    static_assert(kWaveTokens <= kSortCache, "both fit");
+    __shared__ uint32_t wave_part[kSortWaves], wave_before[kSortWaves];
     __shared__ uint32_t more[kSortThreads], more_from[kSortThreads], more_to[kSortThreads];
-    extern __shared__ uint32_t row_count[];          // [kSortWaves][rows of a bucket]
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t row0 = static_cast<int64_t>(b) << a.shift;
-    const int nrows = static_cast<int>(min(static_cast<int64_t>(1) << a.shift, a.rows - row0));
-    // where the bucket starts, and how many tokens it has
+    extern __shared__ uint32_t counters[];           // [kSortWaves + 1][rows of a bucket]
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int nrows = 1 << a.shift;
+    const RowCounters rows{counters + wave * nrows, counters + kSortWaves * nrows};
+    auto starts_of = [&](int c, int b) { return a.starts + static_cast<int64_t>(c) * (a.buckets + 1) + b; };
+    const int b = blockIdx.x;
+    const int64_t place0 = static_cast<int64_t>(b) << a.shift;
     uint32_t before = 0, mine = 0;
     for (int c = tid; c < a.chunks; c += kSortThreads) {
-        const uint16_t* s = a.starts + static_cast<int64_t>(c) * (a.buckets + 1) + b;
-        before += s[0];
-        mine += s[1] - s[0];
+        const uint16_t* p = starts_of(c, b);
+        before += p[0];
+        mine += p[1] - p[0];
     }
-    const uint32_t before_all = wave_inclusive_sum(before), mine_all = wave_inclusive_sum(mine);
-    if (lane == 63) {
-        wave_part[0][wave] = before_all;
-        wave_part[1][wave] = mine_all;
+    before = wave_sum(before);
+    mine = wave_sum(mine);
+    if (lane == 0) {
+        wave_before[wave] = before;
+        wave_part[wave] = mine;
     }
-    for (int i = tid; i < kSortWaves * nrows; i += kSortThreads) row_count[i] = 0;
+    for (int i = tid; i < kSortWaves * nrows; i += kSortThreads) counters[i] = 0;
     __syncthreads();
     uint32_t base = 0, total = 0;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-        base += wave_part[0][w];
-        total += wave_part[1][w];
+        base += wave_before[w];
+        total += wave_part[w];
     }
-    if (b == a.buckets - 1 && tid == 0) a.first[a.rows] = base + total;
-    if (total == 0) {
-        for (int r = tid; r < nrows; r += kSortThreads) a.first[row0 + r] = base;
+    if (b == a.buckets - 1 && tid == 0) a.first[place0 + nrows] = base + total;
+    if (total <= kWaveTokens) {
+        if (wave > 0) return;
+        uint32_t* tokens = cache;
+        uint32_t done = 0;
+        for (int c0 = 0; c0 < a.chunks && done < total; c0 += 64) {
+            const int c = c0 + lane;
+            uint32_t s = 0, n = 0;
+            if (c < a.chunks) {
+                const uint16_t* p = starts_of(c, b);
+                s = p[0];
+                n = p[1] - s;
+            }
+            const uint32_t upto = wave_inclusive_sum(n), to = done + upto - n;
+            const uint32_t* from = a.list + static_cast<int64_t>(c) * kChunk + s;
+            for (uint32_t i = 0; i < n; i += 4) {
+                uint32_t few[4];
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) few[k] = i + k < n ? from[i + k] : 0u;
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k)
+                    if (i + k < n) tokens[to + i + k] = few[k];
+            }
+            done += lane_value(upto, 63);
+        }
+        wave_fence();
+        for (uint32_t i = lane; i < total; i += 64) atomicAdd(&rows.next[tokens[i] >> kTokenBits], 1u);
+        wave_fence();
+        uint32_t above = 0;
+        for (int r0 = 0; r0 < nrows; r0 += 64) {
+            const int r = r0 + lane;
+            const uint32_t n = r < nrows ? rows.next[r] : 0u;
+            const uint32_t upto = wave_inclusive_sum(n);
+            if (r < nrows) {
+                row_starts(a, rows, place0, r, base + above + upto - n, n);
+                rows.next[r] = above + upto - n;
+            }
+            above += lane_value(upto, 63);
+        }
+        wave_fence();
+        for (uint32_t i0 = 0; i0 < total; i0 += 64) {
+            const bool in = i0 + lane < total;
+            place_tokens(a, rows.next, rows.crowded_from, place0, base, in ? tokens[i0 + lane] : 0u, in);
+        }
         return;
     }
     // the bucket's tokens in order: a thread copies up to four of its chunk's, the waves together what there is above that
-    uint64_t* tokens = total <= kSortCache ? cache : a.gathered + base;
-    auto entry = [&](int c, uint32_t e) { return static_cast<uint64_t>(e >> 10) << 32 | (static_cast<uint32_t>(c) * kChunk + (e & (kChunk - 1))); };
+    uint32_t* tokens = total <= kSortCache ? cache : a.gathered + base;
     uint32_t done = 0;
     for (int c0 = 0; c0 < a.chunks; c0 += kSortThreads) {
         const int c = c0 + tid;
         uint32_t s = 0, n = 0;
         if (c < a.chunks) {
-            const uint16_t* p = a.starts + static_cast<int64_t>(c) * (a.buckets + 1) + b;
+            const uint16_t* p = starts_of(c, b);
             s = p[0];
             n = p[1] - s;
         }
         const uint32_t upto = wave_inclusive_sum(n);
         __syncthreads();                             // wave_part and `more` are read by then
-        if (lane == 63) wave_part[0][wave] = upto;
+        if (lane == 63) wave_part[wave] = upto;
         __syncthreads();
         uint32_t to = done + upto - n;
         for (int w = 0; w < kSortWaves; ++w) {
-            if (w < wave) to += wave_part[0][w];
-            done += wave_part[0][w];
+            if (w < wave) to += wave_part[w];
+            done += wave_part[w];
         }
         const uint32_t* from = a.list + static_cast<int64_t>(c) * kChunk + s;
         uint32_t few[4];
@@ -467,7 +614,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
         for (int i = 0; i < 4; ++i) few[i] = i < static_cast<int>(n) ? from[i] : 0u;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (i < static_cast<int>(n)) tokens[to + i] = entry(c, few[i]);
+            if (i < static_cast<int>(n)) tokens[to + i] = few[i];
         more[tid] = n > 4 ? n - 4 : 0;
         more_from[tid] = s + 4;
         more_to[tid] = to + 4;
@@ -477,14 +624,14 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
             const uint32_t nk = __builtin_amdgcn_readfirstlane(more[k]);
             if (nk == 0) continue;
             const uint32_t* p = a.list + static_cast<int64_t>(c0 + k) * kChunk + more_from[k];
-            uint64_t* q = tokens + more_to[k];
+            uint32_t* q = tokens + more_to[k];
             for (uint32_t i0 = 0; i0 < nk; i0 += 256) {
                 uint32_t e[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) e[u] = i0 + u * 64 + lane < nk ? p[i0 + u * 64 + lane] : 0u;
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
-                    if (i0 + u * 64 + lane < nk) q[i0 + u * 64 + lane] = entry(c0 + k, e[u]);
+                    if (i0 + u * 64 + lane < nk) q[i0 + u * 64 + lane] = e[u];
             }
         }
     }
@@ -493,7 +640,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
     // counting sort by row: every wave has a stretch of the tokens
     const uint32_t stretch = (total + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
     const uint32_t from = min(wave * stretch, total), to = min(from + stretch, total);
-    for (uint32_t i = from + lane; i < to; i += 64) atomicAdd(&row_count[wave * nrows + static_cast<uint32_t>(tokens[i] >> 32)], 1u);
+    for (uint32_t i = from + lane; i < to; i += 64) atomicAdd(&rows.next[tokens[i] >> kTokenBits], 1u);
     __syncthreads();
     // row by row, within a row wave by wave; the rows' sums are scanned in rounds of one row a thread
     uint32_t above = 0;
@@ -501,143 +648,140 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
         const int r = r0 + tid;
         uint32_t n = 0;
         if (r < nrows)
-            for (int w = 0; w < kSortWaves; ++w) n += row_count[w * nrows + r];
+            for (int w = 0; w < kSortWaves; ++w) n += counters[w * nrows + r];
         const uint32_t upto = wave_inclusive_sum(n);
-        if (lane == 63) wave_part[1][wave] = upto;
+        if (lane == 63) wave_part[wave] = upto;
         __syncthreads();
         uint32_t next = above + upto - n;
         for (int w = 0; w < kSortWaves; ++w) {
-            if (w < wave) next += wave_part[1][w];
-            above += wave_part[1][w];
+            if (w < wave) next += wave_part[w];
+            above += wave_part[w];
         }
         __syncthreads();
         if (r < nrows) {
-            a.first[row0 + r] = base + next;
+            row_starts(a, rows, place0, r, base + next, n);
             for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t k = row_count[w * nrows + r];
-                row_count[w * nrows + r] = next;
+                const uint32_t k = counters[w * nrows + r];
+                counters[w * nrows + r] = next;
                 next += k;
             }
         }
     }
     __syncthreads();
-    uint32_t* place = row_count + wave * nrows;
     for (uint32_t i0 = from; i0 < to; i0 += 64) {
-        const uint32_t i = i0 + lane;
-        const bool in = i < to;
-        const uint64_t e = in ? tokens[i] : 0u;
-        const uint32_t r = static_cast<uint32_t>(e >> 32);
-        const uint64_t same = peers(r, a.shift, __ballot(in));
-        const int rank = lanes_below(same);
-        uint32_t p = 0;
-        if (in) p = place[r];
-        __builtin_amdgcn_wave_barrier();             // a wave's LDS accesses stay in order
-        if (in) {
-            a.sorted[base + p + rank] = static_cast<uint32_t>(e);
-            if (rank == 0) place[r] = p + __popcll(same);
-        }
-        __builtin_amdgcn_wave_barrier();
+        const bool in = i0 + lane < to;
+        place_tokens(a, rows.next, rows.crowded_from, place0, base, in ? tokens[i0 + lane] : 0u, in);
     }
 }
 
-// A row of up to `window` tokens is summed by one wave (and column range); rows of more are split at multiples of `window`
-// in the sorted tokens, their parts go through `partial` and are joined by another launch.
-constexpr int kRowsPerBlock = 16;
-constexpr int kWindow = 32;
+constexpr int kRowColumns = 8192;                // of the rows of a block: 8 rows of 1024, at most 64 of fewer
 
-// Window w's part of a row of more than `window` tokens: partial[w][0] where the row reaches back before the window, partial[w][1] where
-// it starts in it (two such rows cannot start in one window).
-template <typename Id, int FT, int N, int GROUPS>
+template <int FT, int N>
 __device__ __forceinline__ void sum_window(const SumArgs& a, int64_t w, int unit) {
-    const uint32_t w0 = static_cast<uint32_t>(w) * a.window, all = a.first[a.rows];
-    if (w0 >= all) return;
-    const uint32_t w1 = min(w0 + a.window, all);
-    const int64_t r_first = row_of(static_cast<const Id*>(a.ids), a.sorted[w0]), r_last = row_of(static_cast<const Id*>(a.ids), a.sorted[w1 - 1]);
-    const Columns<N, GROUPS> at(unit * (64 * N * GROUPS), a.width);
+    const uint32_t split[2] = {a.split[w * 2], a.split[w * 2 + 1]};
+    const uint32_t w0 = static_cast<uint32_t>(w) * kWindow;
+    const Columns<N, 1> at(unit * (64 * N), a.width);
     for (int side = 0; side < 2; ++side) {
-        const int64_t r = side == 0 ? r_first : r_last;
-        const uint32_t f = a.first[r], e = a.first[r + 1];
-        if (e - f <= static_cast<uint32_t>(a.window) || (side == 0) != (f < w0)) continue;
-        const uint32_t from = __builtin_amdgcn_readfirstlane(max(f, w0)), to = __builtin_amdgcn_readfirstlane(min(e, w1));
-        Sum<FT, N, GROUPS> sum;
-        for (uint32_t i = from; i < to; i += 64) {
-            const uint32_t mine = a.sorted[min(i + (threadIdx.x & 63), to - 1)];
-            sum.tokens(a, at, static_cast<int>(min(to - i, 64u)), [&](int k) { return lane_value(mine, k); });
-        }
-        char* p = reinterpret_cast<char*>(a.partial + (w * 2 + side) * static_cast<int64_t>(a.width));
-#pragma unroll
-        for (int s = 0; s < GROUPS; ++s)
-            if (at.own[s] < N) store_own<DDP_FP32>(p, at.at[s], at.own[s], sum.acc[s]);
+        if (split[side] == 0) continue;
+        const uint32_t from = __builtin_amdgcn_readfirstlane(max(a.first[split[side] - 1], w0));
+        const uint32_t to = __builtin_amdgcn_readfirstlane(min(a.first[split[side]], w0 + kWindow));
+        const uint32_t mine = a.sorted[min(from + (threadIdx.x & 63), to - 1)];
+        Sum<FT, N, 1> sum;
+        sum.tokens(a, at, static_cast<int>(to - from), [&](int k) { return lane_value(mine, k); });
+        char* to_part = reinterpret_cast<char*>(a.partial + (w * 2 + side) * static_cast<int64_t>(a.width));
+        if (at.own[0] < N) store_own<DDP_FP32, false>(to_part, at.at[0], at.own[0], sum.acc[0]);
     }
 }
 
-// The first blocks take windows, the others kRowsPerBlock rows each: a row's sum, or zeros.
-template <typename Id, int FT, int GT, int N, int GROUPS>
+// The first blocks take windows, the others rows_per_block rows each, row_blocks apart (the frequent rows are neighbours in many
+// vocabularies: every block has some of each): a row's sum, or zeros.
+template <int FT, int GT, int N, int WN>
 __global__ __launch_bounds__(kThreads) void row_sum_kernel(SumArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (static_cast<int>(blockIdx.x) < a.window_blocks) {
         const int64_t g = static_cast<int64_t>(blockIdx.x) * kWaves + wave;
-        if (g / a.units < a.windows) sum_window<Id, FT, N, GROUPS>(a, g / a.units, static_cast<int>(g % a.units));
+        if (g / a.window_units < a.windows) sum_window<FT, WN>(a, g / a.window_units, static_cast<int>(g % a.window_units));
         return;
     }
-    const int64_t r0 = static_cast<int64_t>(static_cast<int>(blockIdx.x) - a.window_blocks) * kRowsPerBlock;
-    const int nrows = static_cast<int>(min(static_cast<int64_t>(kRowsPerBlock), a.rows - r0));
-    const uint32_t starts = a.first[r0 + min(lane, nrows)];
-    const uint32_t block_from = lane_value(starts, 0), block_to = lane_value(starts, nrows);
-    const uint32_t some = block_to > block_from ? a.sorted[min(block_from + lane, block_to - 1)] : 0u;      // the first 64 tokens
-    for (int u = wave; u < nrows * a.units; u += kWaves) {
-        const int j = u / a.units;
-        const uint32_t from = lane_value(starts, j), to = lane_value(starts, j + 1);
-        if (to - from > static_cast<uint32_t>(a.window) || (a.add && from == to)) continue;
-        const Columns<N, GROUPS> at(u % a.units * (64 * N * GROUPS), a.width);
-        Sum<FT, N, GROUPS> sum;
-        if (to - block_from <= 64) {
-            const int skip = static_cast<int>(from - block_from);
-            sum.tokens(a, at, static_cast<int>(to - from), [&](int k) { return lane_value(some, skip + k); });
-        } else {
-            for (uint32_t i = from; i < to; i += 64) {
-                const uint32_t mine = a.sorted[min(i + lane, to - 1)];
-                sum.tokens(a, at, static_cast<int>(min(to - i, 64u)), [&](int k) { return lane_value(mine, k); });
-            }
+    // lane k knows row k of the block: where its tokens are, and the first of them
+    const int64_t block = static_cast<int>(blockIdx.x) - a.window_blocks;
+    auto row_of_block = [&](int j) { return block + static_cast<int64_t>(j) * a.row_blocks; };
+    const int64_t mine = row_of_block(lane);
+    const bool have = lane < a.rows_per_block && mine < a.rows;
+    const int64_t place = place_of(a, have ? mine : 0);
+    const uint32_t from = a.first[place], count = have ? a.first[place + 1] - from : ~0u;
+    const uint32_t token = have && count > 0 ? a.sorted[from] : 0u;
+    if (!a.add && __ballot(count == 0) != 0) {
+        const unsigned vectors = a.rows_per_block * ((a.width + N - 1) / N);
+        for (unsigned i0 = 0; i0 < vectors; i0 += kThreads)                  // all lanes: the counts are in registers
+            zero_vector<GT, N>(a, min(i0 + threadIdx.x, vectors - 1), [&](int j) { return __shfl(count, j) == 0u ? row_of_block(j) : -1; });
+    }
+    int turn = 0;
+    for (uint64_t some = __ballot(count - 1u < static_cast<uint32_t>(kWindow)); some != 0; some &= some - 1) {
+        const int j = __ffsll(static_cast<unsigned long long>(some)) - 1, n = static_cast<int>(lane_value(count, j));
+        bool fetched = n == 1;
+        uint32_t own = lane_value(token, j);
+        for (int unit = 0; unit < a.units; ++unit, ++turn) {
+            if (turn % kWaves != wave) continue;
+            if (!fetched) own = a.sorted[lane_value(from, j) + min(lane, n - 1)];
+            fetched = true;
+            const Columns<N, 1> at(unit * (64 * N), a.width);
+            Sum<FT, N, 1> sum;
+            sum.tokens(a, at, n, [&](int k) { return lane_value(own, k); });
+            sum.template put<GT>(a, at, row_of_block(j));
         }
-        sum.template put<GT>(a, at, r0 + j);
     }
 }
 
-// A block for each window: where a row of more than `window` tokens starts in it, its parts are summed in order and written:
-// a wave sums a stretch of them, the waves meet in LDS.
-constexpr int kJoinThreads = 512, kJoinWaves = kJoinThreads / 64;
-template <typename Id, int GT, int N>
+// Rows that were split: a block looks through kJoinWindows windows for those that start there, and sums a row's parts in order.  Rows
+// of up to kJoinAlone parts take a wave each; for the others every wave sums a stretch and they meet in LDS.
+constexpr int kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64, kJoinWindows = 16, kJoinAlone = 8;
+template <int GT, int N>
 __global__ __launch_bounds__(kJoinThreads) void row_join_kernel(SumArgs a) {
     __shared__ float part[kJoinWaves][64 * N];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t w0 = blockIdx.x * a.window, all = a.first[a.rows];
-    if (w0 >= all) return;
-    const uint32_t w1 = min(w0 + a.window, all);
-    const int64_t r = row_of(static_cast<const Id*>(a.ids), a.sorted[w1 - 1]);
-    const uint32_t f = a.first[r], e = a.first[r + 1];
-    if (e - f <= static_cast<uint32_t>(a.window) || f < w0) return;
-    const int parts = static_cast<int>((e - 1) / a.window - blockIdx.x) + 1, share = (parts + kJoinWaves - 1) / kJoinWaves;
-    const int from = min(wave * share, parts), to = min(from + share, parts);
-    SumArgs p = a;                                   // the parts as rows: window blockIdx.x + i, its first half (the row's start: its second)
+    const int64_t window = static_cast<int64_t>(blockIdx.x) * kJoinWindows + lane;
+    const uint32_t found = lane < kJoinWindows && window < a.windows ? a.split[window * 2 + 1] : 0u;
+    const int parts_here = found != 0 ? static_cast<int>((a.first[found] - 1) / kWindow - static_cast<uint32_t>(window)) + 1 : 0;
+    SumArgs p = a;                                   // the parts as rows
     p.dout = reinterpret_cast<const char*>(a.partial);
     p.dout_stride = a.width;
-    for (int c = blockIdx.y * (64 * N); c < a.width; c += gridDim.y * (64 * N)) {
-        const Columns<N, 1> at(c, a.width);
-        Sum<DDP_FP32, N, 1> sum;
-        sum.tokens(p, at, to - from, [&](int k) { return (blockIdx.x + from + k) * 2 + (from + k == 0 ? 1u : 0u); });
-        if (wave > 0) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) part[wave][k * 64 + lane] = sum.acc[0][k];
+    auto part_of = [&](int l, int i) { return (blockIdx.x * kJoinWindows + l + i) * 2 + (i == 0 ? 1u : 0u); };
+    uint64_t few = __ballot(parts_here > 0 && parts_here <= kJoinAlone), many = __ballot(parts_here > kJoinAlone);
+    for (int i = 0; few != 0; ++i, few &= few - 1) {
+        if (i % kJoinWaves != wave) continue;
+        const int l = __ffsll(static_cast<unsigned long long>(few)) - 1;
+        const int parts = static_cast<int>(lane_value(parts_here, l));
+        const int64_t row = row_at(a, lane_value(found, l) - 1);
+        for (int c = blockIdx.y * (64 * N); c < a.width; c += gridDim.y * (64 * N)) {
+            const Columns<N, 1> at(c, a.width);
+            Sum<DDP_FP32, N, 1> sum;
+            sum.tokens(p, at, parts, [&](int k) { return part_of(l, k); });
+            sum.template put<GT>(a, at, row);
         }
-        __syncthreads();
-        if (wave == 0) {
-            for (int w = 1; w < kJoinWaves; ++w)
+    }
+    for (; many != 0; many &= many - 1) {
+        const int l = __ffsll(static_cast<unsigned long long>(many)) - 1;
+        const int parts = static_cast<int>(lane_value(parts_here, l)), share = (parts + kJoinWaves - 1) / kJoinWaves;
+        const int64_t row = row_at(a, lane_value(found, l) - 1);
+        const int from = min(wave * share, parts), to = min(from + share, parts);
+        for (int c = blockIdx.y * (64 * N); c < a.width; c += gridDim.y * (64 * N)) {
+            const Columns<N, 1> at(c, a.width);
+            Sum<DDP_FP32, N, 1> sum;
+            sum.tokens(p, at, to - from, [&](int k) { return part_of(l, from + k); });
+            if (wave > 0) {
 #pragma unroll
-                for (int k = 0; k < N; ++k) sum.acc[0][k] += part[w][k * 64 + lane];
-            sum.template put<GT>(a, at, r);
+                for (int k = 0; k < N; ++k) part[wave][k * 64 + lane] = sum.acc[0][k];
+            }
+            __syncthreads();
+            if (wave == 0) {
+                for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+                    for (int k = 0; k < N; ++k) sum.acc[0][k] += part[w][k * 64 + lane];
+                sum.template put<GT>(a, at, row);
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
@@ -649,11 +793,10 @@ struct ddp_embedding {
     int32_t device = DDP_DEVICE_NONE;
     hipStream_t stream = nullptr;
     int64_t rows = 0, width = 0, max_tokens = 0;
-    int32_t shift = 0, buckets = 0;
+    int32_t bucket_bits = 0, shift = 0;          // 2^bucket_bits buckets of 2^shift rows
     char* mem = nullptr;                         // workspace of the gradient
     uint16_t* starts = nullptr;
-    uint64_t* gathered = nullptr;
-    uint32_t *list = nullptr, *sorted = nullptr, *first = nullptr;
+    uint32_t *list = nullptr, *gathered = nullptr, *sorted = nullptr, *first = nullptr, *split = nullptr;
     float* partial = nullptr;
     std::string err;
 };
@@ -676,18 +819,25 @@ int32_t fail(ddp_embedding* e, int32_t code, const char* msg) {
     } while (0)
 
 // Blocks of one column range each for the joins of a launch.
-constexpr int kJoinRanges = 4;
+constexpr int kJoinRanges = 16;
 
 template <typename Id, int WT, int OT>
 void launch_lookup(ddp_embedding* e, int64_t tokens, const void* ids, const void* table, int64_t table_stride, float scale, void* out, int64_t out_stride) {
     constexpr int N = WT == DDP_FP32 || OT == DDP_FP32 ? 4 : 8;
     const dim3 grid(static_cast<unsigned>((tokens + kWaves - 1) / kWaves)), block(kThreads);
-    if (e->width >= N)
-        hipLaunchKernelGGL((lookup_kernel<Id, WT, OT, N>), grid, block, 0, e->stream, static_cast<const Id*>(ids), tokens,
-                           static_cast<const char*>(table), e->rows, static_cast<int>(e->width), table_stride, scale, static_cast<char*>(out), out_stride);
+    const int stream = tokens * e->width * ElemBytes<OT>::value >= kStreamBytes;
+    auto* const from = static_cast<const char*>(table);
+    auto* const to = static_cast<char*>(out);
+    const int width = static_cast<int>(e->width);
+    if (width < N)
+        hipLaunchKernelGGL((lookup_kernel<Id, WT, OT, 1>), grid, block, 0, e->stream, static_cast<const Id*>(ids), tokens, from, e->rows, width, table_stride,
+                           scale, to, out_stride, stream);
+    else if (width > 32 * N)
+        hipLaunchKernelGGL((lookup_kernel<Id, WT, OT, N>), grid, block, 0, e->stream, static_cast<const Id*>(ids), tokens, from, e->rows, width, table_stride,
+                           scale, to, out_stride, stream);
     else
-        hipLaunchKernelGGL((lookup_kernel<Id, WT, OT, 1>), grid, block, 0, e->stream, static_cast<const Id*>(ids), tokens,
-                           static_cast<const char*>(table), e->rows, static_cast<int>(e->width), table_stride, scale, static_cast<char*>(out), out_stride);
+        hipLaunchKernelGGL((narrow_lookup_kernel<Id, WT, OT, N>), dim3(static_cast<unsigned>((tokens * ((width + N - 1) / N) + kThreads - 1) / kThreads)), block, 0,
+                           e->stream, static_cast<const Id*>(ids), static_cast<unsigned>(tokens), from, e->rows, width, table_stride, scale, to, out_stride, stream);
 }
 template <typename Id, typename... Rest>
 void launch_lookup(int wt, int ot, Rest... rest) {
@@ -704,32 +854,40 @@ void launch_lookup(int wt, int ot, Rest... rest) {
     }
 }
 
-template <typename Id, int FT, int GT, int N, int GROUPS>
+template <typename Id, int FT, int GT, int N>
 hipError_t launch_scan(ddp_embedding* e, SumArgs a) {
-    a.units = static_cast<int32_t>((a.width + 64 * N * GROUPS - 1) / (64 * N * GROUPS));
+    a.units = static_cast<int32_t>((a.width + 64 * N - 1) / (64 * N));
     const int64_t blocks = int64_t(1) << a.log2_blocks;
-    const size_t flags = static_cast<size_t>(((a.rows >> a.log2_blocks) + 32) / 32) * 4;
-    hipLaunchKernelGGL((scan_sum_kernel<Id, FT, GT, N, GROUPS>), dim3(static_cast<unsigned>(std::min(blocks, a.rows))), dim3(kScanThreads), flags, e->stream, a);
+    const size_t counters = (static_cast<size_t>(a.rows >> a.log2_blocks) + 1) * 4;
+    const unsigned ranges = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(a.units, kScanBlocks / std::min(blocks, a.rows))));
+    hipLaunchKernelGGL((scan_sum_kernel<Id, FT, GT, N>), dim3(static_cast<unsigned>(std::min(blocks, a.rows)), ranges), dim3(kScanThreads), counters, e->stream, a);
     return hipGetLastError();
 }
-template <typename Id, int FT, int GT, int N, int GROUPS>
+template <int FT, int GT, int N, int WN>
 hipError_t launch_rows(ddp_embedding* e, SumArgs a) {
-    a.units = static_cast<int32_t>((a.width + 64 * N * GROUPS - 1) / (64 * N * GROUPS));
-    a.window_blocks = static_cast<int32_t>((static_cast<int64_t>(a.windows) * a.units + kWaves - 1) / kWaves);
-    const int64_t blocks = a.window_blocks + (a.rows + kRowsPerBlock - 1) / kRowsPerBlock;
-    hipLaunchKernelGGL((row_sum_kernel<Id, FT, GT, N, GROUPS>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, e->stream, a);
+    auto ranges_of = [&](int columns) { return static_cast<int32_t>((a.width + columns - 1) / columns); };
+    a.units = ranges_of(64 * N);
+    a.window_units = ranges_of(64 * WN);
+    a.window_blocks = static_cast<int32_t>((static_cast<int64_t>(a.windows) * a.window_units + kWaves - 1) / kWaves);
+    a.rows_per_block = std::max(8, std::min(64, kRowColumns / a.width));
+    a.row_blocks = static_cast<int32_t>((a.rows + a.rows_per_block - 1) / a.rows_per_block);
+    const int64_t blocks = static_cast<int64_t>(a.window_blocks) + a.row_blocks;
+    hipLaunchKernelGGL((row_sum_kernel<FT, GT, N, WN>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, e->stream, a);
     const hipError_t err = hipGetLastError();
-    if (err != hipSuccess || a.windows <= 1) return err;
+    if (err != hipSuccess) return err;
     constexpr int JN = N == 1 ? 1 : 4;
-    const int ranges = std::min(kJoinRanges, (a.width + 64 * JN - 1) / (64 * JN));
-    hipLaunchKernelGGL((row_join_kernel<Id, GT, JN>), dim3(static_cast<unsigned>(a.windows), static_cast<unsigned>(ranges)), dim3(kJoinThreads), 0, e->stream, a);
+    const int ranges = std::min(kJoinRanges, ranges_of(64 * JN));
+    hipLaunchKernelGGL((row_join_kernel<GT, JN>), dim3(static_cast<unsigned>((a.windows + kJoinWindows - 1) / kJoinWindows), static_cast<unsigned>(ranges)),
+                       dim3(kJoinThreads), 0, e->stream, a);
     return hipGetLastError();
 }
 template <typename Id, int FT, int GT>
 hipError_t launch_sum(ddp_embedding* e, const SumArgs& a, bool scan) {
-    constexpr int N = FT == DDP_FP32 ? 4 : 8;
-    if (a.width < N) return scan ? launch_scan<Id, FT, GT, 1, 1>(e, a) : launch_rows<Id, FT, GT, 1, 1>(e, a);
-    return scan ? launch_scan<Id, FT, GT, N, 16 / N>(e, a) : launch_rows<Id, FT, GT, N, 16 / N>(e, a);
+    constexpr int N = FT == DDP_FP32 || GT == DDP_FP32 ? 4 : 8;    // 16 bytes of the wider side: stores of whole lines
+    constexpr int WN = FT == DDP_FP32 ? 4 : 8;
+    if (a.width < WN) return scan ? launch_scan<Id, FT, GT, 1>(e, a) : launch_rows<FT, GT, 1, 1>(e, a);
+    if (!scan) return launch_rows<FT, GT, N, WN>(e, a);
+    return launch_scan<Id, FT, GT, N>(e, a);
 }
 template <typename Id>
 hipError_t launch_sum(int ft, int gt, ddp_embedding* e, const SumArgs& a, bool scan) {
@@ -751,7 +909,7 @@ hipError_t launch_sort(ddp_embedding* e, const SortArgs& a) {
     hipLaunchKernelGGL((chunk_sort_kernel<Id>), dim3(a.chunks), dim3(kChunk), static_cast<size_t>(a.buckets) * 4, e->stream, a);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(bucket_sort_kernel, dim3(a.buckets), dim3(kSortThreads), (static_cast<size_t>(kSortWaves) << a.shift) * 4, e->stream, a);
+    hipLaunchKernelGGL(bucket_sort_kernel, dim3(a.buckets), dim3(kSortThreads), (static_cast<size_t>(kSortWaves + 1) << a.shift) * 4, e->stream, a);
     return hipGetLastError();
 }
 
@@ -769,7 +927,7 @@ int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, 
     if (device < DDP_DEVICE_NONE) return fail(nullptr, DDP_ERR_ARG, "ddp_embedding_create: bad device");
     if (rows < 1 || width < 1 || max_tokens < 0) return fail(nullptr, DDP_ERR_ARG, "ddp_embedding_create: rows and width are at least 1, max_tokens at least 0");
     if (rows > kMaxRows || width > kMaxWidth || max_tokens > kMaxTokens)
-        return fail(nullptr, DDP_ERR_UNSUPPORTED, "ddp_embedding_create: more than 2^23 rows, 2^20 columns or 2^24 tokens");
+        return fail(nullptr, DDP_ERR_UNSUPPORTED, "ddp_embedding_create: more than 2^23 rows, 2^20 columns or 2^22 tokens");
     if (device != DDP_DEVICE_NONE) {
         int count = 0;
         if (hipGetDeviceCount(&count) != hipSuccess || device >= count)
@@ -782,25 +940,27 @@ int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, 
     e->rows = rows;
     e->width = width;
     e->max_tokens = max_tokens;
-    while (e->shift < 10 && ((rows - 1) >> e->shift) + 1 > 1024) ++e->shift;
-    e->buckets = static_cast<int32_t>(((rows - 1) >> e->shift) + 1);
-    static_assert((kMaxRows >> 10) <= kMaxBuckets && (1 << 10) <= kSortRows, "LDS of the sorting kernels");
+    // up to 1024 buckets, more where a bucket would have more than kSortRows rows
+    while ((int64_t(1) << (e->bucket_bits + e->shift)) < rows) ++(e->bucket_bits < 10 || e->shift == 10 ? e->bucket_bits : e->shift);
+    static_assert((kMaxRows >> 10) <= kMaxBuckets && (1 << 10) == kSortRows, "LDS of the sorting kernels");
     if (device != DDP_DEVICE_NONE && max_tokens > 0) {
         const int64_t chunks = (max_tokens + kChunk - 1) / kChunk;
-        const int64_t gathered = up(max_tokens * 8, 256), tokens = up(max_tokens * 4, 256), first = up((rows + 1) * 4, 256);
-        const int64_t partial = up((max_tokens + kWindow - 1) / kWindow * 2 * width * 4, 256), starts = up(chunks * (e->buckets + 1) * 2, 256);
+        const int64_t places = int64_t(1) << (e->bucket_bits + e->shift), buckets = int64_t(1) << e->bucket_bits;
+        const int64_t tokens = up(max_tokens * 4, 256), first = up((places + 1) * 4, 256), starts = up(chunks * (buckets + 1) * 2, 256);
+        const int64_t split = up(chunks * (2 * kChunk / kWindow) * 4, 256), partial = up((max_tokens + kWindow - 1) / kWindow * 2 * width * 4, 256);
         hipError_t err = hipSetDevice(device);
-        if (err == hipSuccess) err = hipMalloc(reinterpret_cast<void**>(&e->mem), gathered + 2 * tokens + first + partial + starts);
+        if (err == hipSuccess) err = hipMalloc(reinterpret_cast<void**>(&e->mem), 3 * tokens + first + split + partial + starts);
         if (err != hipSuccess) {
             delete e;
             return fail(nullptr, DDP_ERR_HIP, hipGetErrorString(err));
         }
         char* at = e->mem;
-        e->gathered = reinterpret_cast<uint64_t*>(at);
-        e->list = reinterpret_cast<uint32_t*>(at += gathered);
+        e->gathered = reinterpret_cast<uint32_t*>(at);
+        e->list = reinterpret_cast<uint32_t*>(at += tokens);
         e->sorted = reinterpret_cast<uint32_t*>(at += tokens);
         e->first = reinterpret_cast<uint32_t*>(at += tokens);
-        e->partial = reinterpret_cast<float*>(at += first);
+        e->split = reinterpret_cast<uint32_t*>(at += first);
+        e->partial = reinterpret_cast<float*>(at += split);
         e->starts = reinterpret_cast<uint16_t*>(at += partial);
     }
     *out = e;
@@ -821,7 +981,7 @@ int32_t ddp_embedding_destroy(ddp_embedding* e) {
 int32_t ddp_embedding_lookup(ddp_embedding* e, int64_t tokens, const void* ids, int32_t id_bits, const void* table, int32_t table_dtype,
                              int64_t table_stride, float scale, void* out, int32_t out_dtype, int64_t out_stride) {
     if (!e) return DDP_ERR_ARG;
-    if (tokens < 0 || tokens > kMaxTokens) return fail(e, DDP_ERR_ARG, "ddp_embedding_lookup: tokens outside [0, 2^24]");
+    if (tokens < 0 || tokens > kMaxTokens) return fail(e, DDP_ERR_ARG, "ddp_embedding_lookup: tokens outside [0, 2^22]");
     if (id_bits != 32 && id_bits != 64) return fail(e, DDP_ERR_ARG, "ddp_embedding_lookup: ids have 32 or 64 bits");
     if (!known_dtype(table_dtype) || !known_dtype(out_dtype)) return fail(e, DDP_ERR_ARG, "ddp_embedding_lookup: unknown dtype");
     if (table_stride < e->width || out_stride < e->width || table_stride > INT32_MAX || out_stride > INT32_MAX)
@@ -860,20 +1020,22 @@ int32_t ddp_embedding_grad(ddp_embedding* e, int64_t tokens, const void* ids, in
     a.dout = static_cast<const char*>(dout);
     a.grad = static_cast<char*>(grad);
     a.partial = e->partial;
+    a.split = e->split;
     a.tokens = tokens;
     a.rows = e->rows;
     a.width = static_cast<int32_t>(e->width);
     a.dout_stride = dout_stride;
     a.grad_stride = grad_stride;
     a.padding = padding_row;
-    a.window = kWindow;
-    a.windows = static_cast<int32_t>((tokens + a.window - 1) / a.window);
+    a.windows = static_cast<int32_t>((tokens + kWindow - 1) / kWindow);
     a.add = accumulate != 0;
     a.scale = scale;
+    a.shift = e->shift;
+    a.bucket_bits = e->bucket_bits;
     const int64_t each = std::min<int64_t>(1024, std::max<int64_t>(kScanRows, kScanRows * 1024 / e->width));
     while ((a.rows - 1) >> a.log2_blocks >= each) ++a.log2_blocks;
     while (a.log2_blocks < 9 && (int64_t(1) << a.log2_blocks) < a.rows) ++a.log2_blocks;
-    const bool scan = tokens <= kScanTokens;
+    const bool scan = tokens <= std::min<int64_t>(kScanTokens, std::max<int64_t>(1024, 128 * e->rows));
     if (!scan) {
         SortArgs s{};
         s.ids = ids;
@@ -881,14 +1043,15 @@ int32_t ddp_embedding_grad(ddp_embedding* e, int64_t tokens, const void* ids, in
         s.rows = e->rows;
         s.padding = padding_row;
         s.shift = e->shift;
-        s.buckets = e->buckets;
-        while ((1 << s.bucket_bits) < s.buckets) ++s.bucket_bits;
+        s.buckets = 1 << e->bucket_bits;
+        s.bucket_bits = e->bucket_bits;
         s.chunks = static_cast<int32_t>((tokens + kChunk - 1) / kChunk);
         s.starts = e->starts;
         s.list = e->list;
         s.gathered = e->gathered;
         s.sorted = e->sorted;
         s.first = e->first;
+        s.split = e->split;
         EMB_HIP(e, id_bits == 32 ? launch_sort<int32_t>(e, s) : launch_sort<int64_t>(e, s));
     }
     EMB_HIP(e, id_bits == 32 ? launch_sum<int32_t>(dout_dtype, grad_dtype, e, a, scan) : launch_sum<int64_t>(dout_dtype, grad_dtype, e, a, scan));

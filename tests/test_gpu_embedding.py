@@ -172,6 +172,15 @@ def test_grad_sizes(rows, width, tokens, spread):
     check_grad(rows, width, ids, BF16, FP32)
 
 
+@pytest.mark.parametrize("rows,tokens", [(1 << 20, 5000), ((1 << 20) + 3, 9000), (70000, 30000)])
+def test_grad_many_rows(rows, tokens):
+    """Buckets of up to 1024 rows, more than 1024 buckets; spread thin, and with frequent rows."""
+    rng = np.random.default_rng(rows)
+    check_grad(rows, 4, rng.integers(0, rows, tokens), BF16, FP32)
+    check_grad(rows, 4, zipf(rng, rows, tokens), FP32, FP32, add=True)
+    check_grad(rows, 4, rng.integers(0, 3, tokens) * 1024 + rng.integers(0, 2, tokens), FP16, FP32)
+
+
 @pytest.mark.parametrize("tokens", [0, 1, 31, 32, 33, 63, 64, 65, 96, 97, 4095, 4096, 4097])
 def test_grad_of_one_row(tokens):
     """Every length at which a row's tokens are split or end a part, next to rows with one token."""
@@ -225,6 +234,16 @@ def test_grad_values_that_are_not_finite_stay_in_their_row():
     bad = (~torch.isfinite(grad)).nonzero().cpu().tolist()
     assert bad == [[1, 2], [3, 5]]
     t.close()
+
+
+@pytest.mark.parametrize("tokens", [4097, 9000, 40000])
+def test_grad_long_calls_of_few_rows(tokens):
+    """Every row is split into many parts; a bucket holds more tokens than LDS does."""
+    rng = np.random.default_rng(tokens)
+    check_grad(2, 260, rng.integers(0, 2, tokens), FP32, FP32)
+    check_grad(1, 8, np.zeros(tokens), BF16, BF16)
+    check_grad(40, 12, zipf(rng, 40, tokens), BF16, FP32, padding=0, poison=True)
+    check_grad(3000, 9, np.where(rng.random(tokens) < 0.7, 1024, rng.integers(0, 3000, tokens)), FP16, FP32)
 
 
 def test_grad_calls_do_not_see_each_other():
