@@ -40,7 +40,8 @@ constexpr int kHeaderBytes = 256;                // of a state: the number of st
 constexpr int kNormTiles = 4;                    // tiles that a block of a long norm takes
 constexpr int kNormLong = 4096;                  // tiles from which it is one; us, one tile a block / four: 7 M elements 9.4 / 14.0,
                                                  // 25.6 M 23.7 / 19.4, BERT-large in bfloat16 152 / 106 (eight: 120)
-constexpr int kNormAlone = 64;                   // tiles up to which the norm is one launch
+constexpr int kNormAlone = 768;                  // tiles up to which the norm is one launch; us, one / two: 500 thousand
+                                                 // elements 4.9 / 6.5, 2 M 5.9 / 6.6, 3 M 6.7 / 6.5, 10 M 13.7 / 11.9
 constexpr int kMaskWords = 768;                  // words of the used mask that travel in one launch's arguments
 
 struct OptSeg {                                  // 64 bytes
@@ -56,11 +57,10 @@ static_assert(sizeof(OptSeg) == 64, "one scalar load of sixteen words");
 
 struct NormState {                               // in device memory
     double norm;                                 // of the registered gradients, unscaled
-    uint32_t arrived;                            // blocks of the running norm launch that are done; 0 between launches
 };
-// Blocks of the running step that are done, in kCounters groups with a cache line each, and the groups that are; 0 between launches.
+// Blocks of a running launch that are done, in kCounters groups with a cache line each, and the groups that are; 0 between launches.
 // (One counter for all blocks took 10 ns a block, one after the other.)
-constexpr int kCounters = 64, kCounterWords = 32;
+constexpr int kCounters = 64, kCounterWords = 32, kCounterSet = (1 + kCounters) * kCounterWords;
 
 struct StepArgs {
     const OptSeg* seg;
@@ -249,6 +249,21 @@ __device__ __forceinline__ bool skips(const StepArgs& a) {
     return a.skip_nonfinite && !isfinite(table_load(&a.norm->norm));
 }
 
+// Called by one thread of each block: whether all other blocks have been here.  What they have stored before with device-scope
+// atomics (which write through the caches) and waited for is then there to be read likewise; a release would write
+// back the caches instead, which took 35 ns a block, one after the other.
+__device__ __forceinline__ bool arrives_last(uint32_t* counters) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const unsigned group = blockIdx.x % kCounters, in_group = (gridDim.x - group + kCounters - 1) / kCounters;
+    uint32_t* mine = counters + (1 + group) * kCounterWords;
+    if (__hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != in_group - 1) return false;
+    __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const unsigned groups = gridDim.x < kCounters ? gridDim.x : kCounters;
+    if (__hip_atomic_fetch_add(counters, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != groups - 1) return false;
+    __hip_atomic_store(counters, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+
 template <int PT, int GT, int CT, bool Q8>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a, int64_t tile_base) {
     const int64_t tile = tile_base + blockIdx.x;
@@ -262,15 +277,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(StepArgs a, int64_t til
     if (a.counters == nullptr) return;
     // the last block to get here counts the step: every block has read the old number by then
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    const unsigned group = blockIdx.x % kCounters, in_group = (gridDim.x - group + kCounters - 1) / kCounters;
-    uint32_t* mine = a.counters + (1 + group) * kCounterWords;
-    if (__hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != in_group - 1) return;
-    __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const unsigned groups = gridDim.x < kCounters ? gridDim.x : kCounters;
-    if (__hip_atomic_fetch_add(a.counters, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != groups - 1) return;
-    __hip_atomic_store(a.counters, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *a.step += 1;
+    if (threadIdx.x == 0 && arrives_last(a.counters)) *a.step += 1;
 }
 
 // Counts a step whose launch has too many blocks to do it by itself, or that had none.
@@ -290,6 +297,7 @@ struct NormArgs {
     const int32_t* tile_seg;
     const uint32_t* used;
     NormState* state;
+    uint32_t* counters;
     double* partial;                             // one a block
     float* out;                                  // may be null
     int64_t tiles;
@@ -340,8 +348,7 @@ __device__ __forceinline__ void put_norm(const NormArgs& a, double squares) {
 // costs in lists that fit the 256 MB cache: 12 M elements 12.4 us without, 15.5 with it).
 // Squares are summed in 64 bits: no gradient that a binary32 holds overflows or is lost.  The order of the sum (tiles by
 // block, blocks by index) does not depend on which block is last.
-// LAST: the block that arrives last adds the others' sums up, in place of a launch.  Arriving is an atomic with a
-// release, which costs 35 ns a block, one after the other: for launches of a few blocks.
+// LAST: the block that arrives last adds the others' sums up, in place of another launch.
 template <int TILES, bool LAST>
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(NormArgs a) {
     double sum = 0.0;
@@ -365,19 +372,16 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(NormArgs a) {
     __shared__ bool last;
     if (threadIdx.x == 0) {
         __hip_atomic_store(a.partial + blockIdx.x, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = __hip_atomic_fetch_add(&a.state->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        last = arrives_last(a.counters);
     }
     __syncthreads();
-    if (!last || threadIdx.x >= 64) return;
+    if (!last) return;
     double total = 0.0;
-    for (int i = threadIdx.x; i < static_cast<int>(gridDim.x); i += 64)
+    for (int i = threadIdx.x; i < static_cast<int>(gridDim.x); i += kThreads)
         total += __hip_atomic_load(a.partial + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
-    if (threadIdx.x == 0) {
-        __hip_atomic_store(&a.state->arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        put_norm(a, total);
-    }
+    __syncthreads();                                 // block_sum's words are free again
+    total = block_sum<kThreads>(total);
+    if (threadIdx.x == 0) put_norm(a, total);
 }
 
 __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a, int blocks) {
@@ -560,7 +564,7 @@ int32_t build(ddp_opt* o) {
         return at;
     };
     const int64_t at_seg = take(static_cast<int64_t>(seg.size() * sizeof(OptSeg))), at_step = take(tiles * 4), at_norm = take(norm_tiles * 4);
-    const int64_t at_used = take((n + 31) / 32 * 4), at_counters = take((1 + kCounters) * kCounterWords * 4), at_state = take(sizeof(NormState));
+    const int64_t at_used = take((n + 31) / 32 * 4), at_counters = take(2 * kCounterSet * 4), at_state = take(sizeof(NormState));
     const int64_t at_partial = take(std::max(std::min<int64_t>(norm_tiles, kNormLong), (norm_tiles + kNormTiles - 1) / kNormTiles) * 8);
     OPT_HIP(o, hipMalloc(reinterpret_cast<void**>(&o->mem), bytes));
     o->d_seg = reinterpret_cast<OptSeg*>(o->mem + at_seg);
@@ -575,8 +579,8 @@ int32_t build(ddp_opt* o) {
         OPT_HIP(o, hipMemcpy(o->d_step_seg, step_seg.data(), step_seg.size() * 4, hipMemcpyHostToDevice));
         OPT_HIP(o, hipMemcpy(o->d_norm_seg, norm_seg.data(), norm_seg.size() * 4, hipMemcpyHostToDevice));
     }
-    const uint32_t none[(1 + kCounters) * kCounterWords] = {};
-    OPT_HIP(o, hipMemcpy(o->d_counters, none, sizeof none, hipMemcpyHostToDevice));
+    const std::vector<uint32_t> none(2 * kCounterSet);       // the step's and the norm's
+    OPT_HIP(o, hipMemcpy(o->d_counters, none.data(), none.size() * 4, hipMemcpyHostToDevice));
     const NormState zero{};
     OPT_HIP(o, hipMemcpy(o->d_norm, &zero, sizeof zero, hipMemcpyHostToDevice));
     o->norm_tiles = norm_tiles;
@@ -802,6 +806,7 @@ int32_t ddp_opt_grad_norm(ddp_opt* o, double grad_scale, const uint8_t* used, fl
         a.seg = o->d_seg;
         a.tile_seg = o->d_norm_seg;
         a.state = o->d_norm;
+        a.counters = o->d_counters + kCounterSet;
         a.partial = o->d_partial;
         a.out = norm_out;
         a.tiles = o->norm_tiles;
