@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from operator import index as _index
 from typing import Optional, Sequence
 
 import numpy as np
@@ -276,6 +277,10 @@ _mark, _finalize, _mark_local, _many, _accumulate, _static = (
 _fast.bind(_mark, _finalize, _mark_local, _i32, _many, _accumulate, _static)
 _fast_mark, _fast_finalize, _fast_mark_local = _fast.mark_ready, _fast.finalize_backward, _fast.mark_ready_local
 _fast_many, _fast_accumulate, _fast_static = _fast.mark_ready_many, _fast.no_sync_accumulate, _fast.sync_static
+_fast.bind_around(*(C.cast(f, _vp).value for f in (_lib.ddp_embedding_lookup, _lib.ddp_embedding_grad,
+                                                   _lib.ddp_opt_grad_norm, _lib.ddp_opt_adamw_step)))
+_fast_lookup, _fast_grad = _fast.embedding_lookup, _fast.embedding_grad
+_fast_norm, _fast_step = _fast.opt_grad_norm, _fast.opt_adamw_step
 
 
 def _address(ctx):
@@ -419,6 +424,10 @@ def _sized(values, n: int, what: str, convert):
     return arr
 
 
+def _pointer(address):
+    return _vp(None if address is None else _index(address) or None)
+
+
 def _f32_array(values) -> np.ndarray:
     return np.ascontiguousarray(values, dtype=np.float32)
 
@@ -487,8 +496,10 @@ def ddp_opt_set_state(opt, kind: int, state: int, nbytes: int) -> None:
 
 
 def ddp_opt_grad_norm(opt, grad_scale: float = 1.0, norm_out: int = 0, used=None) -> None:
-    flags = _flags(used, opt)
-    status = _lib.ddp_opt_grad_norm(opt, grad_scale, _or_null(flags, C.c_uint8), norm_out or None)
+    status = _fast_norm(_address(opt), grad_scale, norm_out) if used is None else None
+    if status is None:
+        flags = _flags(used, opt)
+        status = _lib.ddp_opt_grad_norm(opt, float(grad_scale), _or_null(flags, C.c_uint8), _pointer(norm_out))
     if status < 0:
         _check_opt(opt, status)
 
@@ -496,9 +507,13 @@ def ddp_opt_grad_norm(opt, grad_scale: float = 1.0, norm_out: int = 0, used=None
 def ddp_opt_adamw_step(opt, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                        weight_decay: float = 0.0, grad_scale: float = 1.0, max_norm: float = 0.0,
                        skip_nonfinite: bool = False, used=None) -> None:
-    flags = _flags(used, opt)
-    status = _lib.ddp_opt_adamw_step(opt, lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm,
-                                     1 if skip_nonfinite else 0, _or_null(flags, C.c_uint8))
+    status = None
+    if used is None:
+        status = _fast_step(_address(opt), lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm, skip_nonfinite)
+    if status is None:
+        flags = _flags(used, opt)
+        hyper = [float(x) for x in (lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm)]
+        status = _lib.ddp_opt_adamw_step(opt, *hyper, 1 if skip_nonfinite else 0, _or_null(flags, C.c_uint8))
     if status < 0:
         _check_opt(opt, status)
 
@@ -533,8 +548,12 @@ def ddp_embedding_destroy(emb) -> None:
 
 def ddp_embedding_lookup(emb, tokens: int, ids: int, id_bits: int, table: int, table_dtype: int, table_stride: int,
                          scale: float, out: int, out_dtype: int, out_stride: int) -> None:
-    status = _lib.ddp_embedding_lookup(emb, tokens, ids, id_bits, table, table_dtype, table_stride, scale, out,
-                                       out_dtype, out_stride)
+    status = _fast_lookup(_address(emb), tokens, ids, id_bits, table, table_dtype, table_stride, scale, out,
+                          out_dtype, out_stride)
+    if status is None:
+        status = _lib.ddp_embedding_lookup(emb, _index(tokens), _pointer(ids), _index(id_bits), _pointer(table),
+                                           _index(table_dtype), _index(table_stride), float(scale), _pointer(out),
+                                           _index(out_dtype), _index(out_stride))
     if status < 0:
         _check_embedding(emb, status)
 
@@ -542,7 +561,11 @@ def ddp_embedding_lookup(emb, tokens: int, ids: int, id_bits: int, table: int, t
 def ddp_embedding_grad(emb, tokens: int, ids: int, id_bits: int, dout: int, dout_dtype: int, dout_stride: int,
                        scale: float, padding_row: int, accumulate: bool, grad: int, grad_dtype: int,
                        grad_stride: int) -> None:
-    status = _lib.ddp_embedding_grad(emb, tokens, ids, id_bits, dout, dout_dtype, dout_stride, scale, padding_row,
-                                     1 if accumulate else 0, grad, grad_dtype, grad_stride)
+    status = _fast_grad(_address(emb), tokens, ids, id_bits, dout, dout_dtype, dout_stride, scale, padding_row,
+                        accumulate, grad, grad_dtype, grad_stride)
+    if status is None:
+        status = _lib.ddp_embedding_grad(emb, _index(tokens), _pointer(ids), _index(id_bits), _pointer(dout),
+                                         _index(dout_dtype), _index(dout_stride), float(scale), _index(padding_row),
+                                         1 if accumulate else 0, _pointer(grad), _index(grad_dtype), _index(grad_stride))
     if status < 0:
         _check_embedding(emb, status)

@@ -2,7 +2,9 @@
  * parameter (Algorithm 1's autograd_hook fires per gradient), ddp_mark_ready,
  * ddp_mark_ready_local, ddp_finalize_backward, and for those that take a list with
  * an entry per parameter or per tensor, ddp_mark_ready_many,
- * ddp_no_sync_accumulate, ddp_sync_static.  Through ctypes such a call costs
+ * ddp_no_sync_accumulate, ddp_sync_static, and for the calls whose kernels take
+ * a few microseconds, ddp_embedding_lookup, ddp_embedding_grad, ddp_opt_grad_norm,
+ * ddp_opt_adamw_step.  Through ctypes such a call costs
  * about a microsecond of interpreter time, which for a model with hundreds of
  * parameters is as long as the synchronization itself; here it is an integer
  * conversion and an indirect call.  No arithmetic of the method happens here:
@@ -312,7 +314,117 @@ static PyObject* finalize_backward(PyObject* self, PyObject* const* args, Py_ssi
     return PyLong_FromLong((long)g_finalize(ctx));
 }
 
+typedef int32_t (*lookup_fn)(void*, int64_t, const void*, int32_t, const void*, int32_t, int64_t, float, void*, int32_t, int64_t);
+typedef int32_t (*grad_fn)(void*, int64_t, const void*, int32_t, const void*, int32_t, int64_t, float, int64_t, int32_t, void*, int32_t, int64_t);
+typedef int32_t (*norm_fn)(void*, double, const uint8_t*, float*);
+typedef int32_t (*step_fn)(void*, double, double, double, double, double, double, double, int32_t, const uint8_t*);
+
+static lookup_fn g_lookup = NULL;
+static grad_fn g_grad = NULL;
+static norm_fn g_norm = NULL;
+static step_fn g_step = NULL;
+
+/* bind_around(embedding_lookup, embedding_grad, opt_grad_norm, opt_adamw_step): the addresses of the C entry points */
+static PyObject* bind_around(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 4) {
+        PyErr_SetString(PyExc_TypeError, "bind_around(embedding_lookup, embedding_grad, opt_grad_norm, opt_adamw_step)");
+        return NULL;
+    }
+    void* a[4];
+    for (Py_ssize_t i = 0; i < 4; ++i) {
+        a[i] = PyLong_AsVoidPtr(args[i]);
+        if (a[i] == NULL && PyErr_Occurred()) return NULL;
+    }
+    g_lookup = (lookup_fn)a[0];
+    g_grad = (grad_fn)a[1];
+    g_norm = (norm_fn)a[2];
+    g_step = (step_fn)a[3];
+    Py_RETURN_NONE;
+}
+
+/* Plain ints, bools and floats, as the C argument; 0 where it is anything else or does not fit: such calls are
+ * left to ctypes (the functions below return None then). */
+static int plain_i64(PyObject* o, int64_t* v) {
+    if (o == Py_True || o == Py_False) {
+        *v = o == Py_True;
+        return 1;
+    }
+    if (!PyLong_CheckExact(o)) return 0;
+    int overflow = 0;
+    const long long x = PyLong_AsLongLongAndOverflow(o, &overflow);
+    *v = (int64_t)x;
+    return !overflow;
+}
+static int plain_i32(PyObject* o, int32_t* v) {
+    int64_t x;
+    if (!plain_i64(o, &x) || x < INT32_MIN || x > INT32_MAX) return 0;
+    *v = (int32_t)x;
+    return 1;
+}
+static int plain_ptr(PyObject* o, void** v) {          /* None or 0: NULL */
+    int64_t x = 0;
+    if (o != Py_None && (!plain_i64(o, &x) || x < 0)) return 0;
+    *v = (void*)(uintptr_t)x;
+    return 1;
+}
+static int plain_f64(PyObject* o, double* v) {
+    if (!PyFloat_CheckExact(o)) return 0;
+    *v = PyFloat_AS_DOUBLE(o);
+    return 1;
+}
+
+/* embedding_lookup(handle_address, ...) -> status, or None */
+static PyObject* embedding_lookup(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    void *e, *ids, *table, *out;
+    int64_t tokens, table_stride, out_stride;
+    int32_t bits, table_dtype, out_dtype;
+    double scale;
+    if (nargs != 11 || g_lookup == NULL || !plain_ptr(a[0], &e) || !plain_i64(a[1], &tokens) || !plain_ptr(a[2], &ids) || !plain_i32(a[3], &bits) ||
+        !plain_ptr(a[4], &table) || !plain_i32(a[5], &table_dtype) || !plain_i64(a[6], &table_stride) || !plain_f64(a[7], &scale) ||
+        !plain_ptr(a[8], &out) || !plain_i32(a[9], &out_dtype) || !plain_i64(a[10], &out_stride))
+        Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_lookup(e, tokens, ids, bits, table, table_dtype, table_stride, (float)scale, out, out_dtype, out_stride));
+}
+
+/* embedding_grad(handle_address, ...) -> status, or None */
+static PyObject* embedding_grad(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    void *e, *ids, *dout, *grad;
+    int64_t tokens, dout_stride, padding, grad_stride;
+    int32_t bits, dout_dtype, add, grad_dtype;
+    double scale;
+    if (nargs != 13 || g_grad == NULL || !plain_ptr(a[0], &e) || !plain_i64(a[1], &tokens) || !plain_ptr(a[2], &ids) || !plain_i32(a[3], &bits) ||
+        !plain_ptr(a[4], &dout) || !plain_i32(a[5], &dout_dtype) || !plain_i64(a[6], &dout_stride) || !plain_f64(a[7], &scale) ||
+        !plain_i64(a[8], &padding) || !plain_i32(a[9], &add) || !plain_ptr(a[10], &grad) || !plain_i32(a[11], &grad_dtype) || !plain_i64(a[12], &grad_stride))
+        Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_grad(e, tokens, ids, bits, dout, dout_dtype, dout_stride, (float)scale, padding, add, grad, grad_dtype, grad_stride));
+}
+
+/* opt_grad_norm(handle_address, grad_scale, norm_out) -> status, or None: all parameters take part */
+static PyObject* opt_grad_norm(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    void *o, *out;
+    double scale;
+    if (nargs != 3 || g_norm == NULL || !plain_ptr(a[0], &o) || !plain_f64(a[1], &scale) || !plain_ptr(a[2], &out)) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_norm(o, scale, NULL, (float*)out));
+}
+
+/* opt_adamw_step(handle_address, lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm, skip_nonfinite) -> status, or None:
+ * all parameters take part */
+static PyObject* opt_adamw_step(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    void* o;
+    double x[7];
+    int32_t skip;
+    if (nargs != 9 || g_step == NULL || !plain_ptr(a[0], &o) || !plain_i32(a[8], &skip)) Py_RETURN_NONE;
+    for (int i = 0; i < 7; ++i)
+        if (!plain_f64(a[1 + i], &x[i])) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_step(o, x[0], x[1], x[2], x[3], x[4], x[5], x[6], skip != 0, NULL));
+}
+
 static PyMethodDef methods[] = {
+    {"bind_around", (PyCFunction)(void (*)(void))bind_around, METH_FASTCALL, "set the C entry points of embedding and optimizer"},
+    {"embedding_lookup", (PyCFunction)(void (*)(void))embedding_lookup, METH_FASTCALL, "ddp_embedding_lookup"},
+    {"embedding_grad", (PyCFunction)(void (*)(void))embedding_grad, METH_FASTCALL, "ddp_embedding_grad"},
+    {"opt_grad_norm", (PyCFunction)(void (*)(void))opt_grad_norm, METH_FASTCALL, "ddp_opt_grad_norm"},
+    {"opt_adamw_step", (PyCFunction)(void (*)(void))opt_adamw_step, METH_FASTCALL, "ddp_opt_adamw_step"},
     {"bind", (PyCFunction)(void (*)(void))bind_entry_points, METH_FASTCALL, "set the C entry points"},
     {"mark_ready", (PyCFunction)(void (*)(void))mark_ready, METH_FASTCALL, "ddp_mark_ready"},
     {"mark_ready_local", (PyCFunction)(void (*)(void))mark_ready_local, METH_FASTCALL, "ddp_mark_ready_local"},

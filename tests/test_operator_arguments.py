@@ -157,3 +157,27 @@ def test_grad_arguments(d, emb):
     for bad in (dict(tokens=-1), dict(tokens=1001), dict(bits=8), dict(dout_dt=3), dict(grad_dt=-1), dict(dout_stride=15),
                 dict(grad_stride=15), dict(padding=100), dict(padding=-2)):
         refused(d, d.DDP_ERR_ARG, call, **bad)
+
+
+def test_arguments_that_are_not_plain(d, emb, opt):
+    """Numpy integers and floats, ints for floats and out-of-range values take the other way through the binding, with the
+    same answers."""
+    i, f = np.int64, np.float32
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_embedding_lookup, emb, i(5), i(256), i(64), 256, 0, i(16), f(1.0), 256, 0, 16)
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_embedding_lookup, emb, 5, 256, 64, 256, 0, 16, 1, 256, 0, 16)
+    refused(d, d.DDP_ERR_ARG, d.ddp_embedding_lookup, emb, i(-1), 256, 64, 256, 0, 16, 1.0, 256, 0, 16)
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_embedding_grad, emb, i(5), 256, 64, 256, 0, 16, 1.0, i(-1), np.bool_(True), 256, 0, 16)
+    refused(d, d.DDP_ERR_ARG, d.ddp_embedding_grad, emb, 5, 256, 64, 256, 0, 16, 1.0, i(100), False, 256, 0, 16)
+    d.ddp_opt_register(opt, [10], [FP32], None, [FP32], None)
+    d.ddp_opt_set_state(opt, d.DDP_STATE_FP32, 0, 1 << 20)
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_opt_grad_norm, opt, f(2.0))
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_opt_grad_norm, opt, 1)
+    refused(d, d.DDP_ERR_NO_DEVICE, d.ddp_opt_adamw_step, opt, 1, eps=f(1e-8), skip_nonfinite=np.bool_(False))
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_adamw_step, opt, f("nan"))
+    refused(d, d.DDP_ERR_ARG, d.ddp_opt_adamw_step, opt, float("nan"))
+    with pytest.raises((TypeError, ValueError)):
+        d.ddp_opt_grad_norm(opt, "x")
+    with pytest.raises(TypeError):
+        d.ddp_embedding_lookup(emb, 5, 256, 64, 256, 0, 16, None, 256, 0, 16)
+    with pytest.raises(TypeError):
+        d.ddp_embedding_lookup(emb, 5.0, 256, 64, 256, 0, 16, 1.0, 256, 0, 16)
