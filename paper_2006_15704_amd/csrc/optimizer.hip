@@ -254,11 +254,14 @@ __device__ __forceinline__ bool skips(const StepArgs& a) {
 // back the caches instead, which took 35 ns a block, one after the other.
 __device__ __forceinline__ bool arrives_last(uint32_t* counters) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    const unsigned group = blockIdx.x % kCounters, in_group = (gridDim.x - group + kCounters - 1) / kCounters;
-    uint32_t* mine = counters + (1 + group) * kCounterWords;
-    if (__hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != in_group - 1) return false;
-    __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const unsigned groups = gridDim.x < kCounters ? gridDim.x : kCounters;
+    unsigned groups = gridDim.x;                     // few blocks count themselves
+    if (gridDim.x > kCounters) {
+        const unsigned group = blockIdx.x % kCounters, in_group = (gridDim.x - group + kCounters - 1) / kCounters;
+        uint32_t* mine = counters + (1 + group) * kCounterWords;
+        if (__hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != in_group - 1) return false;
+        __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        groups = kCounters;
+    }
     if (__hip_atomic_fetch_add(counters, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != groups - 1) return false;
     __hip_atomic_store(counters, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return true;
