@@ -407,14 +407,14 @@ __global__ __launch_bounds__(kThreads) void read_state_kernel(const char* m, con
             const float top = m_top[b];
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = first_moment(top, static_cast<int8_t>(k >> (8 * i)));
-            store_raw<DDP_FP32, 4>(m_out + e, rounded<DDP_FP32, 4>(x));
+            store_raw<DDP_FP32, 4, true>(m_out + e, rounded<DDP_FP32, 4>(x));
         }
         if (v_out != nullptr) {
             const uint32_t k = *reinterpret_cast<const uint32_t*>(v + e);
             const float top = v_top[b];
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[i] = second_moment(top, k >> (8 * i) & 0xFFu);
-            store_raw<DDP_FP32, 4>(v_out + e, rounded<DDP_FP32, 4>(x));
+            store_raw<DDP_FP32, 4, true>(v_out + e, rounded<DDP_FP32, 4>(x));
         }
     }
 }

@@ -164,7 +164,8 @@ def test_grad_types(dout_dt, grad_dt, add):
 
 @pytest.mark.parametrize("rows,width,tokens", [
     (1, 1, 1), (1, 5, 1000), (2, 64, 512), (3, 1024, 2), (16, 8, 17), (17, 520, 33), (1000, 3, 1023), (1024, 16, 1024),
-    (1025, 16, 1025), (2049, 4, 5000), (5000, 40, 100), (40000, 12, 20000), (513, 1030, 600)])
+    (1025, 16, 1025), (2049, 4, 5000), (5000, 40, 100), (40000, 12, 20000), (513, 1030, 600), (70000, 130, 1500),
+    (30001, 30, 4096), (600, 2000, 3000)])
 @pytest.mark.parametrize("spread", ["zipf", "even", "one"])
 def test_grad_sizes(rows, width, tokens, spread):
     rng = np.random.default_rng(rows + tokens)
