@@ -256,6 +256,7 @@ __device__ __forceinline__ void zero_vector(const SumArgs& a, unsigned i, Row ro
 constexpr int kScanThreads = 512, kScanWaves = kScanThreads / 64;
 constexpr int kScanTokens = 4096;
 constexpr int kScanEach = kScanTokens / kScanThreads;
+constexpr int64_t kScanBlockBytes = 8192;        // to move by each of them
 constexpr int kScanBlocks = 4096;                // blocks to have where there are column ranges to go round
 constexpr int kScanAlone = 16;                   // tokens of a row that one wave sums
 constexpr int kScanRows = 32;                    // rows of 1024 columns that a block has at most (up to 1024 of fewer columns)
@@ -516,7 +517,7 @@ constexpr int kWaveTokens = 256;
 
 __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
     __shared__ uint32_t cache[kSortCache];
-    static_assert(kWaveTokens <= kSortCache, "both fit");
+    static_assert(kWaveTokens <= kSortCache && kWaveTokens >= kWindow, "a bucket for the block has more tokens than a window");
     __shared__ uint32_t wave_part[kSortWaves], wave_before[kSortWaves];
     __shared__ uint32_t more[kSortThreads], more_from[kSortThreads], more_to[kSortThreads];
     extern __shared__ uint32_t counters[];           // [kSortWaves + 1][rows of a bucket]
@@ -593,7 +594,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
         return;
     }
     // the bucket's tokens in order: a thread copies up to four of its chunk's, the waves together what there is above that
-    uint32_t* tokens = total <= kSortCache ? cache : a.gathered + base;
+    uint32_t* tokens = a.shift == 0 ? a.sorted + base : total <= kSortCache ? cache : a.gathered + base;     // (a bucket of one row is sorted by then)
     uint32_t done = 0;
     for (int c0 = 0; c0 < a.chunks; c0 += kSortThreads) {
         const int c = c0 + tid;
@@ -639,6 +640,11 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
             }
         }
     }
+    if (a.shift == 0) {
+        if (tid == 0) row_starts(a, rows, place0, 0, base, total);
+        for (uint32_t w = base / kWindow + 1 + tid; w <= (base + total - 1) / kWindow; w += kSortThreads) a.split[w * 2] = 1 + static_cast<uint32_t>(place0);
+        return;
+    }
     __threadfence_block();
     __syncthreads();
     // counting sort by row: every wave has a stretch of the tokens
@@ -678,7 +684,8 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
     }
 }
 
-constexpr int kRowColumns = 8192;                // of the rows of a block: 8 rows of 1024, at most 64 of fewer
+constexpr int kRowColumns = 8192;                // of the rows of a block: 8 rows of 1024, at most 64 of fewer, ...
+constexpr int kRowBlocks = 1024;                 // ... where that leaves so many blocks
 
 template <int FT, int N>
 __device__ __forceinline__ void sum_window(const SumArgs& a, int64_t w, int unit) {
@@ -863,7 +870,8 @@ hipError_t launch_scan(ddp_embedding* e, SumArgs a) {
     a.units = static_cast<int32_t>((a.width + 64 * N - 1) / (64 * N));
     const int64_t blocks = std::min(int64_t(1) << a.log2_blocks, ((a.rows - 1) >> a.log2_run) + 1);
     const size_t counters = ((static_cast<size_t>(a.rows - 1) >> (a.log2_blocks + a.log2_run)) + 1) * (size_t(4) << a.log2_run);
-    const unsigned ranges = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>(a.units, kScanBlocks / blocks)));
+    const int64_t bytes = a.width * (a.rows * ElemBytes<GT>::value + a.tokens * ElemBytes<FT>::value);
+    const unsigned ranges = static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>({a.units, kScanBlocks / blocks, bytes / (kScanBlockBytes * blocks)})));
     hipLaunchKernelGGL((scan_sum_kernel<Id, FT, GT, N>), dim3(static_cast<unsigned>(blocks), ranges), dim3(kScanThreads), counters, e->stream, a);
     return hipGetLastError();
 }
@@ -873,7 +881,7 @@ hipError_t launch_rows(ddp_embedding* e, SumArgs a) {
     a.units = ranges_of(64 * N);
     a.window_units = ranges_of(64 * WN);
     a.window_blocks = static_cast<int32_t>((static_cast<int64_t>(a.windows) * a.window_units + kWaves - 1) / kWaves);
-    a.rows_per_block = std::max(8, std::min(64, kRowColumns / a.width));
+    a.rows_per_block = static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>({64, kRowColumns / a.width, a.rows / kRowBlocks})));
     a.row_blocks = static_cast<int32_t>((a.rows + a.rows_per_block - 1) / a.rows_per_block);
     const int64_t blocks = static_cast<int64_t>(a.window_blocks) + a.row_blocks;
     hipLaunchKernelGGL((row_sum_kernel<FT, GT, N, WN>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, e->stream, a);
