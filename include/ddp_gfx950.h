@@ -576,7 +576,9 @@ int32_t ddp_opt_grad_norm(ddp_opt* opt, double grad_scale, const uint8_t* used, 
 /* One step, with g' = g * grad_scale * min(1, max_norm / (norm + 1e-6)):
  *   m = beta1 m + (1 - beta1) g'      v = beta2 v + (1 - beta2) g'^2
  *   p = p - lr weight_decay p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * t counts the steps in the state, this one included.  All in binary32 and rounded
+ * t counts the steps in the state, this one included.  All in binary32 (root and
+ * reciprocal to one unit in the last place; a second moment below the smallest normal number may
+ * count as 0 there) and rounded
  * once to a parameter's type; the moments of DDP_STATE_8BIT are rounded after they
  * have served.  max_norm <= 0: no clipping; norm is |grad_scale| times
  * that of the latest ddp_opt_grad_norm, which max_norm > 0 and skip_nonfinite need since the step
@@ -600,7 +602,7 @@ int32_t ddp_opt_read_state(ddp_opt* opt, float* m_out, float* v_out);
 typedef struct ddp_embedding ddp_embedding;
 
 /* A table of `rows` (up to 2^23) rows of `width` (up to 2^20) elements; max_tokens (up to 2^22): of a
- * ddp_embedding_grad call (0: lookups only).  The workspace takes 12 bytes and a
+ * ddp_embedding_grad call (0: lookups only).  The workspace takes 15 to 29 bytes and a
  * sixteenth of a binary32 row per token, and 4 to 8 bytes per row. */
 int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, int64_t rows, int64_t width, int64_t max_tokens);
 int32_t ddp_embedding_destroy(ddp_embedding* emb);   /* waits for the handle's outstanding work */

@@ -147,7 +147,7 @@ struct SumArgs {
     int64_t tokens, rows, dout_stride, grad_stride, padding;
     int32_t width, windows, window_blocks, row_blocks, rows_per_block, add;
     int32_t units, window_units, log2_blocks, log2_run; // units: column ranges of a wave in a row
-    int32_t shift, bucket_bits;                  // of the sort
+    int32_t shift, bucket_bits, log2_window;     // of the sort
     float scale;
 };
 
@@ -394,11 +394,17 @@ __global__ __launch_bounds__(kScanThreads, 6) void scan_sum_kernel(SumArgs a) {
 // over the chunks it is where the bucket starts among all tokens, so no scan over buckets is needed.  A block then
 // gathers a bucket's tokens chunk by chunk (t ascending) and sorts them by row.
 
-// A row of up to kWindow tokens is summed by one wave (and column range).  Rows of more are split at multiples of kWindow in the
+// A row of up to 2^log2_window tokens is summed by one wave (and column range).  Rows of more are split at multiples of the window in the
 // sorted tokens, their parts go through `partial` and are joined by another launch.  split[w][0] is 1 + the place of the row
-// that reaches back before window w, split[w][1] of the one that starts in it, 0 where there is no such row of more than kWindow
-// tokens (two of them cannot start in one window).
-constexpr int kWindow = 32;
+// that reaches back before window w, split[w][1] of the one that starts in it, 0 where there is no such row of more than a window's
+// tokens (two of them cannot start in one window).  Windows are short, so that a wave's rounds of loads are few, but where all rows
+// have many tokens the parts of a row would be.
+constexpr int kLog2Window = 5, kLog2LongWindow = 7;
+// 65536 tokens into two rows of 1024, us, windows of 32 / 128: sums 52 / 48, joins 32 / 10; but 42858 into five of 26 have too few
+// windows for the chip: 28 / 40 in all.
+inline int log2_window(int64_t tokens, int64_t rows, int64_t ranges) {
+    return tokens / rows >= 256 && (tokens >> kLog2LongWindow) * ranges >= 1024 ? kLog2LongWindow : kLog2Window;
+}
 
 constexpr int kChunk = 1024;
 constexpr int kMaxBuckets = 8192;                // 32 KiB of counters
@@ -413,6 +419,7 @@ struct SortArgs {
     const void* ids;
     int64_t tokens, rows, padding;
     int32_t shift, buckets, bucket_bits, chunks; // buckets of 2^shift places
+    int32_t log2_window;
     uint16_t* starts;                            // [chunks][buckets + 1]
     uint32_t* list;                              // [tokens] by chunk, by bucket: entries, place in the bucket << 22 | token
     uint32_t* gathered;                          // [tokens] by bucket, t ascending (buckets that LDS does not hold)
@@ -441,7 +448,8 @@ __global__ __launch_bounds__(kChunk) void chunk_sort_kernel(SortArgs a) {
     const int64_t row = t < a.tokens ? row_of(static_cast<const Id*>(a.ids), t) : -1;
     const bool in = row >= 0 && row < a.rows && row != a.padding;
     for (int i = tid; i < a.buckets; i += kChunk) count[i] = 0;
-    if (tid < 2 * kChunk / kWindow) a.split[static_cast<int64_t>(blockIdx.x) * (2 * kChunk / kWindow) + tid] = 0;
+    const int splits = 2 * kChunk >> a.log2_window;
+    if (tid < splits) a.split[static_cast<int64_t>(blockIdx.x) * splits + tid] = 0;
     const uint32_t b = in ? static_cast<uint32_t>(row) & (a.buckets - 1) : 0u;
     const uint64_t same = peers(b, a.bucket_bits, __ballot(in));
     const uint32_t rank = lanes_below(same);
@@ -484,7 +492,7 @@ __device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
     return __builtin_amdgcn_readfirstlane(x);
 }
 
-// A bucket's counters in LDS: where the next token of each row goes, and where a row of more than kWindow tokens starts in `sorted`
+// A bucket's counters in LDS: where the next token of each row goes, and where a row of more than a window's tokens starts in `sorted`
 // (others: the largest number).
 struct RowCounters {
     uint32_t *next, *crowded_from;
@@ -492,8 +500,9 @@ struct RowCounters {
 // Row r of a bucket has n tokens, the first of them at `from` in `sorted`.
 __device__ __forceinline__ void row_starts(const SortArgs& a, const RowCounters& rows, int64_t place0, int r, uint32_t from, uint32_t n) {
     a.first[place0 + r] = from;
-    rows.crowded_from[r] = n > kWindow ? from : ~0u;
-    if (n > kWindow) a.split[from / kWindow * 2 + 1] = 1 + static_cast<uint32_t>(place0 + r);
+    const bool crowded = n > 1u << a.log2_window;
+    rows.crowded_from[r] = crowded ? from : ~0u;
+    if (crowded) a.split[(from >> a.log2_window) * 2 + 1] = 1 + static_cast<uint32_t>(place0 + r);
 }
 // 64 tokens of a bucket (entries; lanes that are not `in` have none) go to their places behind `base`.
 __device__ __forceinline__ void place_tokens(const SortArgs& a, uint32_t* next, const uint32_t* crowded_from, int64_t place0, uint32_t base, uint32_t e, bool in) {
@@ -506,7 +515,7 @@ __device__ __forceinline__ void place_tokens(const SortArgs& a, uint32_t* next, 
     if (in) {
         const uint32_t at = base + p + rank;
         a.sorted[at] = e & kTokenMask;
-        if (at % kWindow == 0 && crowded_from[r] < at) a.split[at / kWindow * 2] = 1 + static_cast<uint32_t>(place0) + r;
+        if ((at & ((1u << a.log2_window) - 1)) == 0 && crowded_from[r] < at) a.split[(at >> a.log2_window) * 2] = 1 + static_cast<uint32_t>(place0) + r;
         if (rank == 0) next[r] = p + __popcll(same);
     }
     wave_fence();
@@ -515,9 +524,10 @@ __device__ __forceinline__ void place_tokens(const SortArgs& a, uint32_t* next, 
 // Up to this many tokens of a bucket are sorted by the block's first wave alone, without barriers.
 constexpr int kWaveTokens = 256;
 
+// Several blocks (gridDim.y) share the copying where a bucket is one row.
 __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
     __shared__ uint32_t cache[kSortCache];
-    static_assert(kWaveTokens <= kSortCache && kWaveTokens >= kWindow, "a bucket for the block has more tokens than a window");
+    static_assert(kWaveTokens <= kSortCache && kWaveTokens >= 1 << kLog2LongWindow, "a bucket for the block has more tokens than a window");
     __shared__ uint32_t wave_part[kSortWaves], wave_before[kSortWaves];
     __shared__ uint32_t more[kSortThreads], more_from[kSortThreads], more_to[kSortThreads];
     extern __shared__ uint32_t counters[];           // [kSortWaves + 1][rows of a bucket]
@@ -549,7 +559,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
     }
     if (b == a.buckets - 1 && tid == 0) a.first[place0 + nrows] = base + total;
     if (total <= kWaveTokens) {
-        if (wave > 0) return;
+        if (wave > 0 || blockIdx.y > 0) return;
         uint32_t* tokens = cache;
         uint32_t done = 0;
         for (int c0 = 0; c0 < a.chunks && done < total; c0 += 64) {
@@ -614,6 +624,7 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
             done += wave_part[w];
         }
         const uint32_t* from = a.list + static_cast<int64_t>(c) * kChunk + s;
+        if (static_cast<unsigned>(c) / kSortWaves % gridDim.y != blockIdx.y) n = 0;       // another block's chunk
         uint32_t few[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) few[i] = i < static_cast<int>(n) ? from[i] : 0u;
@@ -641,8 +652,9 @@ __global__ __launch_bounds__(kSortThreads) void bucket_sort_kernel(SortArgs a) {
         }
     }
     if (a.shift == 0) {
+        if (blockIdx.y > 0) return;
         if (tid == 0) row_starts(a, rows, place0, 0, base, total);
-        for (uint32_t w = base / kWindow + 1 + tid; w <= (base + total - 1) / kWindow; w += kSortThreads) a.split[w * 2] = 1 + static_cast<uint32_t>(place0);
+        for (uint32_t w = (base >> a.log2_window) + 1 + tid; w <= (base + total - 1) >> a.log2_window; w += kSortThreads) a.split[w * 2] = 1 + static_cast<uint32_t>(place0);
         return;
     }
     __threadfence_block();
@@ -690,15 +702,17 @@ constexpr int kRowBlocks = 1024;                 // ... where that leaves so man
 template <int FT, int N>
 __device__ __forceinline__ void sum_window(const SumArgs& a, int64_t w, int unit) {
     const uint32_t split[2] = {a.split[w * 2], a.split[w * 2 + 1]};
-    const uint32_t w0 = static_cast<uint32_t>(w) * kWindow;
+    const uint32_t w0 = static_cast<uint32_t>(w) << a.log2_window;
     const Columns<N, 1> at(unit * (64 * N), a.width);
     for (int side = 0; side < 2; ++side) {
         if (split[side] == 0) continue;
         const uint32_t from = __builtin_amdgcn_readfirstlane(max(a.first[split[side] - 1], w0));
-        const uint32_t to = __builtin_amdgcn_readfirstlane(min(a.first[split[side]], w0 + kWindow));
-        const uint32_t mine = a.sorted[min(from + (threadIdx.x & 63), to - 1)];
+        const uint32_t to = __builtin_amdgcn_readfirstlane(min(a.first[split[side]], w0 + (1u << a.log2_window)));
         Sum<FT, N, 1> sum;
-        sum.tokens(a, at, static_cast<int>(to - from), [&](int k) { return lane_value(mine, k); });
+        for (uint32_t i = from; i < to; i += 64) {
+            const uint32_t mine = a.sorted[min(i + (threadIdx.x & 63), to - 1)];
+            sum.tokens(a, at, static_cast<int>(min(to - i, 64u)), [&](int k) { return lane_value(mine, k); });
+        }
         char* to_part = reinterpret_cast<char*>(a.partial + (w * 2 + side) * static_cast<int64_t>(a.width));
         if (at.own[0] < N) store_own<DDP_FP32, false>(to_part, at.at[0], at.own[0], sum.acc[0]);
     }
@@ -728,17 +742,21 @@ __global__ __launch_bounds__(kThreads) void row_sum_kernel(SumArgs a) {
             zero_vector<GT, N>(a, min(i0 + threadIdx.x, vectors - 1), [&](int j) { return __shfl(count, j) == 0u ? row_of_block(j) : -1; });
     }
     int turn = 0;
-    for (uint64_t some = __ballot(count - 1u < static_cast<uint32_t>(kWindow)); some != 0; some &= some - 1) {
+    for (uint64_t some = __ballot(count - 1u < 1u << a.log2_window); some != 0; some &= some - 1) {
         const int j = __ffsll(static_cast<unsigned long long>(some)) - 1, n = static_cast<int>(lane_value(count, j));
         bool fetched = n == 1;
         uint32_t own = lane_value(token, j);
         for (int unit = 0; unit < a.units; ++unit, ++turn) {
             if (turn % kWaves != wave) continue;
             if (!fetched) own = a.sorted[lane_value(from, j) + min(lane, n - 1)];
-            fetched = true;
+            fetched = n <= 64;
             const Columns<N, 1> at(unit * (64 * N), a.width);
             Sum<FT, N, 1> sum;
-            sum.tokens(a, at, n, [&](int k) { return lane_value(own, k); });
+            sum.tokens(a, at, min(n, 64), [&](int k) { return lane_value(own, k); });
+            for (int i = 64; i < n; i += 64) {
+                const uint32_t more = a.sorted[lane_value(from, j) + min(i + lane, n - 1)];
+                sum.tokens(a, at, min(n - i, 64), [&](int k) { return lane_value(more, k); });
+            }
             sum.template put<GT>(a, at, row_of_block(j));
         }
     }
@@ -753,7 +771,7 @@ __global__ __launch_bounds__(kJoinThreads) void row_join_kernel(SumArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t window = static_cast<int64_t>(blockIdx.x) * kJoinWindows + lane;
     const uint32_t found = lane < kJoinWindows && window < a.windows ? a.split[window * 2 + 1] : 0u;
-    const int parts_here = found != 0 ? static_cast<int>((a.first[found] - 1) / kWindow - static_cast<uint32_t>(window)) + 1 : 0;
+    const int parts_here = found != 0 ? static_cast<int>(((a.first[found] - 1) >> a.log2_window) - static_cast<uint32_t>(window)) + 1 : 0;
     SumArgs p = a;                                   // the parts as rows
     p.dout = reinterpret_cast<const char*>(a.partial);
     p.dout_stride = a.width;
@@ -881,7 +899,7 @@ hipError_t launch_rows(ddp_embedding* e, SumArgs a) {
     a.units = ranges_of(64 * N);
     a.window_units = ranges_of(64 * WN);
     a.window_blocks = static_cast<int32_t>((static_cast<int64_t>(a.windows) * a.window_units + kWaves - 1) / kWaves);
-    a.rows_per_block = static_cast<int32_t>(std::max<int64_t>(8, std::min<int64_t>({64, kRowColumns / a.width, a.rows / kRowBlocks})));
+    a.rows_per_block = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({64, std::max(8, kRowColumns / a.width), a.rows / kRowBlocks})));
     a.row_blocks = static_cast<int32_t>((a.rows + a.rows_per_block - 1) / a.rows_per_block);
     const int64_t blocks = static_cast<int64_t>(a.window_blocks) + a.row_blocks;
     hipLaunchKernelGGL((row_sum_kernel<FT, GT, N, WN>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, e->stream, a);
@@ -921,7 +939,7 @@ hipError_t launch_sort(ddp_embedding* e, const SortArgs& a) {
     hipLaunchKernelGGL((chunk_sort_kernel<Id>), dim3(a.chunks), dim3(kChunk), static_cast<size_t>(a.buckets) * 4, e->stream, a);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(bucket_sort_kernel, dim3(a.buckets), dim3(kSortThreads), (static_cast<size_t>(kSortWaves + 1) << a.shift) * 4, e->stream, a);
+    hipLaunchKernelGGL(bucket_sort_kernel, dim3(a.buckets, a.shift == 0 && a.buckets <= 64 ? std::min(8, a.chunks) : 1), dim3(kSortThreads), (static_cast<size_t>(kSortWaves + 1) << a.shift) * 4, e->stream, a);
     return hipGetLastError();
 }
 
@@ -959,9 +977,10 @@ int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, 
         const int64_t chunks = (max_tokens + kChunk - 1) / kChunk;
         const int64_t places = int64_t(1) << (e->bucket_bits + e->shift), buckets = int64_t(1) << e->bucket_bits;
         const int64_t tokens = up(max_tokens * 4, 256), first = up((places + 1) * 4, 256), starts = up(chunks * (buckets + 1) * 2, 256);
-        const int64_t split = up(chunks * (2 * kChunk / kWindow) * 4, 256), partial = up((max_tokens + kWindow - 1) / kWindow * 2 * width * 4, 256);
+        const int64_t split = up(chunks * (2 * kChunk >> kLog2Window) * 4, 256);
+        const int64_t partial = (((max_tokens - 1) >> kLog2Window) + 1) * 2 * width * 4;
         hipError_t err = hipSetDevice(device);
-        if (err == hipSuccess) err = hipMalloc(reinterpret_cast<void**>(&e->mem), 3 * tokens + first + split + partial + starts);
+        if (err == hipSuccess) err = hipMalloc(reinterpret_cast<void**>(&e->mem), 3 * tokens + first + split + up(partial, 256) + starts);
         if (err != hipSuccess) {
             delete e;
             return fail(nullptr, DDP_ERR_HIP, hipGetErrorString(err));
@@ -973,7 +992,7 @@ int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, 
         e->first = reinterpret_cast<uint32_t*>(at += tokens);
         e->split = reinterpret_cast<uint32_t*>(at += first);
         e->partial = reinterpret_cast<float*>(at += split);
-        e->starts = reinterpret_cast<uint16_t*>(at += partial);
+        e->starts = reinterpret_cast<uint16_t*>(at += up(partial, 256));
     }
     *out = e;
     return DDP_OK;
@@ -1039,7 +1058,8 @@ int32_t ddp_embedding_grad(ddp_embedding* e, int64_t tokens, const void* ids, in
     a.dout_stride = dout_stride;
     a.grad_stride = grad_stride;
     a.padding = padding_row;
-    a.windows = static_cast<int32_t>((tokens + kWindow - 1) / kWindow);
+    a.log2_window = log2_window(tokens, e->rows, (e->width * elem_bytes(dout_dtype) + 1023) / 1024);
+    a.windows = static_cast<int32_t>((tokens + (1 << a.log2_window) - 1) >> a.log2_window);
     a.add = accumulate != 0;
     a.scale = scale;
     a.shift = e->shift;
@@ -1068,6 +1088,7 @@ int32_t ddp_embedding_grad(ddp_embedding* e, int64_t tokens, const void* ids, in
         s.sorted = e->sorted;
         s.first = e->first;
         s.split = e->split;
+        s.log2_window = a.log2_window;
         EMB_HIP(e, id_bits == 32 ? launch_sort<int32_t>(e, s) : launch_sort<int64_t>(e, s));
     }
     EMB_HIP(e, id_bits == 32 ? launch_sum<int32_t>(dout_dtype, grad_dtype, e, a, scan) : launch_sum<int64_t>(dout_dtype, grad_dtype, e, a, scan));

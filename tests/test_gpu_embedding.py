@@ -247,6 +247,19 @@ def test_grad_long_calls_of_few_rows(tokens):
     check_grad(3000, 9, np.where(rng.random(tokens) < 0.7, 1024, rng.integers(0, 3000, tokens)), FP16, FP32)
 
 
+@pytest.mark.parametrize("rows", [2, 33, 120])
+def test_grad_long_windows(rows):
+    """Tables of few and wide rows have longer parts: rows of more, fewer and just as many tokens."""
+    rng = np.random.default_rng(rows)
+    ids = zipf(rng, rows, 40000)
+    if rows > 100:
+        for r, n in ((100, 127), (101, 128), (102, 129), (103, 64), (104, 65), (105, 1)):
+            ids[ids == r] = 0
+            ids[rng.choice(np.flatnonzero(ids == 0), n, replace=False)] = r
+    check_grad(rows, 1030, ids, FP32, FP32)
+    check_grad(rows, 2060, ids, BF16, BF16, add=True)
+
+
 def test_grad_calls_do_not_see_each_other():
     """One handle, calls of different lengths and spreads in turn: nothing of a longer call is left."""
     rng = np.random.default_rng(5)
