@@ -389,7 +389,13 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(NormArgs a) {
 
 __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a, int blocks) {
     double sum = 0.0;
-    for (int i = threadIdx.x; i < blocks; i += 1024) sum += a.partial[i];
+    for (int i = threadIdx.x; i < blocks; i += 8 * 1024) {
+        double x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = i + k * 1024 < blocks ? a.partial[i + k * 1024] : 0.0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += x[k];
+    }
     sum = block_sum<1024>(sum);
     if (threadIdx.x == 0) put_norm(a, sum);
 }
