@@ -38,8 +38,10 @@ template <bool Q8> constexpr int kStepTile = kThreads * 4 * kRounds<Q8>;
 constexpr int kNormTile = 4096;                  // elements of a tile of the norm
 constexpr int kHeaderBytes = 256;                // of a state: the number of steps, then nothing
 constexpr int kNormTiles = 4;                    // tiles that a block of a long norm takes
-constexpr int kNormLong = 4096;                  // tiles from which it is one; us, one tile a block / four: 7 M elements 9.4 / 14.0,
-                                                 // 25.6 M 23.7 / 19.4, BERT-large in bfloat16 152 / 106 (eight: 120)
+constexpr int64_t kNormLong = 90000000;          // bytes of gradients from which it is one; us, one tile a block / four (the loads of four pass
+                                                 // the caches): binary32 68 MB 16.3 / 17.1, 80 MB 17.1 / 17.7, 100 MB 22.8 / 19.6,
+                                                 // bfloat16 50 MB 14.1 / 15.1, 80 MB 18.9 / 20.7, 160 MB 37.9 / 30.7, 670 MB 136 / 103
+                                                 // (eight: 105)
 constexpr int kNormAlone = 768;                  // tiles up to which the norm is one launch; us, one / two: 500 thousand
                                                  // elements 4.9 / 6.5, 2 M 5.9 / 6.6, 3 M 6.7 / 6.5, 10 M 13.7 / 11.9
 constexpr int kMaskWords = 768;                  // words of the used mask that travel in one launch's arguments
@@ -139,7 +141,7 @@ __device__ __forceinline__ uint32_t byte_of(float x, int i, uint32_t into) { ret
 
 // One pass over four or five streams that are read and as many that are written.  Loads and stores carry the non-temporal hint: nothing is
 // used again before everything else has been (60 M elements, binary32: 322 us without, 288 with it, 325 with it on the stores
-// alone).  BERT-large, bfloat16 gradients and copies: 28 bytes an element in 1635 us, 5.7 TB/s; 8-bit states, 16 bytes, 905 us, 5.9 TB/s
+// alone).  BERT-large, bfloat16 gradients and copies: 28 bytes an element in 1620 us, 5.8 TB/s; 8-bit states, 16 bytes, 905 us, 5.9 TB/s
 // (a plain copy reaches 4.8 to 5.8).  8 bits: 75 vector instructions an element, which memory just covers; with IEEE roots and divisions
 // it was 1270 us.
 template <int PT, int GT, int CT, bool Q8, bool FULL>
@@ -347,7 +349,7 @@ __device__ __forceinline__ void put_norm(const NormArgs& a, double squares) {
     if (a.out != nullptr) *a.out = static_cast<float>(norm * a.scale);
 }
 
-// Bound by memory: 670 MB of BERT-large's bfloat16 gradients in 106 us, 6.3 TB/s (5.6 without the non-temporal hint, which
+// Bound by memory: 670 MB of BERT-large's bfloat16 gradients in 103 us, 6.5 TB/s (5.6 without the non-temporal hint, which
 // costs in lists that fit the 256 MB cache: 12 M elements 12.4 us without, 15.5 with it).
 // Squares are summed in 64 bits: no gradient that a binary32 holds overflows or is lost.  The order of the sum (tiles by
 // block, blocks by index) does not depend on which block is last.
@@ -401,6 +403,8 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a, int blocks)
 }
 
 // ---- states as values ----
+
+// A stream: 2 bytes an element are read, 8 written, past the caches.  BERT-large, both moments: 3.4 GB in 560 us, 6.1 TB/s.
 
 __global__ __launch_bounds__(kThreads) void read_state_kernel(const char* m, const char* v, const float* m_top, const float* v_top,
                                                               float* m_out, float* v_out, int64_t elems) {
@@ -469,6 +473,7 @@ struct ddp_opt {
     StateLayout layout;
     std::vector<Launch> launches;
     int64_t norm_tiles = 0;
+    int norm_each = 1;                           // tiles that a block takes
     // device memory owned by the library: segments, tile maps, used mask, counters, partial sums, NormState
     char* mem = nullptr;
     OptSeg* d_seg = nullptr;
@@ -527,10 +532,11 @@ int32_t build(ddp_opt* o) {
     std::vector<OptSeg> seg;
     std::vector<int32_t> step_seg, norm_seg;
     o->launches.clear();
-    int64_t tiles = 0, norm_tiles = 0;
+    int64_t tiles = 0, norm_tiles = 0, norm_bytes = 0;
     for (int i : order) {
         tiles += tiles_of(o->numel[i], tile_elems);
         norm_tiles += tiles_of(o->numel[i], kNormTile);
+        norm_bytes += o->numel[i] * elem_bytes(o->grad_type[i]);
     }
     if (tiles > INT32_MAX) return fail(o, DDP_ERR_UNSUPPORTED, "model too large for one launch grid");
     step_seg.reserve(tiles);
@@ -574,7 +580,7 @@ int32_t build(ddp_opt* o) {
     };
     const int64_t at_seg = take(static_cast<int64_t>(seg.size() * sizeof(OptSeg))), at_step = take(tiles * 4), at_norm = take(norm_tiles * 4);
     const int64_t at_used = take((n + 31) / 32 * 4), at_counters = take(2 * kCounterSet * 4), at_state = take(sizeof(NormState));
-    const int64_t at_partial = take(std::max(std::min<int64_t>(norm_tiles, kNormLong), (norm_tiles + kNormTiles - 1) / kNormTiles) * 8);
+    const int64_t at_partial = take(norm_tiles * 8);
     OPT_HIP(o, hipMalloc(reinterpret_cast<void**>(&o->mem), bytes));
     o->d_seg = reinterpret_cast<OptSeg*>(o->mem + at_seg);
     o->d_step_seg = reinterpret_cast<int32_t*>(o->mem + at_step);
@@ -593,6 +599,7 @@ int32_t build(ddp_opt* o) {
     const NormState zero{};
     OPT_HIP(o, hipMemcpy(o->d_norm, &zero, sizeof zero, hipMemcpyHostToDevice));
     o->norm_tiles = norm_tiles;
+    o->norm_each = norm_bytes < kNormLong ? 1 : kNormTiles;
     o->built = true;
     o->fresh_norm = false;
     return DDP_OK;
@@ -823,8 +830,8 @@ int32_t ddp_opt_grad_norm(ddp_opt* o, double grad_scale, const uint8_t* used, fl
         if (o->norm_tiles <= kNormAlone) {
             hipLaunchKernelGGL((grad_norm_kernel<1, true>), dim3(std::max(1, static_cast<int>(o->norm_tiles))), dim3(kThreads), 0, o->stream, a);
         } else {
-            const int each = o->norm_tiles < kNormLong ? 1 : kNormTiles, blocks = static_cast<int>((o->norm_tiles + each - 1) / each);
-            if (each == 1) hipLaunchKernelGGL((grad_norm_kernel<1, false>), dim3(blocks), dim3(kThreads), 0, o->stream, a);
+            const int blocks = static_cast<int>((o->norm_tiles + o->norm_each - 1) / o->norm_each);
+            if (o->norm_each == 1) hipLaunchKernelGGL((grad_norm_kernel<1, false>), dim3(blocks), dim3(kThreads), 0, o->stream, a);
             else hipLaunchKernelGGL((grad_norm_kernel<kNormTiles, false>), dim3(blocks), dim3(kThreads), 0, o->stream, a);
             OPT_HIP(o, hipGetLastError());
             hipLaunchKernelGGL(norm_join_kernel, dim3(1), dim3(1024), 0, o->stream, a, blocks);

@@ -284,6 +284,28 @@ def test_norm_of_large_and_small_gradients():
         prog.close()
 
 
+@pytest.mark.parametrize("grad,numel", [(FP32, [1, 3000001, 0, 70000, 4096, 2000000]), (BF16, [3000001, 7, 2000000, 1, 333]),
+                                        (FP32, [5, 22500001, 0, 4097, 333]), (FP16, [45000003, 1, 4095, 70000, 0])])
+def test_norm_of_longer_lists(grad, numel):
+    """Lists of more blocks than one launch joins, with one tile a block and with several."""
+    torch, d = lib()
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    g = Flat(numel, grad)
+    for i in range(len(numel)):
+        g.view(i).normal_(0.0, 1.0, generator=gen)
+    opt = d.ddp_opt_create(0)
+    d.ddp_opt_register(opt, numel, [grad] * len(numel), None, [grad] * len(numel), g.ptrs())
+    out = torch.zeros(1, dtype=torch.float32, device="cuda")
+    squares = [float((x * x).sum()) for x in g.host()]
+    for used in (None, [int(i != 0) for i in range(len(numel))], [int(i == 0) for i in range(len(numel))], [0] * len(numel)):
+        torch.cuda.synchronize()
+        d.ddp_opt_grad_norm(opt, 1.0, out.data_ptr(), used)
+        torch.cuda.synchronize()
+        want = np.sqrt(sum(x for i, x in enumerate(squares) if used is None or used[i]))
+        assert abs(out.item() - want) <= 2 * U * want, used
+    d.ddp_opt_destroy(opt)
+
+
 def test_norm_without_parameters():
     """A program with a step of its own registers gradients alone."""
     torch, d = lib()
