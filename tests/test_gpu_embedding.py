@@ -223,6 +223,26 @@ def test_grad_strides_and_alignments(gaps, shifts, dt):
     check_grad(61, 131, zipf(rng, 61, 400), dt, dt, gaps=gaps, shifts=shifts, add=True)
 
 
+@pytest.mark.parametrize("tokens", [9, 1500])
+def test_grad_past_32_bits(tokens):
+    """Rows of dout and of the gradient whose offsets need more than 32 bits, by either way through the tokens."""
+    torch, d = lib()
+    rows, width, dout_stride, grad_stride = 5, 1040, (1 << 32) // tokens, 1 << 30
+    ids = np.arange(tokens) % (rows - 1) + 1
+    dout = torch.empty(tokens * dout_stride + width, dtype=torch.bfloat16, device="cuda")[:tokens * dout_stride].view(tokens, dout_stride)
+    grad = torch.empty(rows * grad_stride, dtype=torch.bfloat16, device="cuda").view(rows, grad_stride)
+    dout[:, :width] = torch.arange(tokens, device="cuda").remainder(7).bfloat16()[:, None]
+    grad[:, :width + 8] = 7.0
+    on, emb = ids_on(ids, 64), d.ddp_embedding_create(0, 0, rows, width, tokens)
+    torch.cuda.synchronize()
+    d.ddp_embedding_grad(emb, tokens, on.data_ptr(), 64, dout.data_ptr(), BF16, dout_stride, 0.5, -1, False, grad.data_ptr(), BF16, grad_stride)
+    torch.cuda.synchronize()
+    got = grad[:, :width + 8].double().cpu().numpy()
+    want = 0.5 * np.bincount(ids, weights=np.arange(tokens) % 7, minlength=rows)[:, None]
+    assert (np.abs(got[:, :width] - want) <= UNIT[BF16] * want).all() and (got[:, width:] == 7.0).all()
+    d.ddp_embedding_destroy(emb)
+
+
 def test_grad_values_that_are_not_finite_stay_in_their_row():
     torch, _ = lib()
     dout = torch.ones((40, 16), device="cuda")

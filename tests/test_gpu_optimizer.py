@@ -306,6 +306,32 @@ def test_norm_of_longer_lists(grad, numel):
     d.ddp_opt_destroy(opt)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_tensor_past_32_bits(bits):
+    """Byte offsets in parameters, gradients and states that need more than 32 bits; where the gradient is 0 nothing
+    moves, elsewhere a first step without decay is lr."""
+    torch, d = lib()
+    n = (1 << 31) + 300
+    at = torch.tensor([0, (1 << 30) + 5, (1 << 31) - 1, 1 << 31, n - 1], device="cuda")
+    p, g = torch.ones(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[at] = 2.0
+    kind = d.DDP_STATE_FP32 if bits == 32 else d.DDP_STATE_8BIT
+    _, where = d.ddp_opt_state_layout([n], kind)
+    state, out = torch.zeros(where["bytes"], dtype=torch.uint8, device="cuda"), torch.zeros(1, device="cuda")
+    opt = d.ddp_opt_create(0)
+    d.ddp_opt_register(opt, [n], [BF16], [p.data_ptr()], [BF16], [g.data_ptr()])
+    d.ddp_opt_set_state(opt, kind, state.data_ptr(), where["bytes"])
+    torch.cuda.synchronize()
+    d.ddp_opt_grad_norm(opt, 1.0, out.data_ptr())
+    d.ddp_opt_adamw_step(opt, 0.25)
+    torch.cuda.synchronize()
+    assert abs(out.item() - np.sqrt(20.0)) <= 2 * U * np.sqrt(20.0)
+    assert (p[at] == 0.75).all()
+    p[at] = 1.0
+    assert (p == 1.0).all()
+    d.ddp_opt_destroy(opt)
+
+
 def test_norm_without_parameters():
     """A program with a step of its own registers gradients alone."""
     torch, d = lib()
