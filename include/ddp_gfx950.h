@@ -582,7 +582,9 @@ int32_t ddp_opt_grad_norm(ddp_opt* opt, double grad_scale, const uint8_t* used, 
  * once to a parameter's type; the moments of DDP_STATE_8BIT are rounded after they
  * have served.  max_norm <= 0: no clipping; norm is |grad_scale| times
  * that of the latest ddp_opt_grad_norm, which max_norm > 0 and skip_nonfinite need since the step
- * before (DDP_ERR_STATE otherwise).  skip_nonfinite != 0: where the norm is not finite nothing changes and
+ * before (DDP_ERR_STATE otherwise).  Clipping by an infinite norm is a factor of 0 (the gradients that are not
+ * finite become NaN), by one that is NaN a factor of NaN: every parameter that takes part becomes NaN.
+ * skip_nonfinite != 0: where the norm is not finite nothing changes and
  * no step is counted.  Parameters with used[i] == 0 keep their values and moments.
  * May be captured into a HIP graph, with ddp_opt_grad_norm in front of it (the
  * hyperparameters and flags are those of the capture, the count of steps goes on). */

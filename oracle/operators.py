@@ -50,7 +50,7 @@ def adamw(p, g, m, v, t, lr, beta1, beta2, eps, decay, grad_scale=1.0, max_norm=
     p, g, m, v = (x.astype(np.float64) for x in (p, g, m, v))
     g = g * grad_scale
     if max_norm > 0.0:
-        g = g * min(1.0, max_norm / (abs(grad_scale) * norm + 1e-6))
+        g = g * np.minimum(1.0, max_norm / (abs(grad_scale) * norm + 1e-6))      # NaN where the norm is
     m = beta1 * m + (1.0 - beta1) * g
     v = beta2 * v + (1.0 - beta2) * g * g
     rate = m / (1.0 - beta1 ** t) / (np.sqrt(v / (1.0 - beta2 ** t)) + eps)

@@ -97,7 +97,7 @@ __device__ __forceinline__ Factors factors(const StepArgs& a, const OptSeg& s) {
     double g = a.grad_scale;
     if (a.max_norm > 0.0) {
         const double clip = a.max_norm / (table_load(&a.norm->norm) * fabs(a.grad_scale) + 1e-6);
-        if (clip < 1.0) g *= clip;
+        if (!(clip >= 1.0)) g *= clip;           // (a norm that is NaN shows in every parameter)
     }
     Factors f;
     f.grad = static_cast<float>(g);

@@ -549,3 +549,51 @@ def test_moments_in_8_bits_follow_those_in_32():
     assert np.linalg.norm(off) <= 0.05 * np.linalg.norm(way)
     for prog in (a, b):
         prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad_scale", [1.0, -0.5])
+def test_clipping_by_a_norm_that_is_nan(grad_scale, bits):
+    """The factor is NaN: every parameter shows it, as with the formula, and none takes a step that is not clipped."""
+    _, d = lib()
+    prog = Program(bits=bits, seed=21, copy=BF16)
+    check_step(prog, lambda: step(prog))
+    prog.g.view(7)[4000] = float("nan")
+    p0 = prog.p.host()
+    norm = ops.grad_norm(prog.g.host())
+    assert np.isnan(norm)
+    d.ddp_opt_grad_norm(prog.opt, grad_scale)
+    step(prog, grad_scale=grad_scale, max_norm=0.05)
+    assert prog.steps() == 2
+    for i, (n, got) in enumerate(zip(prog.numel, prog.p.host())):
+        want, _, _ = ops.adamw(p0[i], prog.g.host()[i], 0 * p0[i], 0 * p0[i], 2, 1e-2, 0.9, 0.999, 1e-8, 0.1, grad_scale, 0.05, norm)
+        assert np.isnan(want).all() and np.isnan(got).all(), f"tensor {i} of {n}"
+        assert np.isnan(prog.c.host()[i]).all()
+    assert prog.guards_hold()
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_clipping_by_a_norm_that_is_infinite(bits):
+    """The factor is 0: what is finite takes a step with a gradient of 0, what is not shows itself (8 bits: in its block of 256)."""
+    torch, d = lib()
+    progs = [Program(bits=bits, seed=22) for _ in range(2)]
+    for prog in progs:
+        check_step(prog, lambda: step(prog))
+    progs[0].g.view(7)[4000] = float("inf")
+    for i in range(progs[1].n):
+        progs[1].g.view(i).zero_()
+    d.ddp_opt_grad_norm(progs[0].opt)
+    step(progs[0], max_norm=0.05)
+    step(progs[1])
+    torch.cuda.synchronize()
+    for i, (got, want) in enumerate(zip(progs[0].p.host(), progs[1].p.host())):
+        far = np.ones(len(got), dtype=bool)
+        if i == 7:
+            assert not np.isfinite(got[4000])
+            far[4000 if bits == 32 else slice(3840, 4096)] = False
+            if bits == 32:
+                far[4000] = False
+        assert (got == want)[far].all(), i
+    for prog in progs:
+        prog.close()

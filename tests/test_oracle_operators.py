@@ -76,3 +76,13 @@ def test_codes():
     assert np.abs(ops.held_first(codes, tops) / x - 1).max() < 0.0115
     codes, tops, _ = ops.nearest_second(x)
     assert np.abs(ops.held_second(codes, tops) / x - 1).max() < 0.0095
+
+
+def test_clipping_by_norms_that_are_not_finite():
+    """min(1, NaN) is NaN; an infinite norm leaves nothing of a finite gradient."""
+    p, g, m, v = np.ones(3), np.array([0.5, -1.0, 2.0]), np.full(3, 0.1), np.full(3, 0.2)
+    for norm, factor in ((np.inf, 0.0), (np.nan, np.nan), (10.0, 1.0 / (10.0 + 1e-6)), (0.5, 1.0)):
+        got = ops.adamw(p, g, m, v, 3, 1e-2, 0.9, 0.99, 1e-8, 0.1, 1.0, 1.0, norm)
+        want = ops.adamw(p, g * factor, m, v, 3, 1e-2, 0.9, 0.99, 1e-8, 0.1)
+        for x, y in zip(got, want):
+            np.testing.assert_allclose(x, y, rtol=1e-15, equal_nan=True)
