@@ -549,7 +549,8 @@ const char* ddp_opt_last_error(const ddp_opt* opt);
 
 /* n tensors: element counts (0 allowed), types and device addresses of the
  * parameters (param_ptrs NULL: for ddp_opt_grad_norm alone) and of their
- * gradients; contiguous, aligned to their element size, all regions apart.
+ * gradients; contiguous, aligned to their element size, all regions apart; in all some
+ * 6 * 10^10 elements (DDP_ERR_UNSUPPORTED above that where the tables are laid out).
  * Types may differ from tensor to tensor and between a parameter and its
  * gradient (binary32 averages of ddp_set_outputs for bfloat16 parameters, or
  * bfloat16 gradients for binary32 parameters). */

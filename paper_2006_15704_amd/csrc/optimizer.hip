@@ -44,6 +44,9 @@ constexpr int64_t kNormLong = 90000000;          // bytes of gradients from whic
                                                  // (eight: 105)
 constexpr int kNormAlone = 768;                  // tiles up to which the norm is one launch; us, one / two: 500 thousand
                                                  // elements 4.9 / 6.5, 2 M 5.9 / 6.6, 3 M 6.7 / 6.5, 10 M 13.7 / 11.9
+constexpr int64_t kGridBlocks = (int64_t(1) << 24) - 1; // that a grid can have: it ends at 2^32 threads
+constexpr int64_t kLaunchBlocks = int64_t(1) << 20;     // of a launch of the step: a run of equal types with more tiles takes several
+                                                 // (5 ms each and more, of which the drain in between is a thousandth)
 constexpr int kMaskWords = 768;                  // words of the used mask that travel in one launch's arguments
 
 struct OptSeg {                                  // 64 bytes
@@ -546,7 +549,9 @@ int32_t build(ddp_opt* o) {
         norm_tiles += tiles_of(o->numel[i], kNormTile);
         norm_bytes += o->numel[i] * elem_bytes(o->grad_type[i]);
     }
-    if (tiles > INT32_MAX) return fail(o, DDP_ERR_UNSUPPORTED, "model too large for one launch grid");
+    const int64_t read_blocks = (at + kThreads * 4 * kReadRounds - 1) / (kThreads * 4 * kReadRounds);
+    if (tiles > INT32_MAX || norm_tiles > kGridBlocks * kNormTiles || read_blocks > kGridBlocks)
+        return fail(o, DDP_ERR_UNSUPPORTED, "more elements than the launches of norm and read-out reach");
     step_seg.reserve(tiles);
     norm_seg.reserve(norm_tiles);
     for (int i : order) {
@@ -567,8 +572,14 @@ int32_t build(ddp_opt* o) {
             o->launches.back().grad_type != o->grad_type[i] || o->launches.back().copy_type != copy_of(i))
             o->launches.push_back(Launch{o->param_type[i], o->grad_type[i], copy_of(i), s.step_tile0, 0});
         const int64_t mine = tiles_of(s.numel, tile_elems);
-        o->launches.back().tiles += mine;
         step_seg.insert(step_seg.end(), static_cast<size_t>(mine), static_cast<int32_t>(seg.size()));
+        for (int64_t left = mine; left > 0;) {
+            Launch& l = o->launches.back();
+            const int64_t here = std::min(left, kLaunchBlocks - l.tiles);
+            l.tiles += here;
+            left -= here;
+            if (left > 0) o->launches.push_back(Launch{l.param_type, l.grad_type, l.copy_type, l.tile_base + l.tiles, 0});
+        }
         norm_seg.insert(norm_seg.end(), static_cast<size_t>(tiles_of(s.numel, kNormTile)), static_cast<int32_t>(seg.size()));
         seg.push_back(s);
     }

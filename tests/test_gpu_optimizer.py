@@ -597,3 +597,55 @@ def test_clipping_by_a_norm_that_is_infinite(bits):
         assert (got == want)[far].all(), i
     for prog in progs:
         prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_list_of_more_blocks_than_one_launch_can_have(bits):
+    """A grid ends at 2^32 threads: 2^24 blocks of 256, 17 thousand million elements with 32-bit states, twice that with 8.  A run of
+    equal types above it takes several launches (a short run in front has a launch of its own), and the step counts once."""
+    torch, d = lib()
+    torch.cuda.empty_cache()
+    n = (1 << (34 if bits == 32 else 35)) + 5000
+    kind = d.DDP_STATE_FP32 if bits == 32 else d.DDP_STATE_8BIT
+    numel = [300, n]
+    offset, where = d.ddp_opt_state_layout(numel, kind)
+    if torch.cuda.mem_get_info()[0] < 4 * n + where["bytes"] + (8 << 30):
+        pytest.skip("needs a card with 220 GB free")
+    from conftest import progress
+    progress(f"step of {n} elements, {bits}-bit states")
+    small, small_g = torch.ones(300, device="cuda"), torch.full((300,), 2.0, device="cuda")
+    at = torch.tensor([0, (1 << 30) + 5, n // 2, n - 5001, n - 5000, n - 1], device="cuda")
+    p, g = torch.empty(n, dtype=torch.bfloat16, device="cuda").fill_(1.0), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    state = torch.zeros(where["bytes"], dtype=torch.uint8, device="cuda")
+    g[at] = 2.0
+    opt = d.ddp_opt_create(0)
+    d.ddp_opt_register(opt, numel, [FP32, BF16], [small.data_ptr(), p.data_ptr()], [FP32, BF16], [small_g.data_ptr(), g.data_ptr()])
+    d.ddp_opt_set_state(opt, kind, state.data_ptr(), where["bytes"])
+    torch.cuda.synchronize()
+    d.ddp_opt_grad_norm(opt)
+    d.ddp_opt_adamw_step(opt, 0.25, max_norm=1e6)
+    torch.cuda.synchronize()
+    progress("stepped")
+    assert int(state[:8].view(torch.int64).item()) == 1
+    assert ((small - 0.75).abs() <= 1e-6).all() and (p[at] == 0.75).all()
+    p[at] = 1.0
+    for part in p.split(1 << 31):
+        assert bool((part == 1.0).all())
+    d.ddp_opt_destroy(opt)
+    del p, g, state, part
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("numel", [[1 << 40], [1 << 36, 1 << 36, 5], [1 << 46]])
+def test_lists_that_no_grid_reaches(numel):
+    """Refused where the tables would be laid out, before a step has moved anything."""
+    _, d = lib()
+    n = len(numel)
+    opt = d.ddp_opt_create(0)
+    d.ddp_opt_register(opt, numel, [BF16] * n, [256] * n, [BF16] * n, [256] * n)
+    _, where = d.ddp_opt_state_layout(numel, d.DDP_STATE_8BIT)
+    for call in (lambda: d.ddp_opt_set_state(opt, d.DDP_STATE_8BIT, 256, where["bytes"]), lambda: d.ddp_opt_grad_norm(opt)):
+        with pytest.raises(d.DdpError) as e:
+            call()
+        assert e.value.code == d.DDP_ERR_UNSUPPORTED
+    d.ddp_opt_destroy(opt)
