@@ -223,6 +223,7 @@ __device__ __forceinline__ void step_tile(const StepArgs& a, const OptSeg& s, in
             const int64_t e = element_of(u), at = s.state + e;
             const float m_inv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inverse), 2 * u));
             const float v_inv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inverse), 2 * u + 1));
+            const float least = v_inv > 0.0f ? 1.0f : 0.0f;
             uint32_t mc = 0, vc = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -236,7 +237,7 @@ __device__ __forceinline__ void step_tile(const StepArgs& a, const OptSeg& s, in
                 k = floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(q)) + 0.4999f);
                 h = (k + 0.5f) * (k + 0.5f);
                 k = h * h <= q ? k + 1.0f : k;
-                vc = byte_of(fmaxf(k, __builtin_amdgcn_fmed3f(q * 1e30f, 0.0f, 1.0f)), i, vc);
+                vc = byte_of(fmaxf(k, v[u][i] > 0.0f ? least : 0.0f), i, vc);      // (from v: q may be below the smallest number)
             }
             if (FULL || e < padded) {
                 __builtin_nontemporal_store(mc ^ 0x80808080u, (DDP_GLOBAL_MEM uint32_t*)(a.m + at));

@@ -649,3 +649,19 @@ def test_lists_that_no_grid_reaches(numel):
             call()
         assert e.value.code == d.DDP_ERR_UNSUPPORTED
     d.ddp_opt_destroy(opt)
+
+
+@pytest.mark.parametrize("large,small", [(1e3, 1e-15), (1e5, 1e-16), (1e5, 1e-18), (1e15, 1e-10), (1e15, 3e-20)])
+def test_second_moments_far_below_their_largest(large, small):
+    """Whatever the ratio (down to subnormal second moments), what is not 0 keeps a code that is not 0."""
+    prog = Program(numel=[512], bits=8)
+    prog.g.view(0).fill_(small)
+    prog.g.view(0)[0] = large
+    prog.g.view(0)[5], prog.g.view(0)[300] = 0.0, large
+    prog.g.view(0)[301:] = 0.0
+    held = prog.g.host()[0]
+    check_step(prog, lambda: step(prog))
+    _, vc, _, _ = prog.codes()
+    assert 1e-3 * small * small > 2.0 ** -148                # a binary32
+    assert (vc == np.where(held == 0, 0, np.where(held > 1.0, 255, 1))).all()
+    prog.close()
