@@ -14,6 +14,11 @@
 namespace ddp {
 
 inline int elem_bytes(int dtype) { return dtype == DDP_FP32 ? 4 : 2; }
+// A failure that a call reports by its status does not stay the thread's last error, which the next launch (of whoever) would report again.
+inline hipError_t taken(hipError_t err) {
+    if (err != hipSuccess) (void)hipGetLastError();
+    return err;
+}
 inline bool known_dtype(int dtype) { return dtype == DDP_FP32 || dtype == DDP_FP16 || dtype == DDP_BF16; }
 
 #if defined(__HIPCC__)

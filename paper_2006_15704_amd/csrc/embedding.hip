@@ -852,7 +852,7 @@ int32_t fail(ddp_embedding* e, int32_t code, const char* msg) {
 
 #define EMB_HIP(e, expr)                                                            \
     do {                                                                            \
-        const hipError_t e_ = (expr);                                               \
+        const hipError_t e_ = taken(expr);                                          \
         if (e_ != hipSuccess) return fail((e), DDP_ERR_HIP, hipGetErrorString(e_)); \
     } while (0)
 
@@ -969,7 +969,7 @@ int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, 
         return fail(nullptr, DDP_ERR_UNSUPPORTED, "ddp_embedding_create: more than 2^23 rows, 2^20 columns or 2^22 tokens");
     if (device != DDP_DEVICE_NONE) {
         int count = 0;
-        if (hipGetDeviceCount(&count) != hipSuccess || device >= count)
+        if (taken(hipGetDeviceCount(&count)) != hipSuccess || device >= count)
             return fail(nullptr, DDP_ERR_HIP, "ddp_embedding_create: no such HIP device (the library needs a GPU; DDP_DEVICE_NONE checks arguments only)");
     }
     ddp_embedding* e = new (std::nothrow) ddp_embedding();
@@ -988,8 +988,8 @@ int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, 
         const int64_t tokens = up(max_tokens * 4, 256), first = up((places + 1) * 4, 256), starts = up(chunks * (buckets + 1) * 2, 256);
         const int64_t split = up(chunks * (2 * kChunk >> kLog2Window) * 4, 256);
         const int64_t partial = (((max_tokens - 1) >> kLog2Window) + 1) * 2 * width * 4;
-        hipError_t err = hipSetDevice(device);
-        if (err == hipSuccess) err = hipMalloc(reinterpret_cast<void**>(&e->mem), 3 * tokens + first + split + up(partial, 256) + starts);
+        hipError_t err = taken(hipSetDevice(device));
+        if (err == hipSuccess) err = taken(hipMalloc(reinterpret_cast<void**>(&e->mem), 3 * tokens + first + split + up(partial, 256) + starts));
         if (err != hipSuccess) {
             delete e;
             return fail(nullptr, DDP_ERR_HIP, hipGetErrorString(err));
@@ -1010,9 +1010,9 @@ int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, 
 int32_t ddp_embedding_destroy(ddp_embedding* e) {
     if (!e) return DDP_ERR_ARG;
     if (e->mem) {
-        (void)hipSetDevice(e->device);
-        (void)hipStreamSynchronize(e->stream);
-        (void)hipFree(e->mem);
+        (void)taken(hipSetDevice(e->device));
+        (void)taken(hipStreamSynchronize(e->stream));
+        (void)taken(hipFree(e->mem));
     }
     delete e;
     return DDP_OK;

@@ -510,7 +510,7 @@ int32_t fail(ddp_opt* o, int32_t code, const char* msg) {
 
 #define OPT_HIP(o, expr)                                                            \
     do {                                                                            \
-        const hipError_t e_ = (expr);                                               \
+        const hipError_t e_ = taken(expr);                                          \
         if (e_ != hipSuccess) return fail((o), DDP_ERR_HIP, hipGetErrorString(e_)); \
     } while (0)
 
@@ -704,7 +704,7 @@ int32_t ddp_opt_create(ddp_opt** out, int32_t device, void* stream) {
     if (device < DDP_DEVICE_NONE) return fail(nullptr, DDP_ERR_ARG, "ddp_opt_create: bad device");
     if (device != DDP_DEVICE_NONE) {
         int count = 0;
-        if (hipGetDeviceCount(&count) != hipSuccess || device >= count)
+        if (taken(hipGetDeviceCount(&count)) != hipSuccess || device >= count)
             return fail(nullptr, DDP_ERR_HIP, "ddp_opt_create: no such HIP device (the library needs a GPU; DDP_DEVICE_NONE checks arguments only)");
     }
     ddp_opt* o = new (std::nothrow) ddp_opt();
@@ -718,9 +718,9 @@ int32_t ddp_opt_create(ddp_opt** out, int32_t device, void* stream) {
 int32_t ddp_opt_destroy(ddp_opt* o) {
     if (!o) return DDP_ERR_ARG;
     if (o->mem) {
-        (void)hipSetDevice(o->device);
-        (void)hipStreamSynchronize(o->stream);
-        (void)hipFree(o->mem);
+        (void)taken(hipSetDevice(o->device));
+        (void)taken(hipStreamSynchronize(o->stream));
+        (void)taken(hipFree(o->mem));
     }
     delete o;
     return DDP_OK;

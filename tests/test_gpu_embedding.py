@@ -356,3 +356,14 @@ def test_grad_captured():
         assert torch.equal(one, two), k
     a.close()
     b.close()
+
+
+def test_a_workspace_that_does_not_fit():
+    """2^22 tokens of a row of 2^20 columns ask for a terabyte.  The refusal is this call's alone: the next ones
+    do not report it again."""
+    torch, d = lib()
+    with pytest.raises(d.DdpError) as e:
+        d.ddp_embedding_create(0, 0, 1, 1 << 20, 1 << 22)
+    assert e.value.code == d.DDP_ERR_HIP
+    check_lookup(7, 40, [1, 2, 6], FP32, FP32)
+    check_grad(7, 40, [1, 2, 6], FP32, FP32)
