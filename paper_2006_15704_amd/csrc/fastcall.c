@@ -404,7 +404,12 @@ static PyObject* opt_grad_norm(PyObject* self, PyObject* const* a, Py_ssize_t na
     void *o, *out;
     double scale;
     if (nargs != 3 || g_norm == NULL || !plain_ptr(a[0], &o) || !plain_f64(a[1], &scale) || !plain_ptr(a[2], &out)) Py_RETURN_NONE;
-    return PyLong_FromLong((long)g_norm(o, scale, NULL, (float*)out));
+    int32_t status;
+    /* the first call may lay out tables, which waits for the stream: other Python threads run meanwhile */
+    Py_BEGIN_ALLOW_THREADS
+    status = g_norm(o, scale, NULL, (float*)out);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong((long)status);
 }
 
 /* opt_adamw_step(handle_address, lr, beta1, beta2, eps, weight_decay, grad_scale, max_norm, skip_nonfinite) -> status, or None:

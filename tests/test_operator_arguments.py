@@ -181,3 +181,36 @@ def test_arguments_that_are_not_plain(d, emb, opt):
         d.ddp_embedding_lookup(emb, 5, 256, 64, 256, 0, 16, None, 256, 0, 16)
     with pytest.raises(TypeError):
         d.ddp_embedding_lookup(emb, 5.0, 256, 64, 256, 0, 16, 1.0, 256, 0, 16)
+
+
+def test_other_threads_run_during_a_norm(d):
+    """The first norm of a handle may allocate tables and wait for the stream: the interpreter's lock is free meanwhile.  Here the
+    call's place is taken by a sleep in C, of as many microseconds as the handle's address says."""
+    import threading
+    import time
+    b = d.binding
+    sleep = C.cast(C.CDLL(None).usleep, C.c_void_p).value
+    own = [C.cast(f, C.c_void_p).value for f in (b._lib.ddp_embedding_lookup, b._lib.ddp_embedding_grad, b._lib.ddp_opt_grad_norm,
+                                                 b._lib.ddp_opt_adamw_step)]
+    ticks, stop = [], threading.Event()
+
+    def tick():
+        while not stop.is_set():
+            ticks.append(time.monotonic())
+            time.sleep(0.005)
+
+    other = threading.Thread(target=tick)
+    b._fast.bind_around(own[0], own[1], sleep, own[3])
+    try:
+        other.start()
+        while not ticks:
+            time.sleep(0.001)
+        start = time.monotonic()
+        assert b._fast.opt_grad_norm(600000, 1.0, 0) == 0
+        end = time.monotonic()
+    finally:
+        stop.set()
+        other.join()
+        b._fast.bind_around(*own)
+    assert end - start >= 0.5
+    assert sum(start + 0.1 < t < end - 0.1 for t in ticks) >= 5
