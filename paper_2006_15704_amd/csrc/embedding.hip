@@ -1009,10 +1009,10 @@ int32_t ddp_embedding_create(ddp_embedding** out, int32_t device, void* stream, 
 
 int32_t ddp_embedding_destroy(ddp_embedding* e) {
     if (!e) return DDP_ERR_ARG;
-    if (e->mem) {
+    if (e->device != DDP_DEVICE_NONE) {
         (void)taken(hipSetDevice(e->device));
-        (void)taken(hipStreamSynchronize(e->stream));
-        (void)taken(hipFree(e->mem));
+        (void)taken(hipStreamSynchronize(e->stream));    // (lookups too: the caller frees what they use)
+        if (e->mem) (void)taken(hipFree(e->mem));
     }
     delete e;
     return DDP_OK;

@@ -367,3 +367,20 @@ def test_a_workspace_that_does_not_fit():
     assert e.value.code == d.DDP_ERR_HIP
     check_lookup(7, 40, [1, 2, 6], FP32, FP32)
     check_grad(7, 40, [1, 2, 6], FP32, FP32)
+
+
+def test_destroy_waits_for_lookups():
+    """A handle for lookups alone has no workspace to free; its outstanding work is waited for all the same."""
+    torch, d = lib()
+    rows, width, tokens = 64, 1024, 1 << 20
+    stream = torch.cuda.Stream()
+    table = torch.ones((rows, width), dtype=torch.bfloat16, device="cuda")
+    ids = torch.zeros(tokens, dtype=torch.int64, device="cuda")
+    out = torch.zeros((tokens, width), dtype=torch.bfloat16, device="cuda")
+    emb = d.ddp_embedding_create(0, stream.cuda_stream, rows, width, 0)
+    torch.cuda.synchronize()
+    for _ in range(50):                                       # some 20 ms
+        d.ddp_embedding_lookup(emb, tokens, ids.data_ptr(), 64, table.data_ptr(), BF16, width, 3.0, out.data_ptr(), BF16, width)
+    d.ddp_embedding_destroy(emb)
+    assert stream.query(), "destroyed with work outstanding"
+    assert (out == 3.0).all()
