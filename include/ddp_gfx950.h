@@ -565,7 +565,8 @@ int32_t ddp_opt_set_groups(ddp_opt* opt, const float* lr_scale, const float* dec
  * forward pass's weights); a NULL address: this tensor has none. */
 int32_t ddp_opt_set_copies(ddp_opt* opt, const int32_t* copy_dtype, void* const* copy_ptrs);
 
-/* The state, aligned to 16 bytes; allocates the handle's tables. */
+/* The state, aligned to 16 bytes; allocates the handle's tables (which a ddp_opt_grad_norm in front of it, or without
+ * parameters ddp_opt_register, does for the norm: capture a norm after one of them). */
 int32_t ddp_opt_set_state(ddp_opt* opt, int32_t kind, void* state, int64_t bytes);
 
 /* The 2-norm over all gradients, summed in 64 bits in a fixed order: |grad_scale|

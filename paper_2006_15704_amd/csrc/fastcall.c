@@ -405,7 +405,7 @@ static PyObject* opt_grad_norm(PyObject* self, PyObject* const* a, Py_ssize_t na
     double scale;
     if (nargs != 3 || g_norm == NULL || !plain_ptr(a[0], &o) || !plain_f64(a[1], &scale) || !plain_ptr(a[2], &out)) Py_RETURN_NONE;
     int32_t status;
-    /* the first call may lay out tables, which waits for the stream: other Python threads run meanwhile */
+    /* the first call may allocate tables and copy them to the GPU: other Python threads run meanwhile */
     Py_BEGIN_ALLOW_THREADS
     status = g_norm(o, scale, NULL, (float*)out);
     Py_END_ALLOW_THREADS

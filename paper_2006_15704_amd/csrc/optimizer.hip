@@ -488,6 +488,7 @@ struct ddp_opt {
     int norm_each = 1;                           // tiles that a block takes
     // device memory owned by the library: segments, tile maps, used mask, counters, partial sums, NormState
     char* mem = nullptr;
+    std::vector<char*> earlier;                  // tables from before ddp_opt_set_state
     OptSeg* d_seg = nullptr;
     int32_t *d_step_seg = nullptr, *d_norm_seg = nullptr;
     uint32_t* d_used = nullptr;
@@ -585,12 +586,10 @@ int32_t build(ddp_opt* o) {
         seg.push_back(s);
     }
     OPT_HIP(o, hipSetDevice(o->device));
-    if (o->mem != nullptr) {                     // built before, for the norm alone
-        o->built = false;
-        OPT_HIP(o, hipStreamSynchronize(o->stream));
-        char* old = o->mem;
+    if (o->mem != nullptr) {                     // built before, for the norm alone: norms under way and captured ones go on reading it
+        o->earlier.push_back(o->mem);
         o->mem = nullptr;
-        OPT_HIP(o, hipFree(old));
+        o->built = false;
     }
     int64_t bytes = 0;
     auto take = [&](int64_t size) {
@@ -717,10 +716,11 @@ int32_t ddp_opt_create(ddp_opt** out, int32_t device, void* stream) {
 
 int32_t ddp_opt_destroy(ddp_opt* o) {
     if (!o) return DDP_ERR_ARG;
-    if (o->mem) {
+    if (o->mem || !o->earlier.empty()) {
         (void)taken(hipSetDevice(o->device));
         (void)taken(hipStreamSynchronize(o->stream));
-        (void)taken(hipFree(o->mem));
+        if (o->mem) (void)taken(hipFree(o->mem));
+        for (char* mem : o->earlier) (void)taken(hipFree(mem));
     }
     delete o;
     return DDP_OK;

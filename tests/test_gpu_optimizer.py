@@ -665,3 +665,36 @@ def test_second_moments_far_below_their_largest(large, small):
     assert 1e-3 * small * small > 2.0 ** -148                # a binary32
     assert (vc == np.where(held == 0, 0, np.where(held > 1.0, 255, 1))).all()
     prog.close()
+
+
+def test_a_norm_captured_before_the_state_is_set():
+    """ddp_opt_set_state lays the tables out anew; a graph from before goes on reading its own."""
+    torch, d = lib()
+    stream = torch.cuda.Stream()
+    numel = [3000, 70, 5000]
+    p, g = Flat(numel, FP32, [np.ones(n) for n in numel]), Flat(numel, BF16, [np.full(n, 0.5) for n in numel])
+    out, held = torch.zeros(1, device="cuda"), []
+    opt = d.ddp_opt_create(0, stream.cuda_stream)
+    d.ddp_opt_register(opt, numel, [FP32] * 3, p.ptrs(), [BF16] * 3, g.ptrs())
+    torch.cuda.synchronize()
+    d.ddp_opt_grad_norm(opt, 1.0, out.data_ptr())            # (the tables are allocated here: not in the capture)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        d.ddp_opt_grad_norm(opt, 2.0, out.data_ptr(), [1, 0, 1])
+    _, where = d.ddp_opt_state_layout(numel, d.DDP_STATE_FP32)
+    state = torch.zeros(where["bytes"], dtype=torch.uint8, device="cuda")
+    d.ddp_opt_set_state(opt, d.DDP_STATE_FP32, state.data_ptr(), where["bytes"])
+    for k in range(4):
+        held.append(torch.full((1 << 16,), float("nan"), device="cuda"))     # (what was free would be somebody else's now)
+        g.view(2).fill_(0.25 * k)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = 2.0 * np.sqrt(3000 * 0.25 + 5000 * (0.25 * k) ** 2)
+        assert abs(out.item() - want) <= 2 * U * want, k
+        d.ddp_opt_grad_norm(opt)
+        d.ddp_opt_adamw_step(opt, 1e-3, max_norm=1.0)
+        torch.cuda.synchronize()
+        assert int(state[:8].view(torch.int64).item()) == k + 1
+    d.ddp_opt_destroy(opt)

@@ -184,7 +184,7 @@ def test_arguments_that_are_not_plain(d, emb, opt):
 
 
 def test_other_threads_run_during_a_norm(d):
-    """The first norm of a handle may allocate tables and wait for the stream: the interpreter's lock is free meanwhile.  Here the
+    """The first norm of a handle may allocate tables and copy them: the interpreter's lock is free meanwhile.  Here the
     call's place is taken by a sleep in C, of as many microseconds as the handle's address says."""
     import threading
     import time
