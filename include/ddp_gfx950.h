@@ -580,7 +580,7 @@ int32_t ddp_opt_grad_norm(ddp_opt* opt, double grad_scale, const uint8_t* used, 
  *   p = p - lr weight_decay p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * t counts the steps in the state, this one included.  All in binary32 (root and
  * reciprocal to one unit in the last place; a second moment below the smallest normal number may
- * count as 0 there) and rounded
+ * count as 0 there; an eps above 0 counts as at least that number) and rounded
  * once to a parameter's type; the moments of DDP_STATE_8BIT are rounded after they
  * have served.  max_norm <= 0: no clipping; norm is |grad_scale| times
  * that of the latest ddp_opt_grad_norm, which max_norm > 0 and skip_nonfinite need since the step

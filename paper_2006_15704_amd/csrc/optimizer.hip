@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -895,7 +896,8 @@ int32_t ddp_opt_adamw_step(ddp_opt* o, double lr, double beta1, double beta2, do
         a.rest1 = static_cast<float>(1.0 - beta1);
         a.beta2 = static_cast<float>(beta2);
         a.rest2 = static_cast<float>(1.0 - beta2);
-        a.eps = static_cast<float>(eps);
+        // below the smallest normal number the reciprocal takes eps for 0: an element of no gradient would be 0 / 0, not 0 / eps
+        a.eps = eps > 0.0 ? std::max(static_cast<float>(eps), FLT_MIN) : 0.0f;
         a.skip_nonfinite = skip_nonfinite != 0;
         bool counted = false;
         for (size_t i = 0; i < o->launches.size(); ++i) {

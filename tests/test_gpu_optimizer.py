@@ -698,3 +698,17 @@ def test_a_norm_captured_before_the_state_is_set():
         torch.cuda.synchronize()
         assert int(state[:8].view(torch.int64).item()) == k + 1
     d.ddp_opt_destroy(opt)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-30, 1e-38, 1e-40, 1e-44, 1e-60, 1e-300])
+def test_an_eps_below_the_smallest_normal_number(eps, bits):
+    """An element without a gradient stays where it is (0 / eps) for every eps above 0; others step by lr."""
+    prog = Program(numel=[600], bits=bits, seed=23)
+    prog.g.view(0)[100:].zero_()
+    hyper = dict(HYPER, eps=eps, weight_decay=0.0)
+    p0 = prog.p.host()[0]
+    for k in range(2):
+        check_step(prog, lambda: step(prog, hyper), hyper, what=f"step {k}")
+    assert (prog.p.host()[0][512:] == p0[512:]).all()        # (a block of zeros with 8 bits, too)
+    prog.close()
