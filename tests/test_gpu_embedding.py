@@ -384,3 +384,146 @@ def test_destroy_waits_for_lookups():
     d.ddp_embedding_destroy(emb)
     assert stream.query(), "destroyed with work outstanding"
     assert (out == 3.0).all()
+
+
+# Calls of more than 4096 tokens go by the sort whatever the table is; the rows' own tokens are at random places among ids
+# that take no part.
+LONG = 4500
+
+
+def among_others(ids, seed, total=LONG):
+    rng = np.random.default_rng(seed)
+    out = np.where(np.arange(total) % 2 == 0, -1, 1 << 30)
+    out[np.sort(rng.choice(total, len(ids), replace=False))] = ids
+    return out
+
+
+@pytest.mark.parametrize("lead", [0, 1, 31, 32, 33])
+@pytest.mark.parametrize("tokens", [1, 31, 32, 33, 63, 64, 65, 96, 97, 4000])
+def test_sorted_grad_of_one_row(tokens, lead):
+    """Every length at which a row's tokens are split or end a part, starting everywhere in a window."""
+    ids = np.concatenate([np.zeros(lead), np.full(tokens, 1), [3]])
+    check_grad(5, 20, among_others(ids, tokens), FP32, FP32, poison=True)
+    check_grad(5, 20, among_others(np.random.default_rng(lead).permutation(ids), tokens), BF16, FP32, add=True)
+
+
+@pytest.mark.parametrize("lead", [0, 1, 127, 128])
+def test_sorted_grad_of_long_windows(lead):
+    """Few and wide rows: windows of 128 tokens."""
+    lengths = (lead, 127, 129, 128, 256, 255, 257, 1, 0, 14000)
+    ids = np.random.default_rng(lead).permutation(np.concatenate([np.full(n, r) for r, n in enumerate(lengths)]))
+    check_grad(len(lengths), 2080, ids, FP32, BF16)
+
+
+@pytest.mark.parametrize("lengths", [(33, 33, 33), (40, 1, 40), (32, 33, 31, 64), (1, 100, 1, 100), (33, 31, 33, 31, 1), (64, 64, 33, 0, 63)])
+def test_sorted_grad_rows_that_meet_in_a_window(lengths):
+    ids = np.concatenate([np.full(n, r) for r, n in enumerate(lengths)])
+    for seed in range(2):
+        mixed = among_others(np.random.default_rng(seed).permutation(ids), seed)
+        check_grad(len(lengths), 24, mixed, BF16, BF16, seed=seed, poison=True)
+        check_grad(len(lengths), 24, mixed, FP32, FP16, seed=seed, add=True)
+
+
+@pytest.mark.parametrize("dout_dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("grad_dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("bits", [32, 64])
+def test_sorted_grad_types(dout_dt, grad_dt, add, bits):
+    rng = np.random.default_rng(2)
+    check_grad(50, 130, zipf(rng, 50, LONG), dout_dt, grad_dt, add=add, bits=bits)
+    check_grad(3000, 37, zipf(rng, 3000, LONG), dout_dt, grad_dt, add=add, bits=bits)
+    check_grad(300, 3, zipf(rng, 300, LONG), dout_dt, grad_dt, add=add, bits=bits)
+
+
+@pytest.mark.parametrize("padding", [-1, 0, 6])
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("bits", [32, 64])
+def test_sorted_grad_padding_is_not_read(padding, add, bits):
+    rng = np.random.default_rng(3)
+    ids = rng.integers(-3, 12, LONG + 1000)
+    ids[7], ids[8] = (2 ** 31 - 1, -2 ** 31) if bits == 32 else (2 ** 40, -2 ** 50)
+    check_grad(9, 77, ids, BF16, FP32, padding=padding, add=add, bits=bits, poison=True)
+    ids = rng.integers(-100, 4000, LONG + 1000)
+    check_grad(3900, 21, ids, FP16, FP16, padding=padding, add=add, bits=bits, poison=True)
+
+
+@pytest.mark.parametrize("bits", [32, 64])
+def test_sorted_grad_without_a_token_that_counts(bits):
+    for rows in (9, 3000):
+        got = check_grad(rows, 33, np.full(LONG, 4), FP32, FP16, padding=4, poison=True, bits=bits)
+        assert (got == 0).all()
+        check_grad(rows, 33, np.full(LONG, 4), FP32, FP16, padding=4, poison=True, add=True, bits=bits)
+        check_grad(rows, 33, np.full(LONG, -1), FP32, FP16, add=True, bits=bits)
+        got = check_grad(rows, 33, np.full(LONG, rows), BF16, BF16, poison=True, bits=bits)
+        assert (got == 0).all()
+
+
+@pytest.mark.parametrize("gaps,shifts", [((3, 0), (0, 1)), ((0, 5), (1, 3)), ((1, 1), (1, 0)), ((8, 8), (4, 4))])
+@pytest.mark.parametrize("dt", [FP32, FP16, BF16])
+def test_sorted_grad_strides_and_alignments(gaps, shifts, dt):
+    rng = np.random.default_rng(4)
+    for rows, width in ((61, 131), (2500, 259), (700, 5)):
+        check_grad(rows, width, zipf(rng, rows, LONG), dt, dt, gaps=gaps, shifts=shifts)
+        check_grad(rows, width, zipf(rng, rows, LONG), dt, FP32 if dt == BF16 else BF16, gaps=gaps, shifts=shifts, add=True)
+
+
+def test_ids_at_any_element():
+    """Ids that start in the middle of an 8- or 16-byte word, by either way through the tokens."""
+    torch, d = lib()
+    rng = np.random.default_rng(9)
+    for bits in (32, 64):
+        for tokens in (700, LONG):
+            values = rng.integers(-2, 40, tokens)
+            dout, grads = torch.randn((tokens, 24), device="cuda"), []
+            t = Table(39, 24, tokens)
+            for shift in (0, 1, 3):
+                on, grad = ids_on(values, bits, shift), torch.empty((39, 24), device="cuda")
+                torch.cuda.synchronize()
+                t.grad(on, dout, FP32, grad, FP32, bits=bits)
+                torch.cuda.synchronize()
+                grads.append(grad)
+            assert torch.equal(grads[0], grads[1]) and torch.equal(grads[0], grads[2])
+            want, size = ops.embedding_grad(39, values, dout.double().cpu().numpy(), 1.5)
+            assert (np.abs(grads[0].double().cpu().numpy() - want) <= (tokens + 3) * U * size).all()
+            t.close()
+
+
+@pytest.mark.parametrize("rows,width", [(300, 64), (5, 300), (20000, 21)])
+def test_sorted_grad_captured(rows, width):
+    """Replays of a captured call that sorts, with other tokens and eager work in between."""
+    torch, _ = lib()
+    tokens = 6000
+    stream = torch.cuda.Stream()
+    rng = np.random.default_rng(8)
+    a, b = Table(rows, width, tokens, stream.cuda_stream), Table(rows, width, tokens)
+    ids = ids_on(zipf(rng, rows, tokens), 64)
+    dout = torch.randn((tokens, width), device="cuda", dtype=torch.bfloat16)
+    one, two = torch.empty((rows, width), device="cuda"), torch.empty((rows, width), device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        a.grad(ids, dout, BF16, one, FP32)
+    for k in range(5):
+        spread = zipf(rng, rows, tokens) if k % 2 else np.where(rng.random(tokens) < 0.5, rng.integers(-3, rows, tokens), k)
+        ids.copy_(torch.from_numpy(spread))
+        dout.normal_()
+        one.fill_(float("nan"))
+        torch.cuda.synchronize()
+        graph.replay()
+        b.grad(ids, dout, BF16, two, FP32)
+        torch.cuda.synchronize()
+        assert torch.equal(one, two), k
+        want, size = ops.embedding_grad(rows, spread, dout.double().cpu().numpy(), 1.5)
+        assert (np.abs(one.double().cpu().numpy() - want) <= (tokens + 3) * U * size).all(), k
+    a.close()
+    b.close()
+
+
+@pytest.mark.parametrize("table_dt,out_dt", [(FP32, FP32), (FP32, BF16), (BF16, BF16), (FP16, FP32), (BF16, FP16)])
+@pytest.mark.parametrize("width,tokens", [(1037, 2300), (67, 33000), (513, 4400)])
+def test_lookup_of_more_than_the_caches_keep(table_dt, out_dt, width, tokens):
+    """More than 4 MiB of rows are stored past the caches: odd widths, gaps and shifted bases."""
+    rng = np.random.default_rng(width)
+    assert width * tokens * (4 if out_dt == FP32 else 2) > 4 << 20
+    check_lookup(41, width, rng.integers(-1, 42, tokens), table_dt, out_dt, 32, gaps=(1, 0), shifts=(1, 1))
+    check_lookup(41, width, rng.integers(-1, 42, tokens), table_dt, out_dt, 64, gaps=(0, 3), shifts=(0, 3))
