@@ -712,3 +712,72 @@ def test_an_eps_below_the_smallest_normal_number(eps, bits):
         check_step(prog, lambda: step(prog, hyper), hyper, what=f"step {k}")
     assert (prog.p.host()[0][512:] == p0[512:]).all()        # (a block of zeros with 8 bits, too)
     prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_counted_by_a_launch_of_their_own(bits):
+    """20000 tensors of one element are 20000 blocks: more than count themselves, for both kinds of state.  Each step is counted once, one
+    that is skipped is not."""
+    torch, d = lib()
+    n = 20000
+    prog = Program(numel=[1] * n, bits=bits, skew=0, seed=24)
+    p0 = prog.p.buf.clone()
+    step(prog)
+    assert prog.steps() == 1 and (prog.p.buf != p0).cpu().numpy()[8:8 + n].all()
+    d.ddp_opt_grad_norm(prog.opt)
+    step(prog, max_norm=1.0, skip_nonfinite=True)
+    assert prog.steps() == 2
+    for bad in (float("nan"), float("-inf")):
+        held = [x.clone() for x in (prog.p.buf, prog.state)]
+        keep = prog.g.view(n - 1).clone()
+        prog.g.view(n - 1).fill_(bad)
+        torch.cuda.synchronize()
+        d.ddp_opt_grad_norm(prog.opt)
+        step(prog, max_norm=1.0, skip_nonfinite=True)
+        torch.cuda.synchronize()
+        assert torch.equal(prog.p.buf, held[0]) and torch.equal(prog.state, held[1]) and prog.steps() == 2
+        prog.g.view(n - 1).copy_(keep)
+    check = prog.p.host()
+    want = [ops.adamw(check[i], prog.g.host()[i], *prog.moments()[i], 3, 1e-2, 0.9, 0.999, 1e-8, 0.1)[0] for i in (0, 7777, n - 1)]
+    torch.cuda.synchronize()
+    step(prog)
+    assert prog.steps() == 3
+    for i, w in zip((0, 7777, n - 1), want):
+        got = prog.p.view(i).double().cpu().numpy()
+        assert np.abs(got - w).max() <= 40 * U * 1e-2 * 12 + 4 * U * (np.abs(check[i]) + np.abs(w)).max(), i
+    prog.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_of_nothing_are_counted(bits):
+    """A list of empty tensors: no blocks at all, and the count goes on, unless the step is skipped."""
+    _, d = lib()
+    prog = Program(numel=[0, 0, 0], bits=bits)
+    step(prog)
+    d.ddp_opt_grad_norm(prog.opt)
+    step(prog, max_norm=1.0, skip_nonfinite=True)            # a norm of 0
+    assert prog.steps() == 2
+    prog.close()
+
+
+def test_types_in_launches_of_which_some_count_by_themselves():
+    """The last run of equal types decides who counts: a long one, and a short one behind a long one."""
+    torch, d = lib()
+    for types in ([FP32, BF16], [BF16, FP32]):
+        numel = [17 * (1 << 20) + 3, 700]
+        ps = [torch.ones(n, dtype=torch_type(torch, t), device="cuda") for n, t in zip(numel, types)]
+        gs = [torch.full((n,), 0.5, dtype=torch_type(torch, t), device="cuda") for n, t in zip(numel, types)]
+        _, where = d.ddp_opt_state_layout(numel, d.DDP_STATE_FP32)
+        state = torch.zeros(where["bytes"], dtype=torch.uint8, device="cuda")
+        opt = d.ddp_opt_create(0)
+        d.ddp_opt_register(opt, numel, types, [x.data_ptr() for x in ps], types, [x.data_ptr() for x in gs])
+        d.ddp_opt_set_state(opt, d.DDP_STATE_FP32, state.data_ptr(), where["bytes"])
+        torch.cuda.synchronize()
+        for k in range(3):
+            d.ddp_opt_adamw_step(opt, 0.125)
+            torch.cuda.synchronize()
+            assert int(state[:8].view(torch.int64).item()) == k + 1
+            for x in ps:                                     # a constant gradient: every step is lr, to binary32 roundings and those of the type
+                want = 1.0 - 0.125 * (k + 1)
+                assert ((x.float() - want).abs() <= 2.0 ** -8 if x.dtype == torch.bfloat16 else (x - want).abs() <= 1e-5).all()
+        d.ddp_opt_destroy(opt)
