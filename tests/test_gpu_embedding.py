@@ -527,3 +527,88 @@ def test_lookup_of_more_than_the_caches_keep(table_dt, out_dt, width, tokens):
     assert width * tokens * (4 if out_dt == FP32 else 2) > 4 << 20
     check_lookup(41, width, rng.integers(-1, 42, tokens), table_dt, out_dt, 32, gaps=(1, 0), shifts=(1, 1))
     check_lookup(41, width, rng.integers(-1, 42, tokens), table_dt, out_dt, 64, gaps=(0, 3), shifts=(0, 3))
+
+
+def check_whole(rows, width, ids, add=False, bits=64, max_tokens=None):
+    """Small whole numbers: every sum is exact in binary32, whatever its order, so the gradient is compared with equality."""
+    torch, d = lib()
+    gen = torch.Generator(device="cuda").manual_seed(rows + width)
+    ids = torch.as_tensor(ids, device="cuda")
+    T = len(ids)
+    dout = torch.randint(-3, 4, (T, width), generator=gen, device="cuda", dtype=torch.int8).bfloat16()
+    grad = torch.full((rows + 1, width), 5.0, device="cuda")
+    used = ((ids >= 0) & (ids < rows)).nonzero().reshape(-1)
+    want = torch.full((rows, width), 5.0 if add else 0.0, device="cuda", dtype=torch.float64)
+    if rows <= 8:
+        for r in range(rows):
+            for some in (ids == r).nonzero().reshape(-1).split(1 << 18):
+                want[r] += 2.0 * dout[some].double().sum(0)
+    else:
+        for some in used.split(1 << 18):
+            want.index_add_(0, ids[some].long(), 2.0 * dout[some].double())
+    on = ids.to(torch.int64 if bits == 64 else torch.int32)
+    emb = d.ddp_embedding_create(0, 0, rows, width, max_tokens or T)
+    for _ in range(1 if add else 2):
+        torch.cuda.synchronize()
+        d.ddp_embedding_grad(emb, T, on.data_ptr(), bits, dout.data_ptr(), BF16, width, 2.0, -1, add, grad.data_ptr(), FP32, width)
+    torch.cuda.synchronize()
+    assert torch.equal(grad[:rows].double(), want) and (grad[rows] == 5.0).all()
+    d.ddp_embedding_destroy(emb)
+
+
+@pytest.mark.parametrize("rows,width", [((1 << 19) + 1, 12), ((1 << 20) + 3, 5), (1 << 23, 1), (40000, 1030), (30522, 64)])
+@pytest.mark.parametrize("tokens", [1, 700, 4096, 4097, 20000])
+@pytest.mark.parametrize("add", [False, True])
+def test_grad_of_large_tables(rows, width, tokens, add):
+    """Up to the largest table there can be, by either way through the tokens; blocks of the first have rows in pairs here."""
+    rng = np.random.default_rng(rows)
+    near = np.concatenate([[0, 1, rows - 1, rows - 2], rng.integers(0, 8, tokens)])[:tokens]
+    check_whole(rows, width, rng.integers(-2, rows + 2, tokens), add)
+    check_whole(rows, width, np.where(rng.random(tokens) < 0.5, near, rng.integers(0, rows, tokens)), add, bits=32)
+
+
+@pytest.mark.parametrize("rows,width", [(1, 3), (2, 40), (5, 3), (700, 20), (30522, 9), (1 << 21, 2)])
+@pytest.mark.parametrize("tokens", [524288, 524289, 1 << 22])
+def test_grad_of_the_longest_calls(rows, width, tokens):
+    """More chunks of tokens than a block of the sort has threads, up to the most tokens of a call."""
+    rng = np.random.default_rng(tokens)
+    check_whole(rows, width, zipf(rng, rows, tokens))
+    check_whole(rows, width, rng.integers(-1, rows, tokens), bits=32)
+    sparse = np.where(np.arange(tokens) % 4099 == 7, rng.integers(0, rows, tokens), -1)
+    check_whole(rows, width, sparse)
+    sparse[-100:] = rows - 1                     # of the last chunk alone
+    check_whole(rows, width, sparse, add=True)
+
+
+@pytest.mark.parametrize("tokens", [3, 1025])
+@pytest.mark.parametrize("width", [1 << 20, (1 << 20) - 3])
+def test_the_widest_rows(tokens, width):
+    torch, d = lib()
+    ids = np.arange(tokens) % 4 - 1
+    check_whole(3, width, ids)
+    check_whole(3, width, ids, add=True)
+    table = torch.randint(-9, 9, (3, width), device="cuda").half()
+    on, out = torch.as_tensor(ids[:7].copy(), device="cuda"), torch.full((len(ids[:7]), width), 7.0, device="cuda")
+    emb = d.ddp_embedding_create(0, 0, 3, width, 0)
+    torch.cuda.synchronize()
+    d.ddp_embedding_lookup(emb, len(on), on.data_ptr(), 64, table.data_ptr(), FP16, width, 0.5, out.data_ptr(), FP32, width)
+    torch.cuda.synchronize()
+    want = torch.where((on >= 0)[:, None], table[on.clamp(min=0)].float() * 0.5, 0.0)
+    assert torch.equal(out, want)
+    d.ddp_embedding_destroy(emb)
+
+
+def test_calls_of_no_tokens():
+    """A lookup of none does nothing and needs no addresses; a gradient of none is zeros."""
+    torch, d = lib()
+    emb = d.ddp_embedding_create(0, 0, 5, 33, 10)
+    d.ddp_embedding_lookup(emb, 0, 0, 64, 0, FP32, 33, 1.0, 0, BF16, 33)
+    grad = torch.full((6, 33), 5.0, device="cuda")
+    torch.cuda.synchronize()
+    d.ddp_embedding_grad(emb, 0, 0, 32, 0, BF16, 33, 1.0, -1, True, grad.data_ptr(), FP32, 33)
+    torch.cuda.synchronize()
+    assert (grad == 5.0).all()
+    d.ddp_embedding_grad(emb, 0, 0, 32, 0, BF16, 33, 1.0, -1, False, grad.data_ptr(), FP32, 33)
+    torch.cuda.synchronize()
+    assert (grad[:5] == 0.0).all() and (grad[5] == 5.0).all()
+    d.ddp_embedding_destroy(emb)
