@@ -614,7 +614,7 @@ const char* ddp_embedding_last_error(const ddp_embedding* emb);
 
 /* out[t, :] = scale * table[ids[t], :], in binary32, rounded once to the type of out.
  * ids: device array of 32- or 64-bit integers (id_bits); an id outside
- * [0, rows) reads nothing and gives zeros.  Strides in elements, at least the width;
+ * [0, rows) gives zeros.  Strides in elements, at least the width;
  * any alignment to the element size.  table and out must not overlap. */
 int32_t ddp_embedding_lookup(ddp_embedding* emb, int64_t tokens, const void* ids, int32_t id_bits, const void* table, int32_t table_dtype,
                              int64_t table_stride, float scale, void* out, int32_t out_dtype, int64_t out_stride);

@@ -261,7 +261,7 @@ constexpr int kScanEach = kScanTokens / kScanThreads;
 constexpr int64_t kScanBlockBytes = 8192;        // to move by each of them
 constexpr int kScanBlocks = 4096;                // blocks to have where there are column ranges to go round
 constexpr int kScanAlone = 16;                   // tokens of a row that one wave sums
-constexpr int kScanRows = 32;                    // rows of 1024 columns that a block has at most (up to 1024 of fewer columns)
+constexpr int kScanRows = 32;                    // rows of 1024 columns that a block has at most, single (up to 1024 of fewer columns); twice that in pairs
 
 template <typename Id, int FT, int GT, int N>
 __global__ __launch_bounds__(kScanThreads, 6) void scan_sum_kernel(SumArgs a) {
@@ -403,7 +403,11 @@ __global__ __launch_bounds__(kScanThreads, 6) void scan_sum_kernel(SumArgs a) {
 // have many tokens the parts of a row would be.
 constexpr int kLog2Window = 5, kLog2LongWindow = 7;
 // 65536 tokens into two rows of 1024, us, windows of 32 / 128: sums 52 / 48, joins 32 / 10; but 42858 into five of 26 have too few
-// windows for the chip: 28 / 40 in all.
+// windows for the chip: 28 / 40 in all.  Over 192 calls (8192 to 131072 tokens, rows of 512 to 8192 bytes, 48 tokens a row and more): with
+// fewer than 600 column ranges of windows 32 wins, by up to half (8192 into 27 of 512 in bfloat16 21.5 / 30.8); at 1024 the two are within a tenth
+// (65536 into 128 of 1024 42.8 / 40.5), from 2048 on 128 wins by a tenth to a fifth (131072 into 256 of 1024 68 / 60), and one row takes half
+// the time (65536 into one of 1024 82 / 49).  Where the rule is not the better one it loses up to a quarter (48 to 255 tokens a row, many
+// ranges: 65536 into 682 of 4096 147 / 119; rows of 512 bytes: 131072 into 436 32 / 38), for one row of few ranges a half (71 / 47).
 inline int log2_window(int64_t tokens, int64_t rows, int64_t ranges) {
     return tokens / rows >= 256 && (tokens >> kLog2LongWindow) * ranges >= 1024 ? kLog2LongWindow : kLog2Window;
 }

@@ -145,7 +145,7 @@ __device__ __forceinline__ uint32_t byte_of(float x, int i, uint32_t into) { ret
 
 // One pass over four or five streams that are read and as many that are written.  Loads and stores carry the non-temporal hint: nothing is
 // used again before everything else has been (60 M elements, binary32: 322 us without, 288 with it, 325 with it on the stores
-// alone).  BERT-large, bfloat16 gradients and copies: 28 bytes an element in 1620 us, 5.8 TB/s; 8-bit states, 16 bytes, 905 us, 5.9 TB/s
+// alone).  BERT-large, bfloat16 gradients and copies: 28 bytes an element in 1620 us, 5.8 TB/s; 8-bit states, 16 bytes, 935 us, 5.8 TB/s
 // (a plain copy reaches 4.8 to 5.8).  8 bits: 75 vector instructions an element, which memory just covers; with IEEE roots and divisions
 // it was 1270 us.
 template <int PT, int GT, int CT, bool Q8, bool FULL>
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormArgs a, int blocks)
 
 // ---- states as values ----
 
-// A stream: 2 bytes an element are read, 8 written, past the caches.  BERT-large, both moments: 3.4 GB in 545 us, 6.2 TB/s.
+// A stream: 2 bytes an element are read, 8 written, past the caches.  BERT-large, both moments: 3.4 GB in 565 us, 6.0 TB/s.
 // A block takes kReadRounds vectors a thread, all on the way together, so that a cache line of scales belongs to two blocks: step and
 // read-out of BERT-large with 1 / 2 / 4 / 8 of them 1467 / 1491 / 1453 / 1512 us, of 3 M elements 19.4 / 18.9 / 19.1 / 20.4.
 constexpr int kReadRounds = 4;
