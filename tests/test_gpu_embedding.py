@@ -612,3 +612,52 @@ def test_calls_of_no_tokens():
     torch.cuda.synchronize()
     assert (grad[:5] == 0.0).all() and (grad[5] == 5.0).all()
     d.ddp_embedding_destroy(emb)
+
+
+def same_bits(got, want):
+    """Equal, signs of zeros included; NaN is NaN, whatever its payload."""
+    torch, _ = lib()
+    whole = {torch.float32: torch.int32, torch.float16: torch.int16, torch.bfloat16: torch.int16}[got.dtype]
+    nan = torch.isnan(want)
+    return torch.equal(torch.isnan(got), nan) and torch.equal(got.view(whole)[~nan], want.view(whole)[~nan])
+
+
+def every_pattern(dt):
+    """[rows, 64]: all 16-bit patterns, or binary32 ones around every edge of the three types' ranges and roundings."""
+    torch, _ = lib()
+    if dt != FP32:
+        return torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16).view(torch_type(torch, dt)).view(-1, 64)
+    edges = [0, 1, 2, 0x7FFF, 0x8000, 0x8001, 0xFFFF, 0x10000, 0x18000, 0x7FFFFF, 0x800000, 0x800001, 0x7F7FFFFF, 0x7F7F7FFF, 0x7F7F8000, 0x7F800000,
+             0x7F800001, 0x7FC00000, 0x33000000, 0x33000001, 0x33800000, 0x387FC000, 0x387FE000, 0x38800000, 0x477FEFFF, 0x477FF000, 0x47800000,
+             0x3F800000, 0x3F801000, 0x3F803000, 0x3F808000, 0x3F818000]
+    rng = np.random.default_rng(12)
+    bits = np.concatenate([np.array(edges), rng.integers(0, 0x7F800000, 8192 - 32)]).astype(np.uint32)
+    return torch.from_numpy(np.concatenate([bits, bits | 0x80000000]).view(np.float32).copy()).view(-1, 64)
+
+
+@pytest.mark.parametrize("table_dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("out_dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("scale", [1.0, 3.0, 2.0 ** -20, -2.0 ** 30])
+def test_lookup_and_grad_of_every_pattern(table_dt, out_dt, scale):
+    """Subnormal numbers, the ends of the ranges, ties, infinities and NaN: one product in binary32, one rounding.  A gradient of one token
+    a row is 0 + x, scaled (so that -0 becomes +0 times the scale)."""
+    torch, d = lib()
+    table = every_pattern(table_dt)
+    rows, width = table.shape
+    want = (table.float() * scale).to(torch_type(torch, out_dt))
+    summed = ((table.float() + 0.0) * scale).to(torch_type(torch, out_dt))
+    on = table.cuda()
+    for tokens in (rows, 5000):
+        ids = torch.cat([torch.randperm(rows, generator=torch.Generator().manual_seed(tokens)), torch.full((max(0, tokens - rows),), -1)])
+        there, out = ids.cuda(), torch.empty((len(ids), width), dtype=torch_type(torch, out_dt), device="cuda")
+        dout = torch.full((len(ids), width), float("nan"), dtype=table.dtype, device="cuda")
+        dout[:rows] = on[there[:rows]]
+        grad = torch.empty((rows, width), dtype=torch_type(torch, out_dt), device="cuda")
+        emb = d.ddp_embedding_create(0, 0, rows, width, len(ids))
+        torch.cuda.synchronize()
+        d.ddp_embedding_lookup(emb, len(ids), there.data_ptr(), 64, on.data_ptr(), table_dt, width, scale, out.data_ptr(), out_dt, width)
+        d.ddp_embedding_grad(emb, len(ids), there.data_ptr(), 64, dout.data_ptr(), table_dt, width, scale, -1, False, grad.data_ptr(), out_dt, width)
+        torch.cuda.synchronize()
+        assert same_bits(out[:rows].cpu(), want[ids[:rows]]) and (out[rows:] == 0).all()
+        assert same_bits(grad.cpu(), summed)
+        d.ddp_embedding_destroy(emb)
