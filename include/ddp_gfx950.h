@@ -629,6 +629,112 @@ int32_t ddp_embedding_grad(ddp_embedding* emb, int64_t tokens, const void* ids, 
                            int64_t dout_stride, float scale, int64_t padding_row, int32_t accumulate, void* grad, int32_t grad_dtype,
                            int64_t grad_stride);
 
+/* ---- Inside a layer: norm, relative position bias, routing to experts --------
+ *
+ * The parts of a transformer layer beside its matrix products whose parameters
+ * are small and shared by all tokens.  Their gradients are reductions over the
+ * batch that go into registered gradient tensors, as the embedding's does.
+ * Handles and conventions as for ddp_embedding: work is enqueued on the handle's
+ * stream, calls on a handle (and graphs captured from it) share its workspace and
+ * run one after the other, nothing is allocated after create, all calls may be
+ * captured.  The caller's current device is left as it was.  Strides are in
+ * elements, pointers are aligned to their element size, outputs overlap neither
+ * each other nor an input unless stated.  What lies behind the last row, between
+ * the rows and in masked places of an input is not used. */
+typedef struct ddp_layernorm ddp_layernorm;
+
+/* Rows of `width` (up to 2^20) elements.  The workspace takes up to 16 MiB, above 2^17 columns 128 bytes a column. */
+int32_t ddp_layernorm_create(ddp_layernorm** out, int32_t device, void* stream, int64_t width);
+int32_t ddp_layernorm_destroy(ddp_layernorm* norm);   /* waits for the handle's outstanding work */
+const char* ddp_layernorm_last_error(const ddp_layernorm* norm);
+
+/* s = x + residual (residual NULL: s = x), mean and rstd = 1 / sqrt(variance + eps) of each row of s,
+ * y = (s - mean) * rstd * gamma + beta, all in binary32 (the variance from the differences to the mean)
+ * and rounded once to the types of what is written: sum (s, may be NULL), y, and mean and rstd (one
+ * binary32 a row, may be NULL).  x, residual and sum are of x_dtype; y is of x_dtype too, or of any type
+ * where x is binary32 (DDP_ERR_UNSUPPORTED otherwise); gamma and beta (NULL: 1 and 0) of param_dtype. */
+int32_t ddp_layernorm_forward(ddp_layernorm* norm, int64_t rows, const void* x, int32_t x_dtype, int64_t x_stride, const void* residual,
+                              int64_t residual_stride, const void* gamma, const void* beta, int32_t param_dtype, float eps, void* sum,
+                              int64_t sum_stride, void* y, int32_t y_dtype, int64_t y_stride, float* mean, float* rstd);
+
+/* With xh = (x - mean) * rstd, x what was normalized (sum, where there was a residual), and g = dy * gamma:
+ *   dx = (g - mean(g) - xh * mean(g * xh)) * rstd + dsum
+ *   dgamma = sum over the rows of dy * xh      dbeta = sum over the rows of dy
+ * dsum (x_dtype, NULL: 0) is what flows back along the sum by itself.  dx is the gradient of x and of the residual alike.
+ * dx (x_dtype), dgamma and dbeta (grad_dtype) may be NULL each.  accumulate != 0: dgamma and dbeta are added to what they hold.
+ * Types as in the forward pass, dy as y.  In binary32, in an order that depends on the sizes alone (repeated calls give the same
+ * bits), rounded once. */
+int32_t ddp_layernorm_backward(ddp_layernorm* norm, int64_t rows, const void* dy, int32_t dy_dtype, int64_t dy_stride, const void* x,
+                               int32_t x_dtype, int64_t x_stride, const float* mean, const float* rstd, const void* gamma,
+                               int32_t param_dtype, const void* dsum, int64_t dsum_stride, void* dx, int64_t dx_stride,
+                               int32_t accumulate, void* dgamma, void* dbeta, int32_t grad_dtype);
+
+typedef struct ddp_position_bias ddp_position_bias;
+
+/* A learned bias of attention scores by relative position, r = position of the key - position of the query.  Distances have buckets:
+ *   f(d) = d below `exact`, then min(n - 1, exact + floor((n - exact) * log(d / exact) / log(max_distance / exact)))
+ * both == 0: n = buckets, the bucket of r is f(max(-r, 0)) (keys behind the query share bucket 0); both != 0: n = buckets / 2,
+ * f(|r|), + n for r > 0.  exact == n: every distance below n - 1 has its own, no logarithm.  The steps of the logarithm are
+ * settled in whole numbers.  Up to 4096 heads, 1024 buckets, a distance of 2^20. */
+int32_t ddp_position_bias_create(ddp_position_bias** out, int32_t device, void* stream, int32_t heads, int32_t buckets, int32_t exact,
+                                 int64_t max_distance, int32_t both);
+int32_t ddp_position_bias_destroy(ddp_position_bias* bias);   /* waits for the handle's outstanding work */
+const char* ddp_position_bias_last_error(const ddp_position_bias* bias);
+
+/* first[n] (host): the smallest distance of each bucket of one direction.  Returns n.  f(d) is the last bucket whose first
+ * distance is not above d. */
+int32_t ddp_position_bias_buckets(const ddp_position_bias* bias, int32_t* first);
+
+/* out[b, h, i, j] = scale * table[bucket(j - i - offset)][h] (+ out[b, h, i, j] with accumulate != 0) for every batch entry, head,
+ * query and key; `masked` (rounded to the type of out; what is there is not used) where the key is not visible: j >= key_lengths[b] (device, NULL: all
+ * visible; counts below 0 are 0), or with causal != 0 a key behind the query, j > i + offset.  offset: position of query 0 counted from
+ * key 0 (the number of cached keys, where queries follow them).  table: [buckets][heads] with a stride.  out: any three strides with which no two
+ * places coincide; keys are adjacent.  In binary32, rounded once. */
+int32_t ddp_position_bias_apply(ddp_position_bias* bias, int64_t batch, int64_t queries, int64_t keys, int64_t offset, const void* table,
+                                int32_t table_dtype, int64_t table_stride, float scale, const int32_t* key_lengths, int32_t causal,
+                                float masked, int32_t accumulate, void* out, int32_t out_dtype, int64_t batch_stride, int64_t head_stride,
+                                int64_t query_stride);
+
+/* grad[k][h] = scale * sum of dscores[b, h, i, j] over the visible places of bucket k (zeros where there are none; accumulate != 0:
+ * added to what grad holds).  Places are visible as above, and only queries i < query_lengths[b] (NULL: all) take part.  Strides of dscores
+ * may be anything from 0 on (0: the same scores for all).  Sums in binary32 along a diagonal and binary64 across, in an order that depends on the sizes
+ * alone (repeated calls give the same bits), rounded once. */
+int32_t ddp_position_bias_grad(ddp_position_bias* bias, int64_t batch, int64_t queries, int64_t keys, int64_t offset, const void* dscores,
+                               int32_t dtype, int64_t batch_stride, int64_t head_stride, int64_t query_stride, float scale,
+                               const int32_t* key_lengths, const int32_t* query_lengths, int32_t causal, int32_t accumulate, void* grad,
+                               int32_t grad_dtype, int64_t grad_stride);
+
+typedef struct ddp_router ddp_router;
+
+#define DDP_SCORE_SOFTMAX 0
+#define DDP_SCORE_SIGMOID 1
+
+/* Routing of tokens to `chosen` of `experts` (up to 64 of 1024).  With s the softmax over a token's logits or the sigmoid of each, and key = s + bias:
+ * groups of experts / groups neighbours have as score their largest key (top == 1) or the sum of their two largest (top == 2); the `kept`
+ * best groups are open; the open experts with the largest keys are chosen.  renormalise: weights are scale * s / (sum of the chosen s),
+ * otherwise scale * s. */
+int32_t ddp_router_create(ddp_router** out, int32_t device, void* stream, int32_t experts, int32_t chosen, int32_t groups, int32_t kept,
+                          int32_t top, int32_t score, int32_t renormalise, float scale);
+int32_t ddp_router_destroy(ddp_router* router);   /* waits for the handle's outstanding work */
+const char* ddp_router_last_error(const ddp_router* router);
+
+/* experts_out[t, :] (int32, [tokens][chosen]): the chosen experts in the order of their keys, as binary64 has them, ties to the lower
+ * index; weights[t, :] (of weights_dtype, [tokens][chosen]): theirs.  bias: binary32 [experts], NULL: zeros.  An expert whose logit is -inf or whose
+ * key is -inf or NaN is never chosen (nor does it count in its group; a softmax over a NaN or +inf gives NaN to all); places left over get index -1 and
+ * weight 0, and so does a sum of 0.  counts (int32 [experts], may be NULL): tokens that chose each expert; accumulate != 0: added to what is
+ * there.  A count of 0 on a replica is a 0 in ddp_mark_ready_local's flags for that expert's parameters. */
+int32_t ddp_router_route(ddp_router* router, int64_t tokens, const void* logits, int32_t dtype, int64_t stride, const float* bias,
+                         int32_t* experts_out, void* weights, int32_t weights_dtype, int32_t* counts, int32_t accumulate);
+
+/* dlogits (of dtype) from the gradient of the weights, for the choice that experts_in holds (indices outside [0, experts) take no part;
+ * a token without any gets zeros).  The bias has no gradient.  dlogits may be logits (address and stride). */
+int32_t ddp_router_grad(ddp_router* router, int64_t tokens, const void* logits, int32_t dtype, int64_t stride, const int32_t* experts_in,
+                        const void* dweights, int32_t dweights_dtype, void* dlogits, int64_t dlogits_stride);
+
+/* bias_out[e] = bias[e] + rate where the replicas' counts ([replicas][experts]) of an expert sum to less than the mean over the experts,
+ * - rate where to more, as it is at the mean.  bias_out may be bias. */
+int32_t ddp_router_balance(ddp_router* router, int32_t replicas, const int32_t* counts, float rate, const float* bias, float* bias_out);
+
 /* Library version string. */
 const char* ddp_version(void);
 

@@ -45,6 +45,7 @@ DDP_STAT_REPAIRED_LAUNCHES, DDP_STAT_EARLY_LAUNCHES = 100, 101
 DDP_PIPELINE_STAGED, DDP_PIPELINE_FUSED = 0, 1
 DDP_STATIC_SCRATCH_BYTES = 32 << 20
 DDP_STATE_FP32, DDP_STATE_8BIT = 0, 1
+DDP_SCORE_SOFTMAX, DDP_SCORE_SIGMOID = 0, 1
 DDP_K_PACK, DDP_K_REDUCE, DDP_K_UNPACK, DDP_K_ACCUMULATE, DDP_K_ITERATION = 0, 1, 2, 3, 4
 
 EXPORTS = [
@@ -61,6 +62,12 @@ EXPORTS = [
     "ddp_opt_read_state",
     "ddp_embedding_create", "ddp_embedding_destroy", "ddp_embedding_last_error", "ddp_embedding_lookup",
     "ddp_embedding_grad",
+    "ddp_layernorm_create", "ddp_layernorm_destroy", "ddp_layernorm_last_error", "ddp_layernorm_forward",
+    "ddp_layernorm_backward",
+    "ddp_position_bias_create", "ddp_position_bias_destroy", "ddp_position_bias_last_error", "ddp_position_bias_buckets",
+    "ddp_position_bias_apply", "ddp_position_bias_grad",
+    "ddp_router_create", "ddp_router_destroy", "ddp_router_last_error", "ddp_router_route", "ddp_router_grad",
+    "ddp_router_balance",
 ]
 
 
@@ -142,6 +149,29 @@ _lib.ddp_embedding_create.argtypes = [C.POINTER(_vp), _i32, _vp, _i64, _i64, _i6
 _lib.ddp_embedding_destroy.argtypes = [_vp]
 _lib.ddp_embedding_lookup.argtypes = [_vp, _i64, _vp, _i32, _vp, _i32, _i64, _f32, _vp, _i32, _i64]
 _lib.ddp_embedding_grad.argtypes = [_vp, _i64, _vp, _i32, _vp, _i32, _i64, _f32, _i64, _i32, _vp, _i32, _i64]
+_lib.ddp_layernorm_last_error.restype = C.c_char_p
+_lib.ddp_layernorm_last_error.argtypes = [_vp]
+_lib.ddp_layernorm_create.argtypes = [C.POINTER(_vp), _i32, _vp, _i64]
+_lib.ddp_layernorm_destroy.argtypes = [_vp]
+_lib.ddp_layernorm_forward.argtypes = [_vp, _i64, _vp, _i32, _i64, _vp, _i64, _vp, _vp, _i32, _f32, _vp, _i64, _vp, _i32, _i64, _vp, _vp]
+_lib.ddp_layernorm_backward.argtypes = [_vp, _i64, _vp, _i32, _i64, _vp, _i32, _i64, _vp, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _i32,
+                                        _vp, _vp, _i32]
+_lib.ddp_position_bias_last_error.restype = C.c_char_p
+_lib.ddp_position_bias_last_error.argtypes = [_vp]
+_lib.ddp_position_bias_create.argtypes = [C.POINTER(_vp), _i32, _vp, _i32, _i32, _i32, _i64, _i32]
+_lib.ddp_position_bias_destroy.argtypes = [_vp]
+_lib.ddp_position_bias_buckets.argtypes = [_vp, C.POINTER(_i32)]
+_lib.ddp_position_bias_apply.argtypes = [_vp, _i64, _i64, _i64, _i64, _vp, _i32, _i64, _f32, _vp, _i32, _f32, _i32, _vp, _i32, _i64,
+                                         _i64, _i64]
+_lib.ddp_position_bias_grad.argtypes = [_vp, _i64, _i64, _i64, _i64, _vp, _i32, _i64, _i64, _i64, _f32, _vp, _vp, _i32, _i32, _vp, _i32,
+                                        _i64]
+_lib.ddp_router_last_error.restype = C.c_char_p
+_lib.ddp_router_last_error.argtypes = [_vp]
+_lib.ddp_router_create.argtypes = [C.POINTER(_vp), _i32, _vp] + [_i32] * 7 + [_f32]
+_lib.ddp_router_destroy.argtypes = [_vp]
+_lib.ddp_router_route.argtypes = [_vp, _i64, _vp, _i32, _i64, _vp, _vp, _vp, _i32, _vp, _i32]
+_lib.ddp_router_grad.argtypes = [_vp, _i64, _vp, _i32, _i64, _vp, _vp, _i32, _vp, _i64]
+_lib.ddp_router_balance.argtypes = [_vp, _i32, _vp, _f32, _vp, _vp]
 for _name in EXPORTS:
     if not _name.endswith("_last_error") and _name != "ddp_version":
         getattr(_lib, _name).restype = _i32
@@ -569,3 +599,130 @@ def ddp_embedding_grad(emb, tokens: int, ids: int, id_bits: int, dout: int, dout
                                          1 if accumulate else 0, _pointer(grad), _index(grad_dtype), _index(grad_stride))
     if status < 0:
         _check_embedding(emb, status)
+
+
+# ---- inside a layer: norm, relative position bias, routing to experts ----
+# (addresses are ints, 0 or None: NULL; binding checks as for the embedding)
+
+def _check_layer(last_error, handle, status: int) -> int:
+    if status < 0:
+        raise DdpError(status, last_error(handle))
+    return status
+
+
+def ddp_layernorm_last_error(norm) -> str:
+    msg = _lib.ddp_layernorm_last_error(norm)
+    return msg.decode() if msg else ""
+
+
+def ddp_layernorm_create(device: int, stream: int, width: int):
+    """Returns the opaque handle."""
+    handle = _vp()
+    _check_layer(ddp_layernorm_last_error, None, _lib.ddp_layernorm_create(C.byref(handle), device, _vp(stream or None), width))
+    return handle
+
+
+def ddp_layernorm_destroy(norm) -> None:
+    _check_layer(ddp_layernorm_last_error, None, _lib.ddp_layernorm_destroy(norm))
+
+
+def ddp_layernorm_forward(norm, rows: int, x: int, x_dtype: int, x_stride: int, residual: int, residual_stride: int, gamma: int, beta: int,
+                          param_dtype: int, eps: float, sum_: int, sum_stride: int, y: int, y_dtype: int, y_stride: int, mean: int = 0,
+                          rstd: int = 0) -> None:
+    status = _lib.ddp_layernorm_forward(norm, _index(rows), _pointer(x), _index(x_dtype), _index(x_stride), _pointer(residual),
+                                        _index(residual_stride), _pointer(gamma), _pointer(beta), _index(param_dtype), float(eps),
+                                        _pointer(sum_), _index(sum_stride), _pointer(y), _index(y_dtype), _index(y_stride),
+                                        _pointer(mean), _pointer(rstd))
+    _check_layer(ddp_layernorm_last_error, norm, status)
+
+
+def ddp_layernorm_backward(norm, rows: int, dy: int, dy_dtype: int, dy_stride: int, x: int, x_dtype: int, x_stride: int, mean: int, rstd: int,
+                           gamma: int, param_dtype: int, dsum: int, dsum_stride: int, dx: int, dx_stride: int, accumulate: bool,
+                           dgamma: int, dbeta: int, grad_dtype: int) -> None:
+    status = _lib.ddp_layernorm_backward(norm, _index(rows), _pointer(dy), _index(dy_dtype), _index(dy_stride), _pointer(x),
+                                         _index(x_dtype), _index(x_stride), _pointer(mean), _pointer(rstd), _pointer(gamma),
+                                         _index(param_dtype), _pointer(dsum), _index(dsum_stride), _pointer(dx), _index(dx_stride),
+                                         1 if accumulate else 0, _pointer(dgamma), _pointer(dbeta), _index(grad_dtype))
+    _check_layer(ddp_layernorm_last_error, norm, status)
+
+
+def ddp_position_bias_last_error(bias) -> str:
+    msg = _lib.ddp_position_bias_last_error(bias)
+    return msg.decode() if msg else ""
+
+
+def ddp_position_bias_create(device: int, stream: int, heads: int, buckets: int, exact: int, max_distance: int, both: bool):
+    """Returns the opaque handle.  both: keys behind the query have buckets of their own."""
+    handle = _vp()
+    _check_layer(ddp_position_bias_last_error, None, _lib.ddp_position_bias_create(
+        C.byref(handle), device, _vp(stream or None), heads, buckets, exact, max_distance, 1 if both else 0))
+    return handle
+
+
+def ddp_position_bias_destroy(bias) -> None:
+    _check_layer(ddp_position_bias_last_error, None, _lib.ddp_position_bias_destroy(bias))
+
+
+def ddp_position_bias_buckets(bias) -> np.ndarray:
+    """The smallest distance of every bucket of one direction."""
+    first = np.zeros(1024, dtype=np.int32)
+    n = _check_layer(ddp_position_bias_last_error, bias, _lib.ddp_position_bias_buckets(bias, _as(first, _i32)))
+    return first[:n]
+
+
+def ddp_position_bias_apply(bias, batch: int, queries: int, keys: int, offset: int, table: int, table_dtype: int, table_stride: int,
+                            scale: float, key_lengths: int, causal: bool, masked: float, accumulate: bool, out: int, out_dtype: int,
+                            batch_stride: int, head_stride: int, query_stride: int) -> None:
+    status = _lib.ddp_position_bias_apply(bias, _index(batch), _index(queries), _index(keys), _index(offset), _pointer(table),
+                                          _index(table_dtype), _index(table_stride), float(scale), _pointer(key_lengths),
+                                          1 if causal else 0, float(masked), 1 if accumulate else 0, _pointer(out), _index(out_dtype),
+                                          _index(batch_stride), _index(head_stride), _index(query_stride))
+    _check_layer(ddp_position_bias_last_error, bias, status)
+
+
+def ddp_position_bias_grad(bias, batch: int, queries: int, keys: int, offset: int, dscores: int, dtype: int, batch_stride: int,
+                           head_stride: int, query_stride: int, scale: float, key_lengths: int, query_lengths: int, causal: bool,
+                           accumulate: bool, grad: int, grad_dtype: int, grad_stride: int) -> None:
+    status = _lib.ddp_position_bias_grad(bias, _index(batch), _index(queries), _index(keys), _index(offset), _pointer(dscores),
+                                         _index(dtype), _index(batch_stride), _index(head_stride), _index(query_stride), float(scale),
+                                         _pointer(key_lengths), _pointer(query_lengths), 1 if causal else 0, 1 if accumulate else 0,
+                                         _pointer(grad), _index(grad_dtype), _index(grad_stride))
+    _check_layer(ddp_position_bias_last_error, bias, status)
+
+
+def ddp_router_last_error(router) -> str:
+    msg = _lib.ddp_router_last_error(router)
+    return msg.decode() if msg else ""
+
+
+def ddp_router_create(device: int, stream: int, experts: int, chosen: int, groups: int = 1, kept: int = 1, top: int = 1,
+                      score: int = DDP_SCORE_SOFTMAX, renormalise: bool = True, scale: float = 1.0):
+    """Returns the opaque handle."""
+    handle = _vp()
+    _check_layer(ddp_router_last_error, None, _lib.ddp_router_create(C.byref(handle), device, _vp(stream or None), experts, chosen, groups,
+                                                                     kept, top, score, 1 if renormalise else 0, scale))
+    return handle
+
+
+def ddp_router_destroy(router) -> None:
+    _check_layer(ddp_router_last_error, None, _lib.ddp_router_destroy(router))
+
+
+def ddp_router_route(router, tokens: int, logits: int, dtype: int, stride: int, bias: int, experts_out: int, weights: int,
+                     weights_dtype: int, counts: int = 0, accumulate: bool = False) -> None:
+    status = _lib.ddp_router_route(router, _index(tokens), _pointer(logits), _index(dtype), _index(stride), _pointer(bias),
+                                   _pointer(experts_out), _pointer(weights), _index(weights_dtype), _pointer(counts),
+                                   1 if accumulate else 0)
+    _check_layer(ddp_router_last_error, router, status)
+
+
+def ddp_router_grad(router, tokens: int, logits: int, dtype: int, stride: int, experts_in: int, dweights: int, dweights_dtype: int,
+                    dlogits: int, dlogits_stride: int) -> None:
+    status = _lib.ddp_router_grad(router, _index(tokens), _pointer(logits), _index(dtype), _index(stride), _pointer(experts_in),
+                                  _pointer(dweights), _index(dweights_dtype), _pointer(dlogits), _index(dlogits_stride))
+    _check_layer(ddp_router_last_error, router, status)
+
+
+def ddp_router_balance(router, replicas: int, counts: int, rate: float, bias: int, bias_out: int) -> None:
+    status = _lib.ddp_router_balance(router, _index(replicas), _pointer(counts), float(rate), _pointer(bias), _pointer(bias_out))
+    _check_layer(ddp_router_last_error, router, status)

@@ -1,0 +1,387 @@
+// Layer norm over the last dimension with the residual sum in front of it, and its gradients.
+//
+//   s = x (+ residual),  xh = (s - mean) rstd,  y = xh gamma + beta
+//   g = dy gamma,  dx = (g - mean(g) - xh mean(g xh)) rstd (+ dsum)
+//   dgamma = sum over the rows of dy xh,  dbeta = sum over the rows of dy
+//
+// Bound by memory: a few operations an element.
+#include "layer_host.h"
+
+struct ddp_layernorm : ddp::LayerHandle {
+    int64_t width = 0;
+    int32_t chunks = 0;                          // row chunks that the workspace holds sums of
+    float* partial = nullptr;                    // [chunks][2][width]
+};
+
+namespace {
+
+using namespace ddp;
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int64_t kMaxWidth = int64_t(1) << 20, kMaxRows = INT32_MAX;
+
+struct ForwardArgs {
+    const char *x, *residual, *gamma, *beta;
+    char *sum, *y;
+    float *mean, *rstd;
+    int64_t rows, x_stride, residual_stride, sum_stride, y_stride;
+    int32_t width, param;
+    float eps;
+};
+struct BackwardArgs {
+    const char *dy, *x, *gamma, *dsum;
+    const float *mean, *rstd;
+    char *dx;
+    float* partial;
+    int64_t rows, dy_stride, x_stride, dsum_stride, dx_stride, rows_per_chunk;
+    int32_t width, param, chunks;
+};
+
+// gamma or beta: `none` where there is none.
+template <int N>
+__device__ __forceinline__ void load_param(const char* p, int type, int64_t at, int have, float none, float (&v)[N]) {
+    if (p == nullptr) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = none;
+    } else if (type == DDP_FP32) {
+        load_some<DDP_FP32, N>(p + at * 4, have, v);
+    } else if (type == DDP_FP16) {
+        load_some<DDP_FP16, N>(p + at * 2, have, v);
+    } else {
+        load_some<DDP_BF16, N>(p + at * 2, have, v);
+    }
+}
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+// Of all threads of a block, in all of them.
+__device__ __forceinline__ float block_sum(float x, float* part) {
+    x = wave_sum(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    float sum = part[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) sum += part[w];
+    return sum;
+}
+
+// A block a row, three passes over it (the second and third come from the caches).
+constexpr int kN = 4;
+template <int XT>
+__device__ __forceinline__ void load_sum(const ForwardArgs& a, int64_t row, int c, float (&s)[kN]) {
+    const int have = a.width - c;
+    load_some<XT, kN>(a.x + (row * a.x_stride + c) * ElemBytes<XT>::value, have, s);
+    if (a.residual != nullptr) {
+        float r[kN];
+        load_some<XT, kN>(a.residual + (row * a.residual_stride + c) * ElemBytes<XT>::value, have, r);
+#pragma unroll
+        for (int i = 0; i < kN; ++i) s[i] += r[i];
+    }
+}
+template <int XT, int YT>
+__global__ __launch_bounds__(kThreads) void forward_kernel(ForwardArgs a) {
+    __shared__ float part[kWaves];
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        float sum = 0.0f;
+        for (int c = threadIdx.x * kN; c < a.width; c += kThreads * kN) {
+            float s[kN];
+            load_sum<XT>(a, row, c, s);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) sum += s[i];
+        }
+        const float mean = block_sum(sum, part) / a.width;
+        float squares = 0.0f;
+        for (int c = threadIdx.x * kN; c < a.width; c += kThreads * kN) {
+            float s[kN];
+            load_sum<XT>(a, row, c, s);
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (c + i < a.width) squares += (s[i] - mean) * (s[i] - mean);
+        }
+        const float rstd = 1.0f / sqrtf(block_sum(squares, part) / a.width + a.eps);
+        for (int c = threadIdx.x * kN; c < a.width; c += kThreads * kN) {
+            const int have = a.width - c;
+            float s[kN], g[kN], b[kN];
+            load_sum<XT>(a, row, c, s);
+            load_param<kN>(a.gamma, a.param, c, have, 1.0f, g);
+            load_param<kN>(a.beta, a.param, c, have, 0.0f, b);
+            if (a.sum != nullptr) store_some<XT, kN>(a.sum + (row * a.sum_stride + c) * ElemBytes<XT>::value, have, s);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) s[i] = (s[i] - mean) * rstd * g[i] + b[i];
+            store_some<YT, kN>(a.y + (row * a.y_stride + c) * ElemBytes<YT>::value, have, s);
+        }
+        if (threadIdx.x == 0) {
+            if (a.mean != nullptr) a.mean[row] = mean;
+            if (a.rstd != nullptr) a.rstd[row] = rstd;
+        }
+    }
+}
+
+template <int XT, int YT>
+__device__ __forceinline__ void load_pair(const BackwardArgs& a, int64_t row, int c, float mean, float rstd, float (&dy)[kN], float (&xh)[kN]) {
+    const int have = a.width - c;
+    load_some<YT, kN>(a.dy + (row * a.dy_stride + c) * ElemBytes<YT>::value, have, dy);
+    load_some<XT, kN>(a.x + (row * a.x_stride + c) * ElemBytes<XT>::value, have, xh);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) xh[i] = (xh[i] - mean) * rstd;
+}
+template <int XT, int YT>
+__global__ __launch_bounds__(kThreads) void backward_rows_kernel(BackwardArgs a) {
+    __shared__ float part[kWaves];
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float of_g = 0.0f, of_gx = 0.0f;
+        for (int c = threadIdx.x * kN; c < a.width; c += kThreads * kN) {
+            float dy[kN], xh[kN], gamma[kN];
+            load_pair<XT, YT>(a, row, c, mean, rstd, dy, xh);
+            load_param<kN>(a.gamma, a.param, c, a.width - c, 1.0f, gamma);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                if (c + i >= a.width) continue;
+                of_g += dy[i] * gamma[i];
+                of_gx += dy[i] * gamma[i] * xh[i];
+            }
+        }
+        const float c1 = block_sum(of_g, part) / a.width, c2 = block_sum(of_gx, part) / a.width;
+        for (int c = threadIdx.x * kN; c < a.width; c += kThreads * kN) {
+            const int have = a.width - c;
+            float dy[kN], xh[kN], gamma[kN], more[kN] = {};
+            load_pair<XT, YT>(a, row, c, mean, rstd, dy, xh);
+            load_param<kN>(a.gamma, a.param, c, have, 1.0f, gamma);
+            if (a.dsum != nullptr) load_some<XT, kN>(a.dsum + (row * a.dsum_stride + c) * ElemBytes<XT>::value, have, more);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) dy[i] = (dy[i] * gamma[i] - c1 - xh[i] * c2) * rstd + more[i];
+            store_some<XT, kN>(a.dx + (row * a.dx_stride + c) * ElemBytes<XT>::value, have, dy);
+        }
+    }
+}
+
+// A block has 64 kN columns and a chunk of the rows, which go round its waves.
+template <int XT, int YT>
+__global__ __launch_bounds__(kThreads) void backward_columns_kernel(BackwardArgs a) {
+    __shared__ float part[kWaves][2][64 * kN];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = (blockIdx.x * 64 + lane) * kN;
+    const int64_t from = blockIdx.y * a.rows_per_chunk, to = min(from + a.rows_per_chunk, a.rows);
+    float dgamma[kN] = {}, dbeta[kN] = {};
+    if (c < a.width) {
+        for (int64_t row = from + wave; row < to; row += kWaves) {
+            float dy[kN], xh[kN];
+            load_pair<XT, YT>(a, row, c, a.mean[row], a.rstd[row], dy, xh);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                dgamma[i] += dy[i] * xh[i];
+                dbeta[i] += dy[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        part[wave][0][i * 64 + lane] = dgamma[i];
+        part[wave][1][i * 64 + lane] = dbeta[i];
+    }
+    __syncthreads();
+    if (wave >= 2 || c >= a.width) return;           // wave 0 has dgamma, wave 1 dbeta
+    float* to_part = a.partial + (static_cast<int64_t>(blockIdx.y) * 2 + wave) * a.width;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += part[w][wave][i * 64 + lane];
+        if (c + i < a.width) to_part[c + i] = sum;
+    }
+}
+
+struct JoinArgs {
+    const float* partial;
+    char *dgamma, *dbeta;
+    int32_t width, chunks, grad, add;
+};
+// blockIdx.y: dgamma, dbeta.  A thread a column.
+__global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a) {
+    char* out = blockIdx.y == 0 ? a.dgamma : a.dbeta;
+    const int c = blockIdx.x * kThreads + threadIdx.x;
+    if (out == nullptr || c >= a.width) return;
+    float sum = 0.0f;
+    for (int k = 0; k < a.chunks; ++k) sum += a.partial[(static_cast<int64_t>(k) * 2 + blockIdx.y) * a.width + c];
+    if (a.grad == DDP_FP32) {
+        float* to = reinterpret_cast<float*>(out) + c;
+        *to = a.add ? *to + sum : sum;
+    } else if (a.grad == DDP_FP16) {
+        store_one<DDP_FP16>(out + 2 * static_cast<int64_t>(c), a.add ? load_one<DDP_FP16>(out + 2 * static_cast<int64_t>(c)) + sum : sum);
+    } else {
+        store_one<DDP_BF16>(out + 2 * static_cast<int64_t>(c), a.add ? load_one<DDP_BF16>(out + 2 * static_cast<int64_t>(c)) + sum : sum);
+    }
+}
+
+// ---- host ----
+
+constexpr int kRowBlocks = 1 << 16;
+
+template <int XT, int YT>
+hipError_t launch_forward(ddp_layernorm* h, const ForwardArgs& a) {
+    hipLaunchKernelGGL((forward_kernel<XT, YT>), dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kRowBlocks))), dim3(kThreads), 0, h->stream, a);
+    return hipGetLastError();
+}
+template <int XT, int YT>
+hipError_t launch_backward(ddp_layernorm* h, const BackwardArgs& a, bool params) {
+    if (a.dx != nullptr) {
+        hipLaunchKernelGGL((backward_rows_kernel<XT, YT>), dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kRowBlocks))), dim3(kThreads), 0, h->stream, a);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
+    if (!params) return hipSuccess;
+    hipLaunchKernelGGL((backward_columns_kernel<XT, YT>), dim3(static_cast<unsigned>((a.width + 64 * kN - 1) / (64 * kN)), static_cast<unsigned>(a.chunks)),
+                       dim3(kThreads), 0, h->stream, a);
+    return hipGetLastError();
+}
+
+// y has x's type, or any where x is binary32.
+bool known_pair(int xt, int yt) { return xt == DDP_FP32 || xt == yt; }
+template <typename F>
+auto with_types(int xt, int yt, F f) {
+    if (xt == DDP_FP16) return f(std::integral_constant<int, DDP_FP16>(), std::integral_constant<int, DDP_FP16>());
+    if (xt == DDP_BF16) return f(std::integral_constant<int, DDP_BF16>(), std::integral_constant<int, DDP_BF16>());
+    if (yt == DDP_FP32) return f(std::integral_constant<int, DDP_FP32>(), std::integral_constant<int, DDP_FP32>());
+    if (yt == DDP_FP16) return f(std::integral_constant<int, DDP_FP32>(), std::integral_constant<int, DDP_FP16>());
+    return f(std::integral_constant<int, DDP_FP32>(), std::integral_constant<int, DDP_BF16>());
+}
+
+int32_t check_rows(ddp_layernorm* h, int64_t rows, int x_dtype, int y_dtype, int param_dtype) {
+    if (rows < 0 || rows > kMaxRows) return layer_fail(h, DDP_ERR_ARG, "layer norm: rows outside [0, 2^31 - 1]");
+    if (!known_dtype(x_dtype) || !known_dtype(y_dtype) || !known_dtype(param_dtype)) return layer_fail(h, DDP_ERR_ARG, "layer norm: unknown dtype");
+    if (!known_pair(x_dtype, y_dtype)) return layer_fail(h, DDP_ERR_UNSUPPORTED, "layer norm: y of another 16-bit type than x, or binary32 for 16-bit x");
+    return DDP_OK;
+}
+bool bad_stride(const ddp_layernorm* h, const void* p, int64_t stride) { return p && (stride < h->width || stride > INT32_MAX); }
+
+}  // namespace
+
+extern "C" {
+
+const char* ddp_layernorm_last_error(const ddp_layernorm* h) { return h ? h->err.c_str() : ddp_last_error(nullptr); }
+
+int32_t ddp_layernorm_create(ddp_layernorm** out, int32_t device, void* stream, int64_t width) {
+    if (!out) return layer_fail(nullptr, DDP_ERR_ARG, "ddp_layernorm_create: out is null");
+    *out = nullptr;
+    const int32_t status = layer_device("ddp_layernorm_create: bad device", device);
+    if (status != DDP_OK) return status;
+    if (width < 1) return layer_fail(nullptr, DDP_ERR_ARG, "ddp_layernorm_create: the width is at least 1");
+    if (width > kMaxWidth) return layer_fail(nullptr, DDP_ERR_UNSUPPORTED, "ddp_layernorm_create: more than 2^20 columns");
+    ddp_layernorm* h = new (std::nothrow) ddp_layernorm();
+    if (!h) return layer_fail(nullptr, DDP_ERR_HIP, "out of host memory");
+    h->device = device;
+    h->stream = static_cast<hipStream_t>(stream);
+    h->width = width;
+    h->chunks = static_cast<int32_t>(std::max<int64_t>(16, std::min<int64_t>(512, (int64_t(1) << 21) / width)));
+    if (device != DDP_DEVICE_NONE) {
+        const hipError_t err = layer_alloc(h, static_cast<int64_t>(h->chunks) * 2 * width * 4);
+        if (err != hipSuccess) {
+            delete h;
+            return layer_fail(nullptr, DDP_ERR_HIP, hipGetErrorString(err));
+        }
+        h->partial = reinterpret_cast<float*>(h->mem);
+    }
+    *out = h;
+    return DDP_OK;
+}
+
+int32_t ddp_layernorm_destroy(ddp_layernorm* h) {
+    if (!h) return DDP_ERR_ARG;
+    layer_release(h);
+    delete h;
+    return DDP_OK;
+}
+
+int32_t ddp_layernorm_forward(ddp_layernorm* h, int64_t rows, const void* x, int32_t x_dtype, int64_t x_stride, const void* residual,
+                              int64_t residual_stride, const void* gamma, const void* beta, int32_t param_dtype, float eps, void* sum,
+                              int64_t sum_stride, void* y, int32_t y_dtype, int64_t y_stride, float* mean, float* rstd) {
+    if (!h) return DDP_ERR_ARG;
+    const int32_t status = check_rows(h, rows, x_dtype, y_dtype, param_dtype);
+    if (status != DDP_OK) return status;
+    if (!(eps >= 0.0f)) return layer_fail(h, DDP_ERR_ARG, "ddp_layernorm_forward: eps below 0 or not a number");
+    if (x_stride < h->width || x_stride > INT32_MAX || y_stride < h->width || y_stride > INT32_MAX || bad_stride(h, residual, residual_stride) ||
+        bad_stride(h, sum, sum_stride))
+        return layer_fail(h, DDP_ERR_ARG, "ddp_layernorm_forward: a stride is below the width (or above 2^31 - 1)");
+    if (rows > 0 && (!x || !y)) return layer_fail(h, DDP_ERR_ARG, "ddp_layernorm_forward: null pointer");
+    const int xs = elem_bytes(x_dtype), ps = elem_bytes(param_dtype);
+    if (misaligned(x, xs) || misaligned(residual, xs) || misaligned(sum, xs) || misaligned(y, elem_bytes(y_dtype)) || misaligned(gamma, ps) ||
+        misaligned(beta, ps) || misaligned(mean, 4) || misaligned(rstd, 4))
+        return layer_fail(h, DDP_ERR_ARG, "ddp_layernorm_forward: pointer not aligned to its element size");
+    if (h->device == DDP_DEVICE_NONE) return layer_fail(h, DDP_ERR_NO_DEVICE, "ddp_layernorm_forward without a device");
+    if (rows == 0) return DDP_OK;
+    OnDevice on(h->device);
+    LAYER_HIP(h, on.err);
+    ForwardArgs a{};
+    a.x = static_cast<const char*>(x);
+    a.residual = static_cast<const char*>(residual);
+    a.gamma = static_cast<const char*>(gamma);
+    a.beta = static_cast<const char*>(beta);
+    a.sum = static_cast<char*>(sum);
+    a.y = static_cast<char*>(y);
+    a.mean = mean;
+    a.rstd = rstd;
+    a.rows = rows;
+    a.x_stride = x_stride;
+    a.residual_stride = residual_stride;
+    a.sum_stride = sum_stride;
+    a.y_stride = y_stride;
+    a.width = static_cast<int32_t>(h->width);
+    a.param = param_dtype;
+    a.eps = eps;
+    LAYER_HIP(h, with_types(x_dtype, y_dtype, [&](auto xt, auto yt) { return launch_forward<xt.value, yt.value>(h, a); }));
+    return DDP_OK;
+}
+
+int32_t ddp_layernorm_backward(ddp_layernorm* h, int64_t rows, const void* dy, int32_t dy_dtype, int64_t dy_stride, const void* x, int32_t x_dtype,
+                               int64_t x_stride, const float* mean, const float* rstd, const void* gamma, int32_t param_dtype, const void* dsum,
+                               int64_t dsum_stride, void* dx, int64_t dx_stride, int32_t accumulate, void* dgamma, void* dbeta, int32_t grad_dtype) {
+    if (!h) return DDP_ERR_ARG;
+    const int32_t status = check_rows(h, rows, x_dtype, dy_dtype, param_dtype);
+    if (status != DDP_OK) return status;
+    if (!known_dtype(grad_dtype)) return layer_fail(h, DDP_ERR_ARG, "ddp_layernorm_backward: unknown dtype");
+    if (dy_stride < h->width || dy_stride > INT32_MAX || x_stride < h->width || x_stride > INT32_MAX || bad_stride(h, dsum, dsum_stride) ||
+        bad_stride(h, dx, dx_stride))
+        return layer_fail(h, DDP_ERR_ARG, "ddp_layernorm_backward: a stride is below the width (or above 2^31 - 1)");
+    if (rows > 0 && (!dy || !x || !mean || !rstd)) return layer_fail(h, DDP_ERR_ARG, "ddp_layernorm_backward: null pointer");
+    const int xs = elem_bytes(x_dtype), gs = elem_bytes(grad_dtype);
+    if (misaligned(dy, elem_bytes(dy_dtype)) || misaligned(x, xs) || misaligned(dsum, xs) || misaligned(dx, xs) || misaligned(gamma, elem_bytes(param_dtype)) ||
+        misaligned(mean, 4) || misaligned(rstd, 4) || misaligned(dgamma, gs) || misaligned(dbeta, gs))
+        return layer_fail(h, DDP_ERR_ARG, "ddp_layernorm_backward: pointer not aligned to its element size");
+    if (h->device == DDP_DEVICE_NONE) return layer_fail(h, DDP_ERR_NO_DEVICE, "ddp_layernorm_backward without a device");
+    const bool params = dgamma || dbeta;
+    if ((rows == 0 || !dx) && (!params || (rows == 0 && accumulate))) return DDP_OK;
+    OnDevice on(h->device);
+    LAYER_HIP(h, on.err);
+    BackwardArgs a{};
+    a.dy = static_cast<const char*>(dy);
+    a.x = static_cast<const char*>(x);
+    a.gamma = static_cast<const char*>(gamma);
+    a.dsum = static_cast<const char*>(dsum);
+    a.mean = mean;
+    a.rstd = rstd;
+    a.dx = static_cast<char*>(dx);
+    a.partial = h->partial;
+    a.rows = rows;
+    a.dy_stride = dy_stride;
+    a.x_stride = x_stride;
+    a.dsum_stride = dsum_stride;
+    a.dx_stride = dx_stride;
+    a.rows_per_chunk = std::max<int64_t>(64, (rows + h->chunks - 1) / h->chunks);
+    a.chunks = static_cast<int32_t>((rows + a.rows_per_chunk - 1) / a.rows_per_chunk);
+    a.width = static_cast<int32_t>(h->width);
+    a.param = param_dtype;
+    if (rows > 0)
+        LAYER_HIP(h, with_types(x_dtype, dy_dtype, [&](auto xt, auto yt) { return launch_backward<xt.value, yt.value>(h, a, params); }));
+    if (!params) return DDP_OK;
+    JoinArgs j{h->partial, static_cast<char*>(dgamma), static_cast<char*>(dbeta), a.width, a.chunks, grad_dtype, accumulate != 0};
+    hipLaunchKernelGGL(join_kernel, dim3(static_cast<unsigned>((a.width + kThreads - 1) / kThreads), 2), dim3(kThreads), 0, h->stream, j);
+    LAYER_HIP(h, hipGetLastError());
+    return DDP_OK;
+}
+
+}  // extern "C"

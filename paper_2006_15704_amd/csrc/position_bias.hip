@@ -1,0 +1,376 @@
+// Learned relative position bias by buckets, and its gradient.
+//
+//   r = key position - query position = j - i - offset
+//   f(d) = d for d < exact, else min(n - 1, exact + floor((n - exact) log(d / exact) / log(distance / exact)))
+//   bucket(r) = f(max(-r, 0)) with n = buckets, or with both directions n = buckets / 2: f(|r|), + n for r > 0
+//   out[b, h, i, j]  = scale table[bucket(j - i - offset)][h]  (+ what is there)
+//   grad[k][h]       = scale (sum of dscores[b, h, i, j] over the visible places of bucket k)  (+ what is there)
+//
+// A bias depends on the diagonal alone: forward is a fill, backward a sum along diagonals.  Both are bound by memory.
+#include "layer_host.h"
+
+#include <cmath>
+#include <vector>
+
+struct ddp_position_bias : ddp::LayerHandle {
+    int32_t heads = 0, buckets = 0, exact = 0, both = 0, sides = 0;      // sides: buckets of one direction
+    int64_t distance = 0;
+    int32_t parts = 0;                           // of the gradient that the workspace holds
+    int32_t* first = nullptr;                    // [sides] the smallest distance of each bucket
+    float* partial = nullptr;                    // [parts][heads][buckets]
+    std::vector<int32_t> first_host;
+};
+
+namespace {
+
+using namespace ddp;
+
+constexpr int kThreads = 256;
+constexpr int kMaxBuckets = 1024, kMaxHeads = 4096;
+constexpr int64_t kMaxDistance = int64_t(1) << 20, kMaxLength = int64_t(1) << 24, kMaxBatch = int64_t(1) << 20;
+
+// Whole numbers of any size: what a logarithm's step at exactly a whole distance takes to be settled.
+struct Big {
+    std::vector<uint32_t> w{1};
+    void times(uint32_t x) {
+        uint64_t carry = 0;
+        for (uint32_t& d : w) {
+            carry += static_cast<uint64_t>(d) * x;
+            d = static_cast<uint32_t>(carry);
+            carry >>= 32;
+        }
+        if (carry) w.push_back(static_cast<uint32_t>(carry));
+    }
+    void times_power(uint32_t x, int n) {
+        for (int i = 0; i < n; ++i) times(x);
+    }
+    bool at_least(const Big& o) const {
+        if (w.size() != o.w.size()) return w.size() > o.w.size();
+        for (size_t i = w.size(); i-- > 0;)
+            if (w[i] != o.w[i]) return w[i] > o.w[i];
+        return true;
+    }
+};
+
+// The smallest whole d with m log(d / e) / log(far / e) >= t, that is d^m >= e^(m - t) far^t.  Where the root is not near a whole
+// number its rounding decides nothing; where it is, the powers are compared.
+int32_t first_distance(int32_t e, int64_t far, int t, int m) {
+    if (t == 0) return e;
+    const long double root = e * std::pow(static_cast<long double>(far) / e, static_cast<long double>(t) / m);
+    const long double near = std::floor(root + 0.5L);
+    if (std::fabs(root - near) > 1e-10L * root) return static_cast<int32_t>(std::ceil(root));
+    Big d, want;
+    d.times_power(static_cast<uint32_t>(near), m);
+    want.times_power(static_cast<uint32_t>(e), m - t);
+    want.times_power(static_cast<uint32_t>(far), t);
+    return static_cast<int32_t>(near) + (d.at_least(want) ? 0 : 1);
+}
+
+struct BiasArgs {
+    const int32_t *first, *key_lengths, *query_lengths;
+    const char* table;
+    char* scores;                                // dscores in the gradient
+    float* partial;
+    int64_t batch, queries, keys, offset, table_stride, s_batch, s_head, s_query, rows_per_part;
+    int32_t heads, buckets, sides, both, causal, add, strips, row_parts;
+    float scale, masked;
+};
+
+__device__ __forceinline__ int bucket_of(const int32_t* first, const BiasArgs& a, int64_t r) {
+    const int64_t d = a.both ? (r < 0 ? -r : r) : (r < 0 ? -r : 0);
+    int lo = 0, hi = a.sides;                        // first[lo] <= d < first[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= d) lo = mid;
+        else hi = mid;
+    }
+    return lo + (a.both && r > 0 ? a.sides : 0);
+}
+__device__ __forceinline__ int64_t length_of(const int32_t* lengths, int64_t b, int64_t most) {
+    if (lengths == nullptr) return most;
+    const int64_t n = lengths[b];
+    return n < 0 ? 0 : n < most ? n : most;
+}
+
+// A block a row of the scores, one element a thread.
+template <int TT, int OT>
+__global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
+    __shared__ int32_t first[kMaxBuckets];
+    for (int k = threadIdx.x; k < a.sides; k += kThreads) first[k] = a.first[k];
+    __syncthreads();
+    const int64_t rows = a.batch * a.heads * a.queries;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const int64_t i = row % a.queries, h = row / a.queries % a.heads, b = row / a.queries / a.heads;
+        const int64_t keys = length_of(a.key_lengths, b, a.keys);
+        char* out = a.scores + (b * a.s_batch + h * a.s_head + i * a.s_query) * ElemBytes<OT>::value;
+        for (int64_t j = threadIdx.x; j < a.keys; j += kThreads) {
+            const int64_t r = j - i - a.offset;
+            char* to = out + j * ElemBytes<OT>::value;
+            float x = a.masked;
+            if (j < keys && !(a.causal && r > 0)) {
+                x = load_one<TT>(a.table + (bucket_of(first, a, r) * a.table_stride + h) * ElemBytes<TT>::value) * a.scale;
+                if (a.add) x += load_one<OT>(to);
+            }
+            store_one<OT>(to, x);
+        }
+    }
+}
+
+// A block has kThreads diagonals of one head, and a part of the rows of all sequences: a thread a diagonal, then a thread a bucket.
+template <int ST>
+__global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
+    __shared__ int32_t first[kMaxBuckets];
+    __shared__ float sums[kThreads];
+    __shared__ int of[kThreads];
+    for (int k = threadIdx.x; k < a.sides; k += kThreads) first[k] = a.first[k];
+    __syncthreads();
+    const int64_t h = blockIdx.y;
+    const int strip = blockIdx.x % a.strips, part = blockIdx.x / a.strips;
+    const int64_t diagonal = static_cast<int64_t>(strip) * kThreads + threadIdx.x - (a.queries - 1);      // j - i
+    const int64_t from = part * a.rows_per_part, to = min(from + a.rows_per_part, a.queries);
+    float sum = 0.0f;
+    if (diagonal < a.keys && !(a.causal && diagonal > a.offset)) {
+        for (int64_t b = 0; b < a.batch; ++b) {
+            const int64_t keys = length_of(a.key_lengths, b, a.keys), queries = length_of(a.query_lengths, b, a.queries);
+            const char* s = a.scores + (b * a.s_batch + h * a.s_head) * ElemBytes<ST>::value;
+            for (int64_t i = max(from, -diagonal); i < to && i < queries && i + diagonal < keys; ++i)
+                sum += load_one<ST>(s + (i * a.s_query + i + diagonal) * ElemBytes<ST>::value);
+        }
+    }
+    sums[threadIdx.x] = sum;
+    of[threadIdx.x] = diagonal < a.keys ? bucket_of(first, a, diagonal - a.offset) : -1;
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.buckets; k += kThreads) {
+        double total = 0.0;
+        for (int d = 0; d < kThreads; ++d)
+            if (of[d] == k) total += sums[d];
+        a.partial[(static_cast<int64_t>(blockIdx.x) * a.heads + h) * a.buckets + k] = static_cast<float>(total);
+    }
+}
+
+struct JoinArgs {
+    const float* partial;
+    char* grad;
+    int64_t grad_stride;
+    int32_t parts, heads, buckets, type, add;
+    float scale;
+};
+__global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a) {
+    const int at = blockIdx.x * kThreads + threadIdx.x;
+    if (at >= a.heads * a.buckets) return;
+    const int h = at / a.buckets, k = at % a.buckets;
+    double sum = 0.0;
+    for (int p = 0; p < a.parts; ++p) sum += a.partial[static_cast<int64_t>(p) * a.heads * a.buckets + at];
+    sum *= a.scale;
+    char* to = a.grad + (k * a.grad_stride + h) * (a.type == DDP_FP32 ? 4 : 2);
+    if (a.type == DDP_FP32) store_one<DDP_FP32>(to, static_cast<float>(a.add ? sum + load_one<DDP_FP32>(to) : sum));
+    else if (a.type == DDP_FP16) store_one<DDP_FP16>(to, static_cast<float>(a.add ? sum + load_one<DDP_FP16>(to) : sum));
+    else store_one<DDP_BF16>(to, static_cast<float>(a.add ? sum + load_one<DDP_BF16>(to) : sum));
+}
+
+// ---- host ----
+
+constexpr int64_t kRowBlocks = int64_t(1) << 20;
+constexpr int64_t kPartBytes = int64_t(1) << 24;     // of the workspace, if 64 parts do not take more
+
+template <int TT>
+hipError_t launch_apply(ddp_position_bias* h, const BiasArgs& a, int out) {
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(a.batch * a.heads * a.queries, kRowBlocks));
+    if (out == DDP_FP32) hipLaunchKernelGGL((apply_kernel<TT, DDP_FP32>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
+    else if (out == DDP_FP16) hipLaunchKernelGGL((apply_kernel<TT, DDP_FP16>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
+    else hipLaunchKernelGGL((apply_kernel<TT, DDP_BF16>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
+    return hipGetLastError();
+}
+
+bool out_of_reach(int64_t n, int64_t stride) { return n > 1 && stride > (int64_t(1) << 46) / (n - 1); }
+
+int32_t check_shape(ddp_position_bias* h, int64_t batch, int64_t queries, int64_t keys, int64_t offset, int32_t dtype, int32_t table_dtype,
+                    int64_t table_stride) {
+    if (batch < 0 || queries < 0 || keys < 0) return layer_fail(h, DDP_ERR_ARG, "position bias: batch, queries and keys are at least 0");
+    if (batch > kMaxBatch || queries > kMaxLength || keys > kMaxLength || offset > kMaxLength || offset < -kMaxLength)
+        return layer_fail(h, DDP_ERR_UNSUPPORTED, "position bias: more than 2^20 sequences, 2^24 queries or keys, or an offset beyond them");
+    if (!known_dtype(dtype) || !known_dtype(table_dtype)) return layer_fail(h, DDP_ERR_ARG, "position bias: unknown dtype");
+    if (table_stride < h->heads || table_stride > INT32_MAX) return layer_fail(h, DDP_ERR_ARG, "position bias: the table's stride is below the number of heads (or above 2^31 - 1)");
+    return DDP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+const char* ddp_position_bias_last_error(const ddp_position_bias* h) { return h ? h->err.c_str() : ddp_last_error(nullptr); }
+
+int32_t ddp_position_bias_create(ddp_position_bias** out, int32_t device, void* stream, int32_t heads, int32_t buckets, int32_t exact,
+                                 int64_t max_distance, int32_t both) {
+    if (!out) return layer_fail(nullptr, DDP_ERR_ARG, "ddp_position_bias_create: out is null");
+    *out = nullptr;
+    const int32_t status = layer_device("ddp_position_bias_create: bad device", device);
+    if (status != DDP_OK) return status;
+    if (heads < 1 || buckets < 1) return layer_fail(nullptr, DDP_ERR_ARG, "ddp_position_bias_create: heads and buckets are at least 1");
+    if (heads > kMaxHeads || buckets > kMaxBuckets || max_distance > kMaxDistance)
+        return layer_fail(nullptr, DDP_ERR_UNSUPPORTED, "ddp_position_bias_create: more than 4096 heads, 1024 buckets or a distance of 2^20");
+    if (both && buckets % 2) return layer_fail(nullptr, DDP_ERR_ARG, "ddp_position_bias_create: an odd number of buckets for two directions");
+    const int32_t sides = both ? buckets / 2 : buckets;
+    if (exact < 1 || exact > sides) return layer_fail(nullptr, DDP_ERR_ARG, "ddp_position_bias_create: exact is from 1 to the buckets of a direction");
+    if (exact < sides && max_distance <= exact) return layer_fail(nullptr, DDP_ERR_ARG, "ddp_position_bias_create: max_distance is above exact");
+    ddp_position_bias* h = new (std::nothrow) ddp_position_bias();
+    if (!h) return layer_fail(nullptr, DDP_ERR_HIP, "out of host memory");
+    h->device = device;
+    h->stream = static_cast<hipStream_t>(stream);
+    h->heads = heads;
+    h->buckets = buckets;
+    h->exact = exact;
+    h->both = both != 0;
+    h->sides = sides;
+    h->distance = max_distance;
+    try {
+        for (int k = 0; k < sides; ++k) h->first_host.push_back(k < exact ? k : first_distance(exact, max_distance, k - exact, sides - exact));
+    } catch (...) {
+        delete h;
+        return layer_fail(nullptr, DDP_ERR_HIP, "out of host memory");
+    }
+    if (device != DDP_DEVICE_NONE) {
+        const int64_t each = static_cast<int64_t>(heads) * buckets * 4;
+        h->parts = static_cast<int32_t>(std::max<int64_t>(64, std::min<int64_t>(4096, kPartBytes / each)));
+        const int64_t firsts = round_up(sides * 4, 256);
+        hipError_t err = layer_alloc(h, firsts + h->parts * each);
+        if (err == hipSuccess) {
+            OnDevice on(device);
+            err = taken(hipMemcpy(h->mem, h->first_host.data(), static_cast<size_t>(sides) * 4, hipMemcpyHostToDevice));
+            if (err != hipSuccess) (void)taken(hipFree(h->mem));
+        }
+        if (err != hipSuccess) {
+            delete h;
+            return layer_fail(nullptr, DDP_ERR_HIP, hipGetErrorString(err));
+        }
+        h->first = reinterpret_cast<int32_t*>(h->mem);
+        h->partial = reinterpret_cast<float*>(h->mem + firsts);
+    }
+    *out = h;
+    return DDP_OK;
+}
+
+int32_t ddp_position_bias_destroy(ddp_position_bias* h) {
+    if (!h) return DDP_ERR_ARG;
+    layer_release(h);
+    delete h;
+    return DDP_OK;
+}
+
+int32_t ddp_position_bias_buckets(const ddp_position_bias* h, int32_t* first) {
+    if (!h) return DDP_ERR_ARG;
+    if (!first) return DDP_ERR_ARG;
+    std::copy(h->first_host.begin(), h->first_host.end(), first);
+    return h->sides;
+}
+
+int32_t ddp_position_bias_apply(ddp_position_bias* h, int64_t batch, int64_t queries, int64_t keys, int64_t offset, const void* table,
+                                int32_t table_dtype, int64_t table_stride, float scale, const int32_t* key_lengths, int32_t causal, float masked,
+                                int32_t accumulate, void* out, int32_t out_dtype, int64_t batch_stride, int64_t head_stride, int64_t query_stride) {
+    if (!h) return DDP_ERR_ARG;
+    const int32_t status = check_shape(h, batch, queries, keys, offset, out_dtype, table_dtype, table_stride);
+    if (status != DDP_OK) return status;
+    const bool some = batch > 0 && queries > 0 && keys > 0;
+    if (some) {
+        // every place is written once: the three strides in the order of their size step over what the shorter ones span
+        struct { int64_t n, stride; } d[3] = {{batch, batch_stride}, {h->heads, head_stride}, {queries, query_stride}};
+        std::sort(d, d + 3, [](const auto& x, const auto& y) { return x.stride < y.stride; });
+        int64_t span = keys;
+        for (const auto& x : d) {
+            if (x.n == 1) continue;
+            if (x.stride < span) return layer_fail(h, DDP_ERR_ARG, "ddp_position_bias_apply: rows of the scores overlap");
+            if (out_of_reach(x.n, x.stride)) return layer_fail(h, DDP_ERR_ARG, "ddp_position_bias_apply: scores of more than 2^46 elements");
+            span += (x.n - 1) * x.stride;
+        }
+    }
+    if (some && (!table || !out)) return layer_fail(h, DDP_ERR_ARG, "ddp_position_bias_apply: null pointer");
+    if (misaligned(table, elem_bytes(table_dtype)) || misaligned(out, elem_bytes(out_dtype)) || misaligned(key_lengths, 4))
+        return layer_fail(h, DDP_ERR_ARG, "ddp_position_bias_apply: pointer not aligned to its element size");
+    if (h->device == DDP_DEVICE_NONE) return layer_fail(h, DDP_ERR_NO_DEVICE, "ddp_position_bias_apply without a device");
+    if (!some) return DDP_OK;
+    OnDevice on(h->device);
+    LAYER_HIP(h, on.err);
+    BiasArgs a{};
+    a.first = h->first;
+    a.key_lengths = key_lengths;
+    a.table = static_cast<const char*>(table);
+    a.scores = static_cast<char*>(out);
+    a.batch = batch;
+    a.queries = queries;
+    a.keys = keys;
+    a.offset = offset;
+    a.table_stride = table_stride;
+    a.s_batch = batch_stride;
+    a.s_head = head_stride;
+    a.s_query = query_stride;
+    a.heads = h->heads;
+    a.buckets = h->buckets;
+    a.sides = h->sides;
+    a.both = h->both;
+    a.causal = causal != 0;
+    a.add = accumulate != 0;
+    a.scale = scale;
+    a.masked = masked;
+    LAYER_HIP(h, table_dtype == DDP_FP32   ? launch_apply<DDP_FP32>(h, a, out_dtype)
+                 : table_dtype == DDP_FP16 ? launch_apply<DDP_FP16>(h, a, out_dtype)
+                                           : launch_apply<DDP_BF16>(h, a, out_dtype));
+    return DDP_OK;
+}
+
+int32_t ddp_position_bias_grad(ddp_position_bias* h, int64_t batch, int64_t queries, int64_t keys, int64_t offset, const void* dscores, int32_t dtype,
+                               int64_t batch_stride, int64_t head_stride, int64_t query_stride, float scale, const int32_t* key_lengths,
+                               const int32_t* query_lengths, int32_t causal, int32_t accumulate, void* grad, int32_t grad_dtype, int64_t grad_stride) {
+    if (!h) return DDP_ERR_ARG;
+    const int32_t status = check_shape(h, batch, queries, keys, offset, dtype, grad_dtype, grad_stride);
+    if (status != DDP_OK) return status;
+    if (batch_stride < 0 || head_stride < 0 || query_stride < 0) return layer_fail(h, DDP_ERR_ARG, "ddp_position_bias_grad: a stride is below 0");
+    if (out_of_reach(batch, batch_stride) || out_of_reach(h->heads, head_stride) || out_of_reach(queries, query_stride))
+        return layer_fail(h, DDP_ERR_ARG, "ddp_position_bias_grad: scores of more than 2^46 elements");
+    const bool some = batch > 0 && queries > 0 && keys > 0;
+    if (!grad || (some && !dscores)) return layer_fail(h, DDP_ERR_ARG, "ddp_position_bias_grad: null pointer");
+    if (misaligned(dscores, elem_bytes(dtype)) || misaligned(grad, elem_bytes(grad_dtype)) || misaligned(key_lengths, 4) || misaligned(query_lengths, 4))
+        return layer_fail(h, DDP_ERR_ARG, "ddp_position_bias_grad: pointer not aligned to its element size");
+    if (h->device == DDP_DEVICE_NONE) return layer_fail(h, DDP_ERR_NO_DEVICE, "ddp_position_bias_grad without a device");
+    OnDevice on(h->device);
+    LAYER_HIP(h, on.err);
+    int64_t parts = 0;
+    if (some) {
+        BiasArgs a{};
+        a.first = h->first;
+        a.key_lengths = key_lengths;
+        a.query_lengths = query_lengths;
+        a.scores = static_cast<char*>(const_cast<void*>(dscores));
+        a.partial = h->partial;
+        a.batch = batch;
+        a.queries = queries;
+        a.keys = keys;
+        a.offset = offset;
+        a.s_batch = batch_stride;
+        a.s_head = head_stride;
+        a.s_query = query_stride;
+        a.heads = h->heads;
+        a.buckets = h->buckets;
+        a.sides = h->sides;
+        a.both = h->both;
+        a.causal = causal != 0;
+        const int64_t strips = (queries + keys - 1 + kThreads - 1) / kThreads;
+        if (strips > h->parts) return layer_fail(h, DDP_ERR_UNSUPPORTED, "ddp_position_bias_grad: more diagonals than the workspace has parts for");
+        a.strips = static_cast<int32_t>(strips);
+        a.rows_per_part = std::max<int64_t>(128, (queries + h->parts / strips - 1) / (h->parts / strips));
+        a.row_parts = static_cast<int32_t>((queries + a.rows_per_part - 1) / a.rows_per_part);
+        parts = strips * a.row_parts;
+        const dim3 grid(static_cast<unsigned>(parts), static_cast<unsigned>(h->heads));
+        if (dtype == DDP_FP32) hipLaunchKernelGGL((diagonal_kernel<DDP_FP32>), grid, dim3(kThreads), 0, h->stream, a);
+        else if (dtype == DDP_FP16) hipLaunchKernelGGL((diagonal_kernel<DDP_FP16>), grid, dim3(kThreads), 0, h->stream, a);
+        else hipLaunchKernelGGL((diagonal_kernel<DDP_BF16>), grid, dim3(kThreads), 0, h->stream, a);
+        LAYER_HIP(h, hipGetLastError());
+    } else if (accumulate) {
+        return DDP_OK;
+    }
+    JoinArgs j{h->partial, static_cast<char*>(grad), grad_stride, static_cast<int32_t>(parts), h->heads, h->buckets, grad_dtype, accumulate != 0, scale};
+    hipLaunchKernelGGL(join_kernel, dim3(static_cast<unsigned>((h->heads * h->buckets + kThreads - 1) / kThreads)), dim3(kThreads), 0, h->stream, j);
+    LAYER_HIP(h, hipGetLastError());
+    return DDP_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,270 @@
+"""Routing to experts, its gradient and the balance bias through the C ABI against the 64-bit oracle.
+
+Choices are compared for equality: they are made as binary64 has the keys, and equal keys (equal logits, equal biases) go to the lower index.
+Weights in binary32: exp(x) of a rounded x is off by |x| u and 2 u of its own, a sum of n terms by (n / 16 + 12) u, so that
+a weight is off by R u of itself, R = 2 (largest difference of logits) + experts / 16 + 40.  The gradient's terms are products of such
+weights: twice R u of the terms' magnitudes."""
+import numpy as np
+import pytest
+
+from layer_cases import BF16, FP16, FP32, GUARD, TINY, U, UNIT, Rows, close, lib, torch_type, vector
+from oracle import layer as ops
+
+pytestmark = pytest.mark.gpu
+
+SOFTMAX, SIGMOID = 0, 1
+KINDS = [(4, 2, 1, 1, 1), (1, 1, 1, 1, 2), (64, 2, 1, 1, 1), (60, 4, 1, 1, 1), (128, 6, 4, 2, 2), (256, 8, 8, 4, 2), (255, 9, 5, 2, 1), (160, 6, 8, 3, 1),
+         (1024, 64, 64, 7, 2), (7, 7, 1, 1, 1), (512, 16, 1, 1, 1), (33, 3, 11, 2, 2), (8, 3, 8, 5, 2)]
+
+
+def spread(x):
+    x = np.where(np.isfinite(x), x, 0.0)
+    return np.maximum(x.max(axis=1) - x.min(axis=1), np.abs(x).max(axis=1))
+
+
+def check_route(tokens, kind, score, renormalise, dt=FP32, wt=FP32, scale=2.5, bias=True, gap=0, shift=0, add=False, seed=0, logits=None, stats=True,
+                handle=None):
+    torch, d = lib()
+    E, k, groups, kept, top = kind
+    rng = np.random.default_rng(seed + E)
+    x = Rows(rng.standard_normal((tokens, E)) * 1.5 if logits is None else logits, dt, gap, shift)
+    b = (rng.integers(-40, 41, E) * np.float32(1e-3)).astype(np.float32) if bias is True else bias
+    b_on = torch.from_numpy(b).cuda() if b is not None and bias is not False else None
+    experts = torch.full((tokens + 1, k), 99, dtype=torch.int32, device="cuda")
+    weights = torch.full((tokens + 1, k), GUARD, dtype=torch_type(wt), device="cuda")
+    counts = torch.arange(E + 1, dtype=torch.int32, device="cuda")
+    h = handle or d.ddp_router_create(0, 0, E, k, groups, kept, top, score, renormalise, scale)
+    torch.cuda.synchronize()
+    d.ddp_router_route(h, tokens, x.ptr, dt, x.stride, b_on.data_ptr() if b_on is not None else 0, experts.data_ptr(), weights.data_ptr(), wt,
+                       counts.data_ptr() if stats else 0, add)
+    torch.cuda.synchronize()
+    want, w = ops.route(x.held, b if b_on is not None else np.zeros(E), k, groups, kept, top, score, renormalise, scale)
+    got = experts[:-1].cpu().numpy()
+    assert (got == want).all(), (np.argwhere(got != want)[:3].tolist(), got[(got != want).any(1)][:2], want[(got != want).any(1)][:2])
+    R = (2 * spread(x.held) + E / 16 + 40)[:, None]
+    close(weights[:-1].double().cpu().numpy(), w, R * U * np.abs(w) + UNIT[wt] * np.abs(w) + max(TINY[wt], 2.0 ** -126), "weights")
+    assert (experts[-1] == 99).all() and (weights[-1] == GUARD).all()
+    load = np.bincount(want[want >= 0], minlength=E) if stats else np.arange(E)
+    if add and stats:
+        load = load + np.arange(E)
+    assert (counts[:-1].cpu().numpy() == load).all() and counts[-1] == E
+    if handle is None:
+        d.ddp_router_destroy(h)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("renormalise", [False, True])
+def test_route(kind, score, renormalise):
+    check_route(150, kind, score, renormalise)
+
+
+@pytest.mark.parametrize("dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("wt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_route_types(dt, wt, score):
+    check_route(90, (64, 6, 4, 2, 2), score, True, dt, wt, gap=3, shift=1, add=True)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_route_equal_keys(kind, score):
+    """Logits of few values: most keys are equal to others, and go to the lower index, among groups too."""
+    rng = np.random.default_rng(kind[0])
+    logits = rng.integers(-2, 3, (120, kind[0])) * 0.5
+    logits[7] = 0.0
+    check_route(120, kind, score, True, BF16, logits=logits, bias=False)
+    check_route(120, kind, score, False, FP32, logits=logits, bias=(rng.integers(0, 2, kind[0]) * 0.125).astype(np.float32))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_route_nearly_equal_keys(kind, score):
+    """Logits one step of binary32 apart: binary64 tells their keys apart, binary32 mostly does not."""
+    rng = np.random.default_rng(kind[0] + 1)
+    logits = (1.0 + rng.integers(0, 4 * kind[0], (80, kind[0])) * 2.0 ** -23).astype(np.float32).astype(np.float64)
+    check_route(80, kind, score, True, logits=logits, bias=False)
+    check_route(80, kind, score, True, logits=logits, bias=np.full(kind[0], 0.37, dtype=np.float32))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_route_masked_experts(kind, score):
+    rng = np.random.default_rng(kind[0])
+    logits = rng.standard_normal((64, kind[0]))
+    logits[rng.random(logits.shape) < 0.5] = -np.inf
+    logits[3] = -np.inf
+    logits[5] = np.nan
+    logits[9, 0] = np.nan
+    logits[11, -1] = np.inf
+    logits[13] = -1e30
+    logits[15] = 1e30
+    check_route(64, kind, score, True, logits=logits)
+    check_route(64, kind, score, False, logits=logits, bias=False)
+    bias = rng.standard_normal(kind[0]).astype(np.float32)
+    bias[::3] = -np.inf
+    bias[1::5] = np.nan
+    check_route(64, kind, score, True, logits=logits, bias=bias)
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("tokens", [0, 1, 2, 3, 15, 16, 17, 4099])
+def test_route_numbers_of_tokens(score, tokens):
+    check_route(tokens, (64, 6, 8, 3, 2), score, True, BF16)
+    check_route(tokens, (40, 2, 1, 1, 1), score, True, FP32, stats=tokens % 2 == 0)
+
+
+def test_route_wide_range():
+    rng = np.random.default_rng(1)
+    logits = rng.standard_normal((50, 96)) * 60.0
+    check_route(50, (96, 8, 1, 1, 1), SOFTMAX, True, logits=logits, bias=False)
+    check_route(50, (96, 8, 1, 1, 1), SIGMOID, True, logits=logits, bias=False)
+
+
+def check_grad(tokens, kind, score, renormalise, dt=FP32, wt=FP32, scale=2.5, gap=0, shift=0, seed=0, experts=None, logits=None):
+    torch, d = lib()
+    E, k = kind[:2]
+    rng = np.random.default_rng(seed + E)
+    x = Rows(rng.standard_normal((tokens, E)) * 1.5 if logits is None else logits, dt, gap, shift)
+    if experts is None:
+        experts = np.argsort(rng.random((tokens, E)), axis=1)[:, :k]
+    at = torch.from_numpy(np.ascontiguousarray(experts)).int().cuda()
+    dw = Rows(rng.standard_normal((tokens, k)), wt)
+    dx = Rows(np.full((tokens, E), GUARD), dt, gap + 2, shift)
+    h = d.ddp_router_create(0, 0, *kind, score, renormalise, scale)
+    torch.cuda.synchronize()
+    d.ddp_router_grad(h, tokens, x.ptr, dt, x.stride, at.data_ptr(), dw.ptr, wt, dx.ptr, dx.stride)
+    torch.cuda.synchronize()
+    want, magnitude = ops.route_grad(x.held, experts, dw.held, score, renormalise, scale)
+    R = (2 * spread(x.held) + E / 16 + 40)[:, None]
+    close(dx.get(), want, 4 * R * U * magnitude + UNIT[dt] * np.abs(want) + max(TINY[dt], 2.0 ** -126), "dlogits")
+    dx.check_guards()
+    d.ddp_router_destroy(h)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("renormalise", [False, True])
+def test_grad(kind, score, renormalise):
+    check_grad(150, kind, score, renormalise)
+
+
+@pytest.mark.parametrize("dt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("wt", [FP32, FP16, BF16])
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_grad_types(dt, wt, score):
+    check_grad(90, (60, 6, 4, 2, 2), score, True, dt, wt, gap=3, shift=1)
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("tokens", [0, 1, 2, 3, 15, 16, 17, 4099])
+def test_grad_numbers_of_tokens(score, tokens):
+    check_grad(tokens, (64, 6, 8, 3, 2), score, True, BF16)
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("renormalise", [False, True])
+def test_grad_of_places_left_over(score, renormalise):
+    """Indices of no expert take no part, a token without any gets zeros, one that is named twice counts twice; masked logits get zeros."""
+    rng = np.random.default_rng(4)
+    experts = np.argsort(rng.random((40, 70)), axis=1)[:, :5]
+    experts[::3, 3:] = -1
+    experts[4] = -1
+    experts[7] = [3, 70, 3, -5, 2 ** 31 - 1]
+    experts[8] = [69, 69, 69, 69, 69]
+    logits = rng.standard_normal((40, 70))
+    logits[::3, 1::2] = -np.inf
+    experts[::3, :3] = [0, 2, 4]
+    check_grad(40, (70, 5, 1, 1, 1), score, renormalise, experts=experts, logits=logits)
+
+
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_grad_of_large_logits(score):
+    rng = np.random.default_rng(5)
+    check_grad(30, (50, 4, 1, 1, 1), score, True, logits=rng.standard_normal((30, 50)) * 20.0)
+
+
+@pytest.mark.parametrize("replicas,experts", [(1, 1), (1, 8), (3, 60), (8, 256), (64, 1024)])
+def test_balance(replicas, experts):
+    torch, d = lib()
+    rng = np.random.default_rng(experts)
+    counts = rng.integers(0, 5, (replicas, experts))
+    counts[:, experts // 2] = 2 ** 31 - 1 if experts > 8 else 2
+    bias = rng.standard_normal(experts).astype(np.float32)
+    on, b = torch.from_numpy(counts).int().cuda(), torch.from_numpy(bias).cuda()
+    out = torch.full((experts + 1,), GUARD, device="cuda")
+    h = d.ddp_router_create(0, 0, experts, 1)
+    torch.cuda.synchronize()
+    d.ddp_router_balance(h, replicas, on.data_ptr(), 1e-3, b.data_ptr(), out.data_ptr())
+    torch.cuda.synchronize()
+    want = torch.from_numpy(ops.balance(counts, bias, 1e-3))
+    assert torch.equal(out[:-1].cpu(), want) and out[-1] == GUARD
+    d.ddp_router_balance(h, replicas, on.data_ptr(), 1e-3, b.data_ptr(), b.data_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(b.cpu(), want)
+    d.ddp_router_destroy(h)
+
+
+def test_tokens_past_32_bits():
+    """Logits of 4.4 GB: the offsets of the last tokens need more than 32 bits."""
+    torch, d = lib()
+    T, E, k = 17_000_000, 130, 1
+    x = torch.zeros((T, E), dtype=torch.bfloat16, device="cuda")
+    x[:, 5] = 1.0
+    x[-1, 5], x[-1, 129] = 0.0, 1.0
+    experts = torch.zeros((T, k), dtype=torch.int32, device="cuda")
+    weights, counts = torch.zeros((T, k), device="cuda"), torch.zeros(E, dtype=torch.int32, device="cuda")
+    h = d.ddp_router_create(0, 0, E, k, score=SIGMOID)
+    torch.cuda.synchronize()
+    d.ddp_router_route(h, T, x.data_ptr(), BF16, E, 0, experts.data_ptr(), weights.data_ptr(), FP32, counts.data_ptr())
+    torch.cuda.synchronize()
+    assert counts[5] == T - 1 and counts[129] == 1 and counts.sum() == T and experts[-1, 0] == 129 and (weights == 1.0).all()
+    d.ddp_router_destroy(h)
+    h = d.ddp_router_create(0, 0, E, k, score=SIGMOID, renormalise=False)
+    weights.fill_(1.0)
+    torch.cuda.synchronize()
+    d.ddp_router_grad(h, T, x.data_ptr(), BF16, E, experts.data_ptr(), weights.data_ptr(), FP32, x.data_ptr(), E)
+    torch.cuda.synchronize()
+    s = 1 / (1 + np.exp(-1.0))
+    assert abs(x[-1, 129].item() - s * (1 - s)) < 2 ** -8 and (x[:-1, 5] == x[-1, 129]).all() and (x[-1, :129] == 0).all()
+    assert x.count_nonzero() == T
+    d.ddp_router_destroy(h)
+
+
+def test_on_another_stream_and_replayed():
+    torch, d = lib()
+    T, E, k = 3000, 64, 4
+    stream = torch.cuda.Stream()
+    h = d.ddp_router_create(0, stream.cuda_stream, E, k, 8, 4, 2, SIGMOID, True, 2.5)
+    x, dx = torch.zeros((T, E), device="cuda"), torch.zeros((T, E), device="cuda")
+    bias, moved = torch.zeros(E, device="cuda"), torch.zeros(E, device="cuda")
+    experts, counts = torch.zeros((T, k), dtype=torch.int32, device="cuda"), torch.zeros(E, dtype=torch.int32, device="cuda")
+    weights = torch.zeros((T, k), device="cuda")
+    torch.cuda.synchronize()
+
+    def all_of_it():
+        d.ddp_router_route(h, T, x.data_ptr(), FP32, E, bias.data_ptr(), experts.data_ptr(), weights.data_ptr(), FP32, counts.data_ptr())
+        d.ddp_router_grad(h, T, x.data_ptr(), FP32, E, experts.data_ptr(), weights.data_ptr(), FP32, dx.data_ptr(), E)
+        d.ddp_router_balance(h, 1, counts.data_ptr(), 0.01, bias.data_ptr(), moved.data_ptr())
+
+    results = experts, weights, counts, dx, moved
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        all_of_it()
+        stream.synchronize()
+        graph.capture_begin()
+        all_of_it()
+        graph.capture_end()
+        for seed in range(4):
+            x.copy_(torch.randn((T, E), generator=torch.Generator("cuda").manual_seed(seed), device="cuda"))
+            all_of_it()
+            stream.synchronize()
+            want = [t.clone() for t in results]
+            for t in results:
+                t.fill_(99)
+            graph.replay()
+            stream.synchronize()
+            for t, w in zip(results, want):
+                assert torch.equal(t, w)
+    torch.cuda.synchronize()
+    d.ddp_router_destroy(h)
