@@ -643,7 +643,7 @@ int32_t ddp_embedding_grad(ddp_embedding* emb, int64_t tokens, const void* ids, 
  * the rows and in masked places of an input is not used. */
 typedef struct ddp_layernorm ddp_layernorm;
 
-/* Rows of `width` (up to 2^20) elements.  The workspace takes up to 16 MiB, above 2^17 columns 128 bytes a column. */
+/* Rows of `width` (up to 2^20) elements.  The workspace takes up to 32 MiB, above 2^18 columns 128 bytes a column. */
 int32_t ddp_layernorm_create(ddp_layernorm** out, int32_t device, void* stream, int64_t width);
 int32_t ddp_layernorm_destroy(ddp_layernorm* norm);   /* waits for the handle's outstanding work */
 const char* ddp_layernorm_last_error(const ddp_layernorm* norm);

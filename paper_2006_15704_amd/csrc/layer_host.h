@@ -79,4 +79,35 @@ inline void layer_release(LayerHandle* h) {
     if (h->mem) (void)taken(hipFree(h->mem));
 }
 
+#if defined(__HIPCC__)
+
+// Sums over the LANES (8, 16, 32 or 64) neighbours of a lane, the same bits in all of them: neighbours within 16 by the VALU's lane
+// moves, further ones by swaps of rows.  (A shuffle is an LDS access: six of them one after the other take some 0.4 us of a wave.)
+template <int CTRL>
+__device__ __forceinline__ float lane_moved(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float rows_of_16_summed(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned a = r[0], b = r[1];               // (a bit cast of a vector's element takes the first)
+    return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+__device__ __forceinline__ float halves_summed(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned a = r[0], b = r[1];               // (a bit cast of a vector's element takes the first)
+    return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float x) {
+    x += lane_moved<0xB1>(x);                        // quad_perm: 1 0 3 2
+    x += lane_moved<0x4E>(x);                        // quad_perm: 2 3 0 1
+    x += lane_moved<0x141>(x);                       // row_half_mirror
+    if constexpr (LANES >= 16) x += lane_moved<0x140>(x);       // row_mirror
+    if constexpr (LANES >= 32) x = rows_of_16_summed(x);
+    if constexpr (LANES >= 64) x = halves_summed(x);
+    return x;
+}
+
+#endif  // __HIPCC__
+
 }  // namespace ddp

@@ -69,6 +69,266 @@ __device__ __forceinline__ float block_sum(float x, float* part) {
     return sum;
 }
 
+// ---- rows that fit into the registers of a team ----
+//
+// A team is LANES neighbouring lanes or WAVES waves, an element kEach times: a row is read once, in whole 16-byte vectors that are all on
+// the way together, and its sums are taken in registers.  Vector v of lane l is at column (v lanes + l) N; the one that would reach over the
+// end of the row is moved back to end with it, and what it shares with the vector in front of it counts there.
+constexpr int kEach = 16;
+
+template <int XT, int YT, int LANES_, int WAVES_, int THREADS_>
+struct Team {
+    static constexpr int LANES = LANES_, WAVES = WAVES_, THREADS = THREADS_;
+    static constexpr int N = XT == DDP_FP32 ? 4 : 8, V = kEach / N, SIZE = LANES * WAVES, TEAMS = THREADS / SIZE;
+    static_assert(LANES == 64 || WAVES == 1, "a team of several waves has whole ones");
+    int at[V], own[V];                               // own: elements from here on are the vector's; N: nothing here
+    bool ragged;
+
+    __host__ __device__ __forceinline__ explicit Team(int width) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        const int lane = static_cast<int>(threadIdx.x) % SIZE;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (v * SIZE + lane) * N;
+            at[v] = c + N <= width ? c : width - N;
+            own[v] = c >= width ? N : c - at[v];
+        }
+        ragged = width != SIZE * kEach;
+#endif
+    }
+    // Elements that are another vector's, as zeros.
+    __device__ __forceinline__ void clear_shared(float (&x)[V][N]) const {
+        if (!ragged) return;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[v][i] = i >= own[v] ? x[v][i] : 0.0f;
+    }
+    template <int DT>
+    __device__ __forceinline__ void load(const char* row, bool live, Parts<DT, N> (&raw)[V]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (live && own[v] < N) raw[v] = load_parts<DT, N>(row + at[v] * ElemBytes<DT>::value);
+            else raw[v] = Parts<DT, N>{};
+    }
+    template <int DT>
+    __device__ __forceinline__ void store(char* row, bool live, const float (&x)[V][N]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!live || own[v] == N) continue;
+            char* to = row + at[v] * ElemBytes<DT>::value;
+            if (own[v] == 0) {
+                store_some<DT, N>(to, N, x[v]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (i >= own[v]) store_one<DT>(to + i * ElemBytes<DT>::value, x[v][i]);
+            }
+        }
+    }
+    __device__ __forceinline__ void params(const char* p, int type, float none, float (&x)[V][N]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) load_param<N>(p, type, at[v], N, none, x[v]);
+    }
+    // Sums over the team.  Several waves meet in LDS: `meet` has room for two values of each wave, and alternates.
+    __device__ __forceinline__ void sum(float& a, float* meet) const {
+        a = lanes_sum<LANES>(a);
+        if constexpr (WAVES > 1) {
+            const int wave = threadIdx.x >> 6;
+            if ((threadIdx.x & 63) == 0) meet[wave] = a;
+            __syncthreads();
+            const float* mine = meet + wave / WAVES * WAVES;
+            a = mine[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) a += mine[w];
+        }
+    }
+    __device__ __forceinline__ void sum(float& a, float& b, float* meet) const {
+        a = lanes_sum<LANES>(a);
+        b = lanes_sum<LANES>(b);
+        if constexpr (WAVES > 1) {
+            const int wave = threadIdx.x >> 6;
+            if ((threadIdx.x & 63) == 0) {
+                meet[wave * 2] = a;
+                meet[wave * 2 + 1] = b;
+            }
+            __syncthreads();
+            const float* mine = meet + wave / WAVES * WAVES * 2;
+            a = mine[0];
+            b = mine[1];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                a += mine[w * 2];
+                b += mine[w * 2 + 1];
+            }
+        }
+    }
+};
+
+template <int XT, int YT, typename T>
+__global__ __launch_bounds__(T::THREADS) void forward_team_kernel(ForwardArgs a) {
+    constexpr int N = T::N, V = T::V;
+    __shared__ float meet[2][T::THREADS / 64];
+    const T team(a.width);
+    float gamma[V][N], beta[V][N];
+    team.params(a.gamma, a.param, 1.0f, gamma);
+    team.params(a.beta, a.param, 0.0f, beta);
+    const float each = 1.0f / a.width;
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * T::TEAMS; base < a.rows; base += static_cast<int64_t>(gridDim.x) * T::TEAMS) {
+        const int64_t row = base + threadIdx.x / T::SIZE;
+        const bool live = row < a.rows;
+        Parts<XT, N> x[V], r[V];
+        team.template load<XT>(a.x + row * a.x_stride * ElemBytes<XT>::value, live, x);
+        if (a.residual != nullptr) team.template load<XT>(a.residual + row * a.residual_stride * ElemBytes<XT>::value, live, r);
+        float s[V][N], sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) widen<XT, N>(x[v], s[v]);
+        if (a.residual != nullptr) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float more[N];
+                widen<XT, N>(r[v], more);
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[v][i] += more[i];
+            }
+        }
+        if (a.sum != nullptr) team.template store<XT>(a.sum + row * a.sum_stride * ElemBytes<XT>::value, live, s);
+        team.clear_shared(s);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum += s[v][i];
+        team.sum(sum, meet[0]);
+        const float mean = sum * each;
+        float squares = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[v][i] -= mean;
+        team.clear_shared(s);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) squares += s[v][i] * s[v][i];
+        team.sum(squares, meet[1]);
+        const float rstd = 1.0f / sqrtf(squares * each + a.eps);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[v][i] = s[v][i] * rstd * gamma[v][i] + beta[v][i];
+        team.template store<YT>(a.y + row * a.y_stride * ElemBytes<YT>::value, live, s);
+        if (live && threadIdx.x % T::SIZE == 0) {
+            if (a.mean != nullptr) a.mean[row] = mean;
+            if (a.rstd != nullptr) a.rstd[row] = rstd;
+        }
+    }
+}
+
+// The block's teams sum dgamma and dbeta over their rows, meet in LDS by halves, and leave one row of sums for the join.
+template <int XT, int YT, typename T>
+__global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs a) {
+    constexpr int N = T::N, V = T::V;
+    constexpr bool WIDE = T::LANES == 64;            // narrower teams meet within their wave first
+    constexpr int MEET = WIDE ? T::TEAMS : T::THREADS / 64;
+    __shared__ float meet[2][T::THREADS / 64 * 2];
+    __shared__ float part[MEET > 1 ? MEET / 2 : 1][2][MEET > 1 ? T::SIZE * kEach : 1];
+    const T team(a.width);
+    float gamma[V][N], dgamma[V][N] = {}, dbeta[V][N] = {};
+    team.params(a.gamma, a.param, 1.0f, gamma);
+    const float each = 1.0f / a.width;
+    int turn = 0;
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * T::TEAMS; base < a.rows; base += static_cast<int64_t>(gridDim.x) * T::TEAMS) {
+        const int64_t row = base + threadIdx.x / T::SIZE;
+        const bool live = row < a.rows;
+        Parts<XT, N> x[V], more[V];
+        Parts<YT, N> dy[V];
+        team.template load<YT>(a.dy + row * a.dy_stride * ElemBytes<YT>::value, live, dy);
+        team.template load<XT>(a.x + row * a.x_stride * ElemBytes<XT>::value, live, x);
+        if (a.dsum != nullptr && a.dx != nullptr) team.template load<XT>(a.dsum + row * a.dsum_stride * ElemBytes<XT>::value, live, more);
+        const float mean = live ? a.mean[row] : 0.0f, rstd = live ? a.rstd[row] : 0.0f;
+        float g[V][N], xh[V][N], of_g = 0.0f, of_gx = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            widen<YT, N>(dy[v], g[v]);
+            widen<XT, N>(x[v], xh[v]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) xh[v][i] = (xh[v][i] - mean) * rstd;
+        }
+        team.clear_shared(g);
+        team.clear_shared(xh);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                dgamma[v][i] += g[v][i] * xh[v][i];
+                dbeta[v][i] += g[v][i];
+                g[v][i] *= gamma[v][i];
+                of_g += g[v][i];
+                of_gx += g[v][i] * xh[v][i];
+            }
+        if (a.dx == nullptr) continue;
+        team.sum(of_g, of_gx, meet[turn]);
+        turn ^= 1;
+        const float c1 = of_g * each, c2 = of_gx * each;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[v][i] = (g[v][i] - c1 - xh[v][i] * c2) * rstd;
+        if (a.dsum != nullptr) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float m[N];
+                widen<XT, N>(more[v], m);
+#pragma unroll
+                for (int i = 0; i < N; ++i) g[v][i] += m[i];
+            }
+        }
+        team.template store<XT>(a.dx + row * a.dx_stride * ElemBytes<XT>::value, live, g);
+    }
+    if (a.partial == nullptr) return;
+    if constexpr (!WIDE) {
+#pragma unroll
+        for (int d = T::LANES; d < 64; d <<= 1)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    dgamma[v][i] += __shfl_xor(dgamma[v][i], d);
+                    dbeta[v][i] += __shfl_xor(dbeta[v][i], d);
+                }
+    }
+    const int me = WIDE ? threadIdx.x / T::SIZE : threadIdx.x >> 6, lane = threadIdx.x % T::SIZE;
+#pragma unroll
+    for (int half = MEET / 2; half > 0; half >>= 1) {
+        if (me >= half && me < 2 * half) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    part[me - half][0][(v * N + i) * T::SIZE + lane] = dgamma[v][i];
+                    part[me - half][1][(v * N + i) * T::SIZE + lane] = dbeta[v][i];
+                }
+        }
+        __syncthreads();
+        if (me < half) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    dgamma[v][i] += part[me][0][(v * N + i) * T::SIZE + lane];
+                    dbeta[v][i] += part[me][1][(v * N + i) * T::SIZE + lane];
+                }
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x >= T::SIZE) return;
+    char* to = reinterpret_cast<char*>(a.partial + static_cast<int64_t>(blockIdx.x) * 2 * a.width);
+    team.template store<DDP_FP32>(to, true, dgamma);
+    team.template store<DDP_FP32>(to + static_cast<int64_t>(a.width) * 4, true, dbeta);
+}
+
+// ---- other rows ----
+
 // A block a row, three passes over it (the second and third come from the caches).
 constexpr int kN = 4;
 template <int XT>
@@ -201,43 +461,83 @@ struct JoinArgs {
     char *dgamma, *dbeta;
     int32_t width, chunks, grad, add;
 };
-// blockIdx.y: dgamma, dbeta.  A thread a column.
-__global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a) {
+// blockIdx.y: dgamma, dbeta.  A wave has 64 columns of a share of the chunks, kJoinWaves of them meet in LDS.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
+    __shared__ double part[kJoinWaves][64];
     char* out = blockIdx.y == 0 ? a.dgamma : a.dbeta;
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (out == nullptr || c >= a.width) return;
-    float sum = 0.0f;
-    for (int k = 0; k < a.chunks; ++k) sum += a.partial[(static_cast<int64_t>(k) * 2 + blockIdx.y) * a.width + c];
-    if (a.grad == DDP_FP32) {
-        float* to = reinterpret_cast<float*>(out) + c;
-        *to = a.add ? *to + sum : sum;
-    } else if (a.grad == DDP_FP16) {
-        store_one<DDP_FP16>(out + 2 * static_cast<int64_t>(c), a.add ? load_one<DDP_FP16>(out + 2 * static_cast<int64_t>(c)) + sum : sum);
-    } else {
-        store_one<DDP_BF16>(out + 2 * static_cast<int64_t>(c), a.add ? load_one<DDP_BF16>(out + 2 * static_cast<int64_t>(c)) + sum : sum);
+    if (out == nullptr) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    double sum = 0.0;
+    if (c < a.width) {
+        const float* from = a.partial + static_cast<int64_t>(blockIdx.y) * a.width + c;
+        for (int k = wave; k < a.chunks; k += kJoinWaves * 8) {
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = k + u * kJoinWaves < a.chunks ? from[static_cast<int64_t>(k + u * kJoinWaves) * 2 * a.width] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sum += x[u];
+        }
     }
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || c >= a.width) return;
+#pragma unroll
+    for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
+    char* to = out + static_cast<int64_t>(c) * (a.grad == DDP_FP32 ? 4 : 2);
+    if (a.grad == DDP_FP32) store_one<DDP_FP32>(to, static_cast<float>(a.add ? sum + load_one<DDP_FP32>(to) : sum));
+    else if (a.grad == DDP_FP16) store_one<DDP_FP16>(to, static_cast<float>(a.add ? sum + load_one<DDP_FP16>(to) : sum));
+    else store_one<DDP_BF16>(to, static_cast<float>(a.add ? sum + load_one<DDP_BF16>(to) : sum));
 }
 
 // ---- host ----
 
 constexpr int kRowBlocks = 1 << 16;
 
+constexpr int kForwardThreads = 256, kForwardBlocks = 2048, kBackwardThreads = 512;
+
+// The team of a width, as a type; false: rows are too short for a vector, or too long for a team.
+template <int XT, int YT, int THREADS, typename F>
+bool with_team(int64_t width, F f) {
+    constexpr int N = XT == DDP_FP32 ? 4 : 8;
+    if (width < N || width > 16 * 64 * kEach) return false;
+    if (width <= 8 * kEach) f(Team<XT, YT, 8, 1, THREADS>(0));
+    else if (width <= 32 * kEach) f(Team<XT, YT, 32, 1, THREADS>(0));
+    else if (width <= 64 * kEach) f(Team<XT, YT, 64, 1, THREADS>(0));
+    else if (width <= 2 * 64 * kEach) f(Team<XT, YT, 64, 2, THREADS>(0));
+    else if (width <= 4 * 64 * kEach) f(Team<XT, YT, 64, 4, THREADS>(0));
+    else if (width <= 8 * 64 * kEach) f(Team<XT, YT, 64, 8, std::max(512, THREADS)>(0));
+    else f(Team<XT, YT, 64, 16, 1024>(0));
+    return true;
+}
+
 template <int XT, int YT>
 hipError_t launch_forward(ddp_layernorm* h, const ForwardArgs& a) {
-    hipLaunchKernelGGL((forward_kernel<XT, YT>), dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kRowBlocks))), dim3(kThreads), 0, h->stream, a);
+    const bool team = with_team<XT, YT, kForwardThreads>(a.width, [&](auto t) {
+        typedef decltype(t) T;
+        const int64_t blocks = std::min<int64_t>((a.rows + T::TEAMS - 1) / T::TEAMS, kForwardBlocks);
+        hipLaunchKernelGGL((forward_team_kernel<XT, YT, T>), dim3(static_cast<unsigned>(blocks)), dim3(T::THREADS), 0, h->stream, a);
+    });
+    if (!team)
+        hipLaunchKernelGGL((forward_kernel<XT, YT>), dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kRowBlocks))), dim3(kThreads), 0, h->stream, a);
     return hipGetLastError();
 }
+// Returns the row chunks that sums are left of.
 template <int XT, int YT>
-hipError_t launch_backward(ddp_layernorm* h, const BackwardArgs& a, bool params) {
-    if (a.dx != nullptr) {
+int32_t launch_backward(ddp_layernorm* h, BackwardArgs a) {
+    int32_t chunks = a.chunks;
+    const bool team = with_team<XT, YT, kBackwardThreads>(a.width, [&](auto t) {
+        typedef decltype(t) T;
+        chunks = static_cast<int32_t>(std::min<int64_t>((a.rows + T::TEAMS - 1) / T::TEAMS, h->chunks));
+        hipLaunchKernelGGL((backward_team_kernel<XT, YT, T>), dim3(static_cast<unsigned>(chunks)), dim3(T::THREADS), 0, h->stream, a);
+    });
+    if (team) return chunks;
+    if (a.dx != nullptr)
         hipLaunchKernelGGL((backward_rows_kernel<XT, YT>), dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kRowBlocks))), dim3(kThreads), 0, h->stream, a);
-        const hipError_t err = hipGetLastError();
-        if (err != hipSuccess) return err;
-    }
-    if (!params) return hipSuccess;
-    hipLaunchKernelGGL((backward_columns_kernel<XT, YT>), dim3(static_cast<unsigned>((a.width + 64 * kN - 1) / (64 * kN)), static_cast<unsigned>(a.chunks)),
-                       dim3(kThreads), 0, h->stream, a);
-    return hipGetLastError();
+    if (a.partial != nullptr)
+        hipLaunchKernelGGL((backward_columns_kernel<XT, YT>), dim3(static_cast<unsigned>((a.width + 64 * kN - 1) / (64 * kN)), static_cast<unsigned>(a.chunks)),
+                           dim3(kThreads), 0, h->stream, a);
+    return chunks;
 }
 
 // y has x's type, or any where x is binary32.
@@ -277,7 +577,7 @@ int32_t ddp_layernorm_create(ddp_layernorm** out, int32_t device, void* stream, 
     h->device = device;
     h->stream = static_cast<hipStream_t>(stream);
     h->width = width;
-    h->chunks = static_cast<int32_t>(std::max<int64_t>(16, std::min<int64_t>(512, (int64_t(1) << 21) / width)));
+    h->chunks = static_cast<int32_t>(std::max<int64_t>(16, std::min<int64_t>(512, (int64_t(1) << 22) / width)));
     if (device != DDP_DEVICE_NONE) {
         const hipError_t err = layer_alloc(h, static_cast<int64_t>(h->chunks) * 2 * width * 4);
         if (err != hipSuccess) {
@@ -365,7 +665,7 @@ int32_t ddp_layernorm_backward(ddp_layernorm* h, int64_t rows, const void* dy, i
     a.mean = mean;
     a.rstd = rstd;
     a.dx = static_cast<char*>(dx);
-    a.partial = h->partial;
+    a.partial = params ? h->partial : nullptr;
     a.rows = rows;
     a.dy_stride = dy_stride;
     a.x_stride = x_stride;
@@ -375,11 +675,14 @@ int32_t ddp_layernorm_backward(ddp_layernorm* h, int64_t rows, const void* dy, i
     a.chunks = static_cast<int32_t>((rows + a.rows_per_chunk - 1) / a.rows_per_chunk);
     a.width = static_cast<int32_t>(h->width);
     a.param = param_dtype;
-    if (rows > 0)
-        LAYER_HIP(h, with_types(x_dtype, dy_dtype, [&](auto xt, auto yt) { return launch_backward<xt.value, yt.value>(h, a, params); }));
+    int32_t chunks = 0;
+    if (rows > 0) {
+        chunks = with_types(x_dtype, dy_dtype, [&](auto xt, auto yt) { return launch_backward<xt.value, yt.value>(h, a); });
+        LAYER_HIP(h, hipGetLastError());
+    }
     if (!params) return DDP_OK;
-    JoinArgs j{h->partial, static_cast<char*>(dgamma), static_cast<char*>(dbeta), a.width, a.chunks, grad_dtype, accumulate != 0};
-    hipLaunchKernelGGL(join_kernel, dim3(static_cast<unsigned>((a.width + kThreads - 1) / kThreads), 2), dim3(kThreads), 0, h->stream, j);
+    JoinArgs j{h->partial, static_cast<char*>(dgamma), static_cast<char*>(dbeta), a.width, chunks, grad_dtype, accumulate != 0};
+    hipLaunchKernelGGL(join_kernel, dim3(static_cast<unsigned>((a.width + 63) / 64), 2), dim3(64 * kJoinWaves), 0, h->stream, j);
     LAYER_HIP(h, hipGetLastError());
     return DDP_OK;
 }
