@@ -25,8 +25,9 @@ namespace {
 
 using namespace ddp;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxBuckets = 1024, kMaxHeads = 4096;
+constexpr int64_t kFar = int64_t(1) << 40;
 constexpr int64_t kMaxDistance = int64_t(1) << 20, kMaxLength = int64_t(1) << 24, kMaxBatch = int64_t(1) << 20;
 
 // Whole numbers of any size: what a logarithm's step at exactly a whole distance takes to be settled.
@@ -71,8 +72,9 @@ struct BiasArgs {
     const char* table;
     char* scores;                                // dscores in the gradient
     float* partial;
-    int64_t batch, queries, keys, offset, table_stride, s_batch, s_head, s_query, rows_per_part;
-    int32_t heads, buckets, sides, both, causal, add, strips, row_parts;
+    int64_t batch, queries, keys, offset, table_stride, s_batch, s_head, s_query;
+    int64_t band0, strips;                       // of the gradient: the first lane of the first strip
+    int32_t heads, buckets, sides, both, causal, add, strip_blocks, shares;
     float scale, masked;
 };
 
@@ -116,36 +118,122 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
     }
 }
 
-// A block has kThreads diagonals of one head, and a part of the rows of all sequences: a thread a diagonal, then a thread a bucket.
+// ---- gradient ----
+//
+// A vector of N keys (16 bytes) that moves one vector to the right with every N rows meets the same 2 N - 1 diagonals in every such step:
+// a lane holds them in registers, loads whole aligned vectors, and adds every element once.  Lane t of the band has columns N (g + t) in the
+// rows N g ... N g + N - 1; neighbours in a wave are neighbours in memory.
+//
+// A block has the 64 lanes' band (64 N diagonals) of one head and a share of its row groups of all sequences, which go round its waves.  Then
+// diagonals are put together in LDS, and buckets, which are ranges of diagonals, summed in binary64.
+
+template <int N> struct Band {
+    static constexpr int diagonals = 64 * N + N - 1, low = N - 1;    // element e of row x of lane t: N t + e - x + low
+};
+// The diagonals that belong to bucket k, as r from lo to hi (hi < lo: none).
+__device__ __forceinline__ void range_of(const int32_t* first, const BiasArgs& a, int k, int64_t& lo, int64_t& hi) {
+    const bool behind = k >= a.sides;
+    const int side = behind ? k - a.sides : k;
+    const int64_t from = first[side], to = side + 1 < a.sides ? first[side + 1] - 1 : kFar;
+    lo = behind ? (from > 1 ? from : 1) : -to;
+    hi = behind ? to : side == 0 && !a.both ? kFar : -from;
+}
+
 template <int ST>
 __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
+    constexpr int N = ST == DDP_FP32 ? 4 : 8, DIAGONALS = Band<N>::diagonals;
+    __shared__ float diagonal[kWaves][DIAGONALS + 1];
     __shared__ int32_t first[kMaxBuckets];
-    __shared__ float sums[kThreads];
-    __shared__ int of[kThreads];
+    extern __shared__ double sums[];                 // of the buckets
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int k = threadIdx.x; k < a.sides; k += kThreads) first[k] = a.first[k];
-    __syncthreads();
-    const int64_t h = blockIdx.y;
-    const int strip = blockIdx.x % a.strips, part = blockIdx.x / a.strips;
-    const int64_t diagonal = static_cast<int64_t>(strip) * kThreads + threadIdx.x - (a.queries - 1);      // j - i
-    const int64_t from = part * a.rows_per_part, to = min(from + a.rows_per_part, a.queries);
-    float sum = 0.0f;
-    if (diagonal < a.keys && !(a.causal && diagonal > a.offset)) {
+    for (int k = threadIdx.x; k < a.buckets; k += kThreads) sums[k] = 0.0;
+    const int64_t h = blockIdx.x % a.heads;
+    const int part = blockIdx.x / a.heads, share = part % a.shares;
+    const int64_t groups = (a.queries + N - 1) / N, vectors = (a.keys + N - 1) / N;
+    const char* scores = a.scores + h * a.s_head * ElemBytes<ST>::value;
+    for (int64_t strip = part / a.shares; strip < a.strips; strip += a.strip_blocks) {
+        const int64_t t0 = a.band0 + strip * 64, t = t0 + lane;
+        // the row groups in which some lane has a column
+        const int64_t g_from = max(int64_t(0), -(t0 + 63)), g_to = min(groups, vectors - t0);
+        const int64_t steps = max(g_to - g_from, int64_t(0)), turns = static_cast<int64_t>(a.shares) * kWaves;
+        const int64_t each = (steps + turns - 1) / turns, turn = static_cast<int64_t>(share) * kWaves + wave;
+        const int64_t mine_from = g_from + min(turn * each, steps), mine_to = g_from + min(turn * each + each, steps);
+        float acc[2 * N - 1] = {};
         for (int64_t b = 0; b < a.batch; ++b) {
             const int64_t keys = length_of(a.key_lengths, b, a.keys), queries = length_of(a.query_lengths, b, a.queries);
-            const char* s = a.scores + (b * a.s_batch + h * a.s_head) * ElemBytes<ST>::value;
-            for (int64_t i = max(from, -diagonal); i < to && i < queries && i + diagonal < keys; ++i)
-                sum += load_one<ST>(s + (i * a.s_query + i + diagonal) * ElemBytes<ST>::value);
+            const char* s = scores + b * a.s_batch * ElemBytes<ST>::value;
+            for (int64_t g = mine_from; g < mine_to; ++g) {
+                const int64_t c = (g + t) * N, i = g * N;
+                if (c < 0 || c >= keys || i >= queries) continue;
+                const char* at = s + (i * a.s_query + c) * ElemBytes<ST>::value;
+                if (c + N <= keys && i + N <= queries) {
+                    Parts<ST, N> v[N];
+#pragma unroll
+                    for (int x = 0; x < N; ++x) v[x] = load_parts<ST, N, true>(at + x * a.s_query * ElemBytes<ST>::value);
+#pragma unroll
+                    for (int x = 0; x < N; ++x) {
+                        float e[N];
+                        widen<ST, N>(v[x], e);
+#pragma unroll
+                        for (int k = 0; k < N; ++k) acc[k - x + N - 1] += e[k];
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < N; ++x) {
+                        float e[N];
+                        load_some<ST, N>(at + x * a.s_query * ElemBytes<ST>::value, i + x < queries ? static_cast<int>(min(keys - c, int64_t(N))) : 0, e);
+#pragma unroll
+                        for (int k = 0; k < N; ++k) acc[k - x + N - 1] += e[k];
+                    }
+                }
+            }
+        }
+        // diagonals of two neighbouring lanes: first each lane's upper ones (and the lowest lane's lower ones), then the others'
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) diagonal[wave][N * lane + k + N - 1] = acc[k + N - 1];
+        if (lane == 0) {
+#pragma unroll
+            for (int k = 0; k < N - 1; ++k) diagonal[wave][k] = acc[k];
+        }
+        __syncthreads();
+        if (lane > 0) {
+#pragma unroll
+            for (int k = 0; k < N - 1; ++k) diagonal[wave][N * lane + k] += acc[k];
+        }
+        __syncthreads();
+        for (int d = threadIdx.x; d < DIAGONALS; d += kThreads) {
+            float sum = diagonal[0][d];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) sum += diagonal[w][d];
+            diagonal[0][d] = sum;
+        }
+        __syncthreads();
+        // buckets go round the threads; those of many diagonals take a wave each
+        const int64_t r0 = t0 * N - Band<N>::low - a.offset;         // of diagonal[0][0]
+        const int64_t top = a.causal ? min(int64_t(0), r0 + DIAGONALS - 1) : r0 + DIAGONALS - 1;
+        for (int k0 = wave * 64; k0 < a.buckets; k0 += kThreads) {
+            int64_t lo = 0, hi = -1;
+            if (k0 + lane < a.buckets) range_of(first, a, k0 + lane, lo, hi);
+            const int d0 = static_cast<int>(max(lo, r0) - r0), n = static_cast<int>(max(min(hi, top) - max(lo, r0) + 1, int64_t(0)));
+            if (n > 0 && n <= 16) {
+                double sum = 0.0;
+                for (int d = 0; d < n; ++d) sum += diagonal[0][d0 + d];
+                sums[k0 + lane] += sum;
+            }
+            for (uint64_t many = __ballot(n > 16); many != 0; many &= many - 1) {
+                const int l = __ffsll(static_cast<unsigned long long>(many)) - 1, from = __shfl(d0, l), count = __shfl(n, l);
+                double sum = 0.0;
+                for (int d = lane; d < count; d += 64) sum += diagonal[0][from + d];
+#pragma unroll
+                for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
+                if (lane == l) sums[k0 + l] += sum;
+            }
         }
     }
-    sums[threadIdx.x] = sum;
-    of[threadIdx.x] = diagonal < a.keys ? bucket_of(first, a, diagonal - a.offset) : -1;
     __syncthreads();
-    for (int k = threadIdx.x; k < a.buckets; k += kThreads) {
-        double total = 0.0;
-        for (int d = 0; d < kThreads; ++d)
-            if (of[d] == k) total += sums[d];
-        a.partial[(static_cast<int64_t>(blockIdx.x) * a.heads + h) * a.buckets + k] = static_cast<float>(total);
-    }
+    for (int k = threadIdx.x; k < a.buckets; k += kThreads) a.partial[(static_cast<int64_t>(part) * a.heads + h) * a.buckets + k] = static_cast<float>(sums[k]);
 }
 
 struct JoinArgs {
@@ -155,13 +243,28 @@ struct JoinArgs {
     int32_t parts, heads, buckets, type, add;
     float scale;
 };
-__global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a) {
-    const int at = blockIdx.x * kThreads + threadIdx.x;
-    if (at >= a.heads * a.buckets) return;
-    const int h = at / a.buckets, k = at % a.buckets;
+// A wave has 64 sums of a share of the parts, kJoinWaves of them meet in LDS.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
+    __shared__ double meet[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = blockIdx.x * 64 + lane, all = a.heads * a.buckets;
     double sum = 0.0;
-    for (int p = 0; p < a.parts; ++p) sum += a.partial[static_cast<int64_t>(p) * a.heads * a.buckets + at];
+    if (at < all) {
+        for (int p = wave; p < a.parts; p += kJoinWaves * 8) {
+            float x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = p + u * kJoinWaves < a.parts ? a.partial[static_cast<int64_t>(p + u * kJoinWaves) * all + at] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sum += x[u];
+        }
+    }
+    meet[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || at >= all) return;
+#pragma unroll
+    for (int w = 1; w < kJoinWaves; ++w) sum += meet[w][lane];
     sum *= a.scale;
+    const int h = at / a.buckets, k = at % a.buckets;
     char* to = a.grad + (k * a.grad_stride + h) * (a.type == DDP_FP32 ? 4 : 2);
     if (a.type == DDP_FP32) store_one<DDP_FP32>(to, static_cast<float>(a.add ? sum + load_one<DDP_FP32>(to) : sum));
     else if (a.type == DDP_FP16) store_one<DDP_FP16>(to, static_cast<float>(a.add ? sum + load_one<DDP_FP16>(to) : sum));
@@ -171,6 +274,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(JoinArgs a) {
 // ---- host ----
 
 constexpr int64_t kRowBlocks = int64_t(1) << 20;
+constexpr int64_t kGradBlocks = 2048, kGradSteps = 4;
 constexpr int64_t kPartBytes = int64_t(1) << 24;     // of the workspace, if 64 parts do not take more
 
 template <int TT>
@@ -353,22 +457,30 @@ int32_t ddp_position_bias_grad(ddp_position_bias* h, int64_t batch, int64_t quer
         a.sides = h->sides;
         a.both = h->both;
         a.causal = causal != 0;
-        const int64_t strips = (queries + keys - 1 + kThreads - 1) / kThreads;
-        if (strips > h->parts) return layer_fail(h, DDP_ERR_UNSUPPORTED, "ddp_position_bias_grad: more diagonals than the workspace has parts for");
-        a.strips = static_cast<int32_t>(strips);
-        a.rows_per_part = std::max<int64_t>(128, (queries + h->parts / strips - 1) / (h->parts / strips));
-        a.row_parts = static_cast<int32_t>((queries + a.rows_per_part - 1) / a.rows_per_part);
-        parts = strips * a.row_parts;
-        const dim3 grid(static_cast<unsigned>(parts), static_cast<unsigned>(h->heads));
-        if (dtype == DDP_FP32) hipLaunchKernelGGL((diagonal_kernel<DDP_FP32>), grid, dim3(kThreads), 0, h->stream, a);
-        else if (dtype == DDP_FP16) hipLaunchKernelGGL((diagonal_kernel<DDP_FP16>), grid, dim3(kThreads), 0, h->stream, a);
-        else hipLaunchKernelGGL((diagonal_kernel<DDP_BF16>), grid, dim3(kThreads), 0, h->stream, a);
+        // lanes of the band: from the one that ends with the last query's first key to the one of the first query's last key, without those
+        // that are all behind the query
+        const int64_t n = dtype == DDP_FP32 ? 4 : 8, groups = (queries + n - 1) / n;
+        int64_t last = (keys + n - 1) / n - 1;
+        if (causal) last = std::min(last, offset + n - 1 >= 0 ? (offset + n - 1) / n : -((-offset) / n));
+        a.band0 = 1 - groups;
+        a.strips = (last - a.band0 + 1 + 63) / 64;
+        if (a.strips > 0) {
+            a.strip_blocks = static_cast<int32_t>(std::min<int64_t>(a.strips, h->parts));
+            const int64_t blocks = static_cast<int64_t>(a.strip_blocks) * h->heads, steps = batch * std::min(groups, last - a.band0 + 1);
+            a.shares = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({kGradBlocks / blocks, h->parts / a.strip_blocks, steps / (kWaves * kGradSteps)})));
+            parts = static_cast<int64_t>(a.strip_blocks) * a.shares;
+            const dim3 grid(static_cast<unsigned>(parts * h->heads));
+            const size_t bytes = static_cast<size_t>(a.buckets) * 8;
+            if (dtype == DDP_FP32) hipLaunchKernelGGL((diagonal_kernel<DDP_FP32>), grid, dim3(kThreads), bytes, h->stream, a);
+            else if (dtype == DDP_FP16) hipLaunchKernelGGL((diagonal_kernel<DDP_FP16>), grid, dim3(kThreads), bytes, h->stream, a);
+            else hipLaunchKernelGGL((diagonal_kernel<DDP_BF16>), grid, dim3(kThreads), bytes, h->stream, a);
+        }
         LAYER_HIP(h, hipGetLastError());
     } else if (accumulate) {
         return DDP_OK;
     }
     JoinArgs j{h->partial, static_cast<char*>(grad), grad_stride, static_cast<int32_t>(parts), h->heads, h->buckets, grad_dtype, accumulate != 0, scale};
-    hipLaunchKernelGGL(join_kernel, dim3(static_cast<unsigned>((h->heads * h->buckets + kThreads - 1) / kThreads)), dim3(kThreads), 0, h->stream, j);
+    hipLaunchKernelGGL(join_kernel, dim3(static_cast<unsigned>((h->heads * h->buckets + 63) / 64)), dim3(64 * kJoinWaves), 0, h->stream, j);
     LAYER_HIP(h, hipGetLastError());
     return DDP_OK;
 }
