@@ -74,7 +74,8 @@ struct BiasArgs {
     float* partial;
     int64_t batch, queries, keys, offset, table_stride, s_batch, s_head, s_query;
     int64_t band0, strips;                       // of the gradient: the first lane of the first strip
-    int32_t heads, buckets, sides, both, causal, add, strip_blocks, shares;
+    int64_t tiles, plane_tiles, col_tiles;       // of the bias
+    int32_t heads, buckets, sides, both, causal, strip_blocks, shares, rows, cols, log2_cols;
     float scale, masked;
 };
 
@@ -94,26 +95,76 @@ __device__ __forceinline__ int64_t length_of(const int32_t* lengths, int64_t b, 
     return n < 0 ? 0 : n < most ? n : most;
 }
 
-// A block a row of the scores, one element a thread.
-template <int TT, int OT>
+// ---- bias ----
+//
+// A block has `cols` vectors of N keys side by side and `down` row groups below each other in turn, `rows` rows each.  The biases of its
+// diagonals are looked up once, into LDS; a thread goes down its rows in steps of N, in which its vector slides over 2 N - 1 diagonals: N new
+// ones a step, N stores of 16 bytes.
+
+constexpr int kTileDiagonals = 4096;
+template <int DT> struct VectorOf { static constexpr int value = DT == DDP_FP32 ? 4 : 8; };
+
+template <int TT, int OT, bool ADD>
 __global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
+    constexpr int N = VectorOf<OT>::value;
+    __shared__ __attribute__((aligned(16))) float of[kTileDiagonals];
     __shared__ int32_t first[kMaxBuckets];
     for (int k = threadIdx.x; k < a.sides; k += kThreads) first[k] = a.first[k];
-    __syncthreads();
-    const int64_t rows = a.batch * a.heads * a.queries;
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const int64_t i = row % a.queries, h = row / a.queries % a.heads, b = row / a.queries / a.heads;
-        const int64_t keys = length_of(a.key_lengths, b, a.keys);
-        char* out = a.scores + (b * a.s_batch + h * a.s_head + i * a.s_query) * ElemBytes<OT>::value;
-        for (int64_t j = threadIdx.x; j < a.keys; j += kThreads) {
-            const int64_t r = j - i - a.offset;
-            char* to = out + j * ElemBytes<OT>::value;
-            float x = a.masked;
-            if (j < keys && !(a.causal && r > 0)) {
-                x = load_one<TT>(a.table + (bucket_of(first, a, r) * a.table_stride + h) * ElemBytes<TT>::value) * a.scale;
-                if (a.add) x += load_one<OT>(to);
+    const int x = threadIdx.x & (a.cols - 1), y = threadIdx.x >> a.log2_cols;
+    const int high = (kThreads >> a.log2_cols) * a.rows, wide = a.cols * N;
+    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+        const int64_t in_plane = tile % a.plane_tiles, plane = tile / a.plane_tiles, h = plane % a.heads, b = plane / a.heads;
+        const int64_t c0 = in_plane % a.col_tiles * wide, i0 = in_plane / a.col_tiles * high;
+        const int rows_here = static_cast<int>(min(a.queries - i0, int64_t(high))), cols_here = static_cast<int>(min(a.keys - c0, int64_t(wide)));
+        // of[d]: of the diagonal that ends in the tile's first column d - high + 1 rows from its first row
+        const int64_t r0 = c0 - i0 - (high - 1) - a.offset;
+        __syncthreads();
+        for (int d = high - rows_here + threadIdx.x; d < high - 1 + cols_here; d += kThreads) {
+            const int64_t r = r0 + d;
+            float v = load_one<TT>(a.table + (bucket_of(first, a, r) * a.table_stride + h) * ElemBytes<TT>::value) * a.scale;
+            if (!ADD && a.causal && r > 0) v = a.masked;
+            of[d] = v;
+        }
+        __syncthreads();
+        const int64_t c = c0 + x * N;
+        if (c >= a.keys) continue;
+        const int have = static_cast<int>(min(a.keys - c, int64_t(N)));
+        const int seen = static_cast<int>(max(min(length_of(a.key_lengths, b, a.keys) - c, int64_t(N)), int64_t(0)));      // of the vector's keys
+        const int64_t i_first = i0 + y * a.rows, i_end = min(i_first + a.rows, a.queries);
+        const int at = x * N - y * a.rows + high - 1;                // of element 0 in the thread's first row
+        char* out = a.scores + (b * a.s_batch + h * a.s_head + i_first * a.s_query + c) * ElemBytes<OT>::value;
+        for (int g = 0; i_first + g < i_end; g += N) {
+            const int rows = static_cast<int>(min(i_end - i_first - g, int64_t(N)));
+            float window[2 * N - 1];                                 // of element e in row k: e - k + N - 1
+#pragma unroll
+            for (int k = 0; k < 2 * N - 1; ++k) window[k] = of[at - g - (N - 1) + k];
+            // causal: element e of row k is visible where e - k <= edge
+            const int64_t behind = i_first + g + a.offset - c;
+            const int edge = a.causal ? static_cast<int>(max(min(behind, int64_t(N)), int64_t(-N))) : N;
+            Parts<OT, N> there[N];                                   // all on the way together
+            if constexpr (ADD) {
+                if (have == N) {
+#pragma unroll
+                    for (int k = 0; k < N; ++k)
+                        if (k < rows) there[k] = load_parts<OT, N>(out + static_cast<int64_t>(g + k) * a.s_query * ElemBytes<OT>::value);
+                }
             }
-            store_one<OT>(to, x);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                if (k >= rows) break;
+                char* to = out + static_cast<int64_t>(g + k) * a.s_query * ElemBytes<OT>::value;
+                float v[N];
+                if constexpr (ADD) {
+                    if (have == N) widen<OT, N>(there[k], v);
+                    else load_some<OT, N>(to, have, v);
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if constexpr (ADD) v[e] = e < seen && e - k <= edge ? window[e - k + N - 1] + v[e] : a.masked;
+                    else v[e] = e < seen ? window[e - k + N - 1] : a.masked;
+                }
+                store_some<OT, N, !ADD>(to, have, v);
+            }
         }
     }
 }
@@ -273,17 +324,37 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
 
 // ---- host ----
 
-constexpr int64_t kRowBlocks = int64_t(1) << 20;
+constexpr int64_t kMaxTiles = int64_t(1) << 20, kTiles = 2048;
+constexpr int kTileRows = 64;
 constexpr int64_t kGradBlocks = 2048, kGradSteps = 4;
 constexpr int64_t kPartBytes = int64_t(1) << 24;     // of the workspace, if 64 parts do not take more
 
-template <int TT>
-hipError_t launch_apply(ddp_position_bias* h, const BiasArgs& a, int out) {
-    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(a.batch * a.heads * a.queries, kRowBlocks));
-    if (out == DDP_FP32) hipLaunchKernelGGL((apply_kernel<TT, DDP_FP32>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
-    else if (out == DDP_FP16) hipLaunchKernelGGL((apply_kernel<TT, DDP_FP16>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
-    else hipLaunchKernelGGL((apply_kernel<TT, DDP_BF16>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
+template <int TT, int OT>
+hipError_t launch_apply(ddp_position_bias* h, BiasArgs a, bool add) {
+    constexpr int N = VectorOf<OT>::value;
+    const int64_t vectors = (a.keys + N - 1) / N, planes = a.batch * a.heads;
+    while (a.log2_cols < 8 && (1 << a.log2_cols) < vectors) ++a.log2_cols;
+    a.cols = 1 << a.log2_cols;
+    const int down = kThreads >> a.log2_cols;
+    a.col_tiles = (vectors + a.cols - 1) / a.cols;
+    // as many rows a thread as leave enough tiles and fit the table
+    a.rows = N;
+    while (a.rows < kTileRows && (2 * a.rows * down + a.cols * N <= kTileDiagonals) && a.rows * down < a.queries &&
+           planes * a.col_tiles * ((a.queries + 2 * a.rows * down - 1) / (2 * a.rows * down)) >= kTiles)
+        a.rows *= 2;
+    const int64_t high = static_cast<int64_t>(a.rows) * down;
+    a.plane_tiles = a.col_tiles * ((a.queries + high - 1) / high);
+    a.tiles = planes * a.plane_tiles;
+    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(a.tiles, kMaxTiles));
+    if (add) hipLaunchKernelGGL((apply_kernel<TT, OT, true>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
+    else hipLaunchKernelGGL((apply_kernel<TT, OT, false>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
     return hipGetLastError();
+}
+template <int TT>
+hipError_t launch_apply(ddp_position_bias* h, const BiasArgs& a, int out, bool add) {
+    if (out == DDP_FP32) return launch_apply<TT, DDP_FP32>(h, a, add);
+    if (out == DDP_FP16) return launch_apply<TT, DDP_FP16>(h, a, add);
+    return launch_apply<TT, DDP_BF16>(h, a, add);
 }
 
 bool out_of_reach(int64_t n, int64_t stride) { return n > 1 && stride > (int64_t(1) << 46) / (n - 1); }
@@ -412,12 +483,11 @@ int32_t ddp_position_bias_apply(ddp_position_bias* h, int64_t batch, int64_t que
     a.sides = h->sides;
     a.both = h->both;
     a.causal = causal != 0;
-    a.add = accumulate != 0;
     a.scale = scale;
     a.masked = masked;
-    LAYER_HIP(h, table_dtype == DDP_FP32   ? launch_apply<DDP_FP32>(h, a, out_dtype)
-                 : table_dtype == DDP_FP16 ? launch_apply<DDP_FP16>(h, a, out_dtype)
-                                           : launch_apply<DDP_BF16>(h, a, out_dtype));
+    LAYER_HIP(h, table_dtype == DDP_FP32   ? launch_apply<DDP_FP32>(h, a, out_dtype, accumulate != 0)
+                 : table_dtype == DDP_FP16 ? launch_apply<DDP_FP16>(h, a, out_dtype, accumulate != 0)
+                                           : launch_apply<DDP_BF16>(h, a, out_dtype, accumulate != 0));
     return DDP_OK;
 }
 
