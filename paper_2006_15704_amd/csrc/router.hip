@@ -28,7 +28,7 @@ struct RouteArgs {
     int64_t tokens, stride;
     int32_t experts, chosen, groups, kept, top, score, renormalise, weights_type;
     int32_t log2_lanes, each, log2_group, listed;    // of a team: lanes, experts a lane, lanes a group, candidates
-    int32_t room;                                    // keys in LDS for each wave
+    int32_t room;                                    // keys (or a lane's sorted words) in LDS for each wave
     float scale;
 };
 struct RouteGradArgs {
@@ -36,7 +36,7 @@ struct RouteGradArgs {
     const int32_t* experts_in;
     char* dlogits;
     int64_t tokens, stride, dstride;
-    int32_t experts, chosen, score, renormalise, dweights_type;
+    int32_t experts, chosen, score, renormalise, dweights_type, log2_lanes;
     float scale;
 };
 
@@ -87,8 +87,8 @@ __device__ __forceinline__ double score64(int score, float x, float largest, dou
     if (score == DDP_SCORE_SIGMOID) return 1.0 / (1.0 + exp(-static_cast<double>(x)));
     return x == kMasked ? 0.0 : exp(static_cast<double>(x) - largest) / sum;
 }
-__device__ __forceinline__ double key64(float x, double s, const float* bias, int e) {
-    const double key = s + (bias != nullptr ? static_cast<double>(bias[e]) : 0.0);
+__device__ __forceinline__ double key64(float x, double s, double bias) {
+    const double key = s + bias;
     return x != kMasked && key > kNone ? key : kNone;            // (NaN is not above)
 }
 
@@ -106,7 +106,7 @@ __device__ void route_token(const RouteArgs& a, int64_t t, double* keys, int32_t
         for (int e = lane; e < a.experts; e += 64) sum += logit(e) == kMasked ? 0.0 : exp(static_cast<double>(logit(e)) - largest);
         sum = wave_sum(sum);
     }
-    for (int e = lane; e < a.experts; e += 64) keys[e] = key64(logit(e), score64(a.score, logit(e), largest, sum), a.bias, e);
+    for (int e = lane; e < a.experts; e += 64) keys[e] = key64(logit(e), score64(a.score, logit(e), largest, sum), a.bias != nullptr ? static_cast<double>(a.bias[e]) : 0.0);
     wave_meets();
     auto best = [&](auto open, double& k, int& at) {
         k = kNone;
@@ -197,8 +197,8 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 // A team of 1 to 64 lanes has up to kEach neighbouring experts a lane.  Keys in binary32 become words that sort as they do, with the place
 // in the lane for their last four bits; a lane sorts its own, and the team takes the largest head, as often as there are candidates: two more than
 // are chosen.  Where the candidates' keys are all further apart than the error of a binary32 key, their order is that of binary64.
-// Where not, the candidates alone are put in order in binary64.  And where that leaves open whether all that belong are among them (the rest comes as near, or
-// the groups do), a wave does the token over: one token in some thousands of ordinary logits.
+// Where not, the candidates alone (or the groups) are put in order in binary64.  And where that leaves open whether all that belong are among them, a wave
+// does the token over: one token in some thousands of 16-bit logits, hardly any other.
 
 constexpr int kEach = 16, kSpare = 2;
 // A key's error in parts of 2^-24 of the largest score and bias: exp, sum and quotient of a softmax over 1024 under 30, the key's
@@ -270,9 +270,11 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
     extern __shared__ double keys[];                 // [kWaves][room], then candidates and counts
     const int lanes = 1 << a.log2_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> a.log2_lanes, teams = kThreads >> a.log2_lanes;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    uint32_t* word = reinterpret_cast<uint32_t*>(keys + kWaves * a.room) + team * a.listed;        // of each candidate: its key, then its weight
-    int32_t* at = reinterpret_cast<int32_t*>(keys + kWaves * a.room) + (teams + team) * a.listed;  // its expert, or -1
-    int32_t* counts = reinterpret_cast<int32_t*>(keys + kWaves * a.room) + 2 * teams * a.listed;
+    char* behind = reinterpret_cast<char*>(keys + kWaves * a.room);
+    uint32_t* word = reinterpret_cast<uint32_t*>(behind) + team * a.listed;          // of each candidate: its key, then its weight
+    int32_t* at = reinterpret_cast<int32_t*>(behind) + (teams + team) * a.listed;    // its expert, or -1
+    int32_t* counts = reinterpret_cast<int32_t*>(behind) + 2 * teams * a.listed;
+    uint32_t* sorted = reinterpret_cast<uint32_t*>(keys + wave * a.room) + lane;     // the lane's words, 64 apart
     clear_counts(a, counts);
     const int e0 = l * a.each, mine = max(min(a.experts - e0, a.each), 0);
     float bias[EACH], of_bias = 0.0f;
@@ -326,6 +328,13 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
         }
         sort_words<EACH>(w);
         bool again = false;                          // the token is for a wave
+        const int of_team0 = lane & ~(lanes - 1);
+        double sum64 = 0.0;                          // of the softmax, where it is asked for
+        auto take_sum64 = [&]() {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) sum64 += x[i] == kMasked ? 0.0 : exp(static_cast<double>(x[i]) - largest);
+            for (int d = 1; d < lanes; d <<= 1) sum64 += __shfl_xor(sum64, d);
+        };
         if (a.kept < a.groups) {
             float first = w[0] != 0 ? key_of(w[0]) : kMasked, second = kMasked;
             if constexpr (EACH > 1) second = w[1] != 0 ? key_of(w[1]) : kMasked;
@@ -338,34 +347,63 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
             const int group = l >> a.log2_group;
             int before = 0;
             for (int g = 0; g < a.groups; ++g) {
-                const float r = __shfl(rank, (lane & ~(lanes - 1)) + (g << a.log2_group));
+                const float r = __shfl(rank, of_team0 + (g << a.log2_group));
                 before += r > rank || (r == rank && g < group);
             }
-            const bool open = before < a.kept;
-            const float worst = -team_max(a.log2_lanes, open && group < a.groups ? -rank : kMasked);
-            const float next = team_max(a.log2_lanes, !open && group < a.groups ? rank : kMasked);
-            again = next > kMasked && !(worst - next > 2.0f * apart);
-            if (!open) {
+            const float worst = -team_max(a.log2_lanes, before < a.kept && group < a.groups ? -rank : kMasked);
+            const float next = team_max(a.log2_lanes, before >= a.kept && group < a.groups ? rank : kMasked);
+            const bool close = live && next > kMasked && !(worst - next > 2.0f * apart);
+            if (__ballot(close) != 0) {
+                if (a.score == DDP_SCORE_SOFTMAX) take_sum64();
+                double first64 = kNone, second64 = kNone;
+#pragma unroll 1
+                for (int i = 0; i < EACH; ++i) {
+                    float v = kMasked, of_v = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < EACH; ++j)
+                        if (j == i) {
+                            v = x[j];
+                            of_v = bias[j];
+                        }
+                    const double key = key64(v, score64(a.score, v, largest, sum64), static_cast<double>(of_v));
+                    second64 = fmax(fmin(first64, key), second64);
+                    first64 = fmax(first64, key);
+                }
+                for (int d = 1; d < 1 << a.log2_group; d <<= 1) {
+                    const double f = __shfl_xor(first64, d), g = __shfl_xor(second64, d);
+                    second64 = fmax(fmin(first64, f), fmax(second64, g));
+                    first64 = fmax(first64, f);
+                }
+                const double rank64 = a.top == 2 && second64 > kNone ? first64 + second64 : first64;
+                int before64 = 0;
+                for (int g = 0; g < a.groups; ++g) {
+                    const double r = __shfl(rank64, of_team0 + (g << a.log2_group));
+                    before64 += r > rank64 || (r == rank64 && g < group);
+                }
+                if (close) before = before64;
+            }
+            if (before >= a.kept) {
 #pragma unroll
                 for (int i = 0; i < EACH; ++i) w[i] = 0;
             }
         }
+#pragma unroll
+        for (int i = 1; i < EACH; ++i) sorted[i * 64] = w[i];
         float left = kMasked;                        // the largest key behind the candidates
+        int taken = 0;
         for (int n = 0; n <= a.listed; ++n) {
             const uint32_t head = w[0] >> 4, top = team_max(a.log2_lanes, head);
             if (n == a.listed) {
                 if (top != 0) left = key_of(top << 4);
                 break;
             }
-            const uint64_t same = __ballot(head == top) >> (lane & ~(lanes - 1));
-            const bool winner = __ffsll(static_cast<unsigned long long>(same)) - 1 == l;
-            if (winner) {
+            const uint64_t same = __ballot(head == top) >> of_team0;
+            if (__ffsll(static_cast<unsigned long long>(same)) - 1 == l) {
                 word[n] = w[0];
                 at[n] = top != 0 ? e0 + 15 - static_cast<int>(w[0] & 15u) : -1;
+                ++taken;
+                w[0] = taken < EACH ? sorted[taken * 64] : 0u;
             }
-#pragma unroll
-            for (int i = 0; i < EACH - 1; ++i) w[i] = winner ? w[i + 1] : w[i];
-            if (winner) w[EACH - 1] = 0;
         }
         wave_meets();
         // candidates go round the lanes: are two of the first a.chosen + 1 too near each other?
@@ -378,23 +416,18 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
             }
         }
         const uint64_t of_team = lanes == 64 ? ~uint64_t(0) : (uint64_t(1) << lanes) - 1;
-        const bool close = (__ballot(near) >> (lane & ~(lanes - 1)) & of_team) != 0;
+        const bool close = (__ballot(near) >> of_team0 & of_team) != 0;
         bool order64 = false;
-        if (__ballot(close && !again && live) != 0) {
-            order64 = close && !again;
-            double sum64 = 1.0;
-            if (a.score == DDP_SCORE_SOFTMAX && a.bias != nullptr) {
-                sum64 = 0.0;
-#pragma unroll
-                for (int i = 0; i < EACH; ++i) sum64 += x[i] == kMasked ? 0.0 : exp(static_cast<double>(x[i]) - largest);
-                for (int d = 1; d < lanes; d <<= 1) sum64 += __shfl_xor(sum64, d);
-            }
+        if (__ballot(close && live) != 0) {
+            order64 = close;
+            if (a.score == DDP_SCORE_SOFTMAX && a.bias != nullptr && sum64 == 0.0) take_sum64();
+            if (a.bias == nullptr) sum64 = 1.0;
             // the wave's room for keys holds the candidates'
             double* exact = keys + wave * a.room + (team & ((64 >> a.log2_lanes) - 1)) * a.listed;
             for (int n = l; n < a.listed; n += lanes) {
                 const int e = at[n];
                 const float v = e >= 0 && live ? load_one<LT>(row + e * ElemBytes<LT>::value) : kMasked;
-                exact[n] = e >= 0 ? key64(v, score64(a.score, v, largest, sum64), a.bias, e) : kNone;
+                exact[n] = e >= 0 ? key64(v, score64(a.score, v, largest, sum64), a.bias != nullptr ? static_cast<double>(a.bias[e]) : 0.0) : kNone;
             }
             wave_meets();
             if (order64) {
@@ -413,7 +446,7 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
                 again = left > kMasked && !(static_cast<float>(last * scale64) - left > apart);
             }
             // one lane of a team decides for all
-            again = (__ballot(again) >> (lane & ~(lanes - 1)) & of_team) != 0;
+            again = (__ballot(again) >> of_team0 & of_team) != 0;
         }
         wave_meets();
         if (live && !again) {
@@ -457,70 +490,99 @@ __global__ __launch_bounds__(kThreads) void clear_kernel(int32_t* counts, int n)
     for (int e = threadIdx.x; e < n; e += kThreads) counts[e] = 0;
 }
 
+// A token's gradient by a team of lanes with EACH neighbouring experts each.  What the chosen experts get is put together in a row in LDS, which is zeros
+// otherwise, and everyone reads what is theirs; of sigmoids nothing else is computed.
 template <int LT, int EACH>
 __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + wave; t < a.tokens; t += static_cast<int64_t>(gridDim.x) * kWaves) {
-        float s[EACH], d[EACH] = {}, largest = -__builtin_huge_valf();
+    extern __shared__ float lds[];                   // [teams]: the row, then of the chosen: gradient, score, expert
+    const int lanes = 1 << a.log2_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> a.log2_lanes, teams = kThreads >> a.log2_lanes;
+    constexpr int STEP = EACH + 4;                   // (lanes four words further apart: fewer of them share a bank)
+    float* row = lds + team * (lanes * STEP + 3 * a.chosen);
+    float* of = row + lanes * STEP;
+    float* score = of + a.chosen;
+    int32_t* at = reinterpret_cast<int32_t*>(score + a.chosen);
+    auto place = [](int e) { return e / EACH * STEP + e % EACH; };
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int e = i * 64 + lane;
-            s[i] = e < a.experts ? load_one<LT>(a.logits + (t * a.stride + e) * ElemBytes<LT>::value) : -__builtin_huge_valf();
-            largest = fmaxf(largest, s[i]);
-        }
+    for (int i = 0; i < EACH; ++i) row[l * STEP + i] = 0.0f;
+    const int e0 = l * EACH, mine = max(min(a.experts - e0, EACH), 0);
+    const int of_team0 = static_cast<int>(threadIdx.x & 63) & ~(lanes - 1);
+    const uint64_t of_team = lanes == 64 ? ~uint64_t(0) : (uint64_t(1) << lanes) - 1;
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * teams; base < a.tokens; base += static_cast<int64_t>(gridDim.x) * teams) {
+        const int64_t t = base + team;
+        const bool live = t < a.tokens;
+        const char* from = a.logits + t * a.stride * ElemBytes<LT>::value;
+        float s[EACH], largest = 0.0f, part = 0.0f;
         if (a.score == DDP_SCORE_SOFTMAX) {
-            largest = wave_max(largest);
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                s[i] = s[i] == -__builtin_huge_valf() ? 0.0f : expf(s[i] - largest);
-                sum += s[i];
-            }
-            sum = wave_sum(sum);
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) s[i] /= sum;
-        }
-        float left[EACH];                            // 1 - s of the sigmoid, without the difference
-        if (a.score == DDP_SCORE_SIGMOID) {
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const float x = s[i], z = expf(-fabsf(x)), big = 1.0f / (1.0f + z), small = z / (1.0f + z);
-                s[i] = x < 0.0f ? small : big;
-                left[i] = x < 0.0f ? big : small;
-                if (x != x) s[i] = left[i] = x;
-            }
-        }
-        // lane n: the n-th choice
-        const int expert = lane < a.chosen ? a.experts_in[t * a.chosen + lane] : -1;
-        const bool named = expert >= 0 && expert < a.experts;
-        float w = 0.0f;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const float v = __shfl(s[i], expert & 63);
-            if (named && expert >> 6 == i) w = v;
-        }
-        float g = named ? load_weight(a.dweights, a.dweights_type, t * a.chosen + lane) * a.scale : 0.0f;
-        if (a.renormalise) {
-            const float sum = wave_sum(w), dot = wave_sum(g * w);
-            g = named && sum > 0.0f ? (g - dot / sum) / sum : 0.0f;
-        }
-        const float dot = a.score == DDP_SCORE_SOFTMAX ? wave_sum(g * w) : 0.0f;
-        const bool any = __ballot(named) != 0;
-        for (int n = 0; n < a.chosen; ++n) {
-            const int e = __shfl(expert, n);
-            const float v = __shfl(g, n);
-            if (e < 0 || e >= a.experts) continue;
+            load_some<LT, EACH>(from + e0 * ElemBytes<LT>::value, live ? mine : 0, s);
+            largest = kMasked;
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
-                if (e == i * 64 + lane) d[i] += v;
+                if (i < mine) largest = fmaxf(largest, s[i]);
+            largest = team_max(a.log2_lanes, largest);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                s[i] = i >= mine || s[i] == kMasked ? 0.0f : expf(s[i] - largest);
+                part += s[i];
+            }
+            part = 1.0f / team_sum(a.log2_lanes, part);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) s[i] *= part;
         }
+        // the chosen go round the lanes
+        bool any = false;
+        float all = 0.0f, dot = 0.0f;
+        for (int n = l; n < a.chosen; n += lanes) {
+            const int e = live ? a.experts_in[t * a.chosen + n] : -1;
+            const bool named = e >= 0 && e < a.experts;
+            float w = 0.0f, g = 0.0f;
+            if (named) {
+                const float x = load_one<LT>(from + e * ElemBytes<LT>::value);
+                w = a.score == DDP_SCORE_SIGMOID ? 1.0f / (1.0f + expf(-x)) : x == kMasked ? 0.0f : expf(x - largest) * part;
+                g = load_weight(a.dweights, a.dweights_type, t * a.chosen + n) * a.scale;
+            }
+            any |= named;
+            all += w;
+            dot += g * w;
+            at[n] = named ? e : -1;
+            of[n] = g;
+            score[n] = w;
+        }
+        any = (__ballot(any) >> of_team0 & of_team) != 0;
+        if (a.renormalise) {
+            all = team_sum(a.log2_lanes, all);
+            dot = team_sum(a.log2_lanes, dot);
+            const float mean = dot / all;
+            dot = 0.0f;
+            for (int n = l; n < a.chosen; n += lanes) {
+                const float g = at[n] >= 0 && all > 0.0f ? (of[n] - mean) / all : 0.0f;
+                of[n] = g;
+                dot += g * score[n];
+            }
+        }
+        dot = a.score == DDP_SCORE_SOFTMAX ? team_sum(a.log2_lanes, dot) : 0.0f;
+        wave_meets();
+        for (int n = l; n < a.chosen; n += lanes) {
+            const int e = at[n];
+            if (e < 0) continue;
+            float sum = 0.0f;                        // (an expert that is named twice)
+            for (int m = 0; m < a.chosen; ++m) sum += at[m] == e ? of[m] : 0.0f;
+            if (a.score == DDP_SCORE_SIGMOID) {
+                const float x = load_one<LT>(from + e * ElemBytes<LT>::value);
+                sum *= score[n] * (1.0f / (1.0f + expf(x)));     // 1 - s, without the difference
+            }
+            row[place(e)] = sum;
+        }
+        wave_meets();
+        float d[EACH];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int e = i * 64 + lane;
-            float x = a.score == DDP_SCORE_SOFTMAX ? s[i] * (d[i] - dot) : d[i] * s[i] * left[i];
-            if (!any) x = 0.0f;
-            if (e < a.experts) store_one<LT>(a.dlogits + (t * a.dstride + e) * ElemBytes<LT>::value, x);
+            d[i] = row[l * STEP + i];
+            if (a.score == DDP_SCORE_SOFTMAX) d[i] = any ? s[i] * (d[i] - dot) : 0.0f;
         }
+        if (live && mine > 0) store_some<LT, EACH>(a.dlogits + (t * a.dstride + e0) * ElemBytes<LT>::value, mine, d);
+        wave_meets();
+        for (int n = l; n < a.chosen; n += lanes)
+            if (at[n] >= 0) row[place(at[n])] = 0.0f;
     }
 }
 
@@ -558,7 +620,7 @@ bool find_team(RouteArgs& a) {
     while (a.each << a.log2_lanes < a.experts) ++a.log2_lanes;
     if (a.log2_lanes > 6) return false;
     a.listed = std::min(a.chosen + kSpare, a.experts);
-    a.room = std::max(a.experts, (64 >> a.log2_lanes) * a.listed);
+    a.room = std::max({a.experts, (64 >> a.log2_lanes) * a.listed, 32 * (a.each > 8 ? 16 : a.each > 4 ? 8 : a.each > 2 ? 4 : a.each)});
     return true;
 }
 template <int LT>
@@ -579,19 +641,16 @@ hipError_t launch_route(ddp_router* h, RouteArgs a) {
     else hipLaunchKernelGGL((route_team_kernel<LT, 1>), blocks, threads, bytes, h->stream, a);
     return hipGetLastError();
 }
-template <int LT, int EACH>
-hipError_t launch_grad(ddp_router* h, const RouteGradArgs& a, unsigned blocks) {
-    hipLaunchKernelGGL((route_grad_kernel<LT, EACH>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
-    return hipGetLastError();
-}
 template <int LT>
-hipError_t launch_grad(ddp_router* h, const RouteGradArgs& a) {
-    const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((a.tokens + kWaves - 1) / kWaves, kBlocks));
-    if (a.experts <= 64) return launch_grad<LT, 1>(h, a, blocks);
-    if (a.experts <= 128) return launch_grad<LT, 2>(h, a, blocks);
-    if (a.experts <= 256) return launch_grad<LT, 4>(h, a, blocks);
-    if (a.experts <= 512) return launch_grad<LT, 8>(h, a, blocks);
-    return launch_grad<LT, 16>(h, a, blocks);
+hipError_t launch_grad(ddp_router* h, RouteGradArgs a) {
+    const int each = a.experts > 256 || (a.experts > 32 && 4 * a.chosen <= a.experts) ? 16 : 4;      // (many chosen take more lanes: their LDS is a team's)
+    while (each << a.log2_lanes < a.experts) ++a.log2_lanes;
+    const int teams = kThreads >> a.log2_lanes;
+    const dim3 blocks(static_cast<unsigned>(std::min<int64_t>((a.tokens + teams - 1) / teams, kBlocks))), threads(kThreads);
+    const size_t bytes = static_cast<size_t>(teams) * (((each + 4) << a.log2_lanes) + 3 * a.chosen) * 4;
+    if (each == 16) hipLaunchKernelGGL((route_grad_kernel<LT, 16>), blocks, threads, bytes, h->stream, a);
+    else hipLaunchKernelGGL((route_grad_kernel<LT, 4>), blocks, threads, bytes, h->stream, a);
+    return hipGetLastError();
 }
 
 int32_t check_tokens(ddp_router* h, int64_t tokens, int32_t dtype, int32_t weights_dtype, int64_t stride) {
