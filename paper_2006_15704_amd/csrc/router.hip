@@ -7,6 +7,7 @@
 #include "layer_host.h"
 
 struct ddp_router : ddp::LayerHandle {
+    int32_t* copies = nullptr;                   // [kCopies][experts] counts, zeros between calls
     int32_t experts = 0, chosen = 0, groups = 0, kept = 0, top = 0, score = 0, renormalise = 0;
     float scale = 1.0f;
 };
@@ -18,15 +19,16 @@ using namespace ddp;
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxExperts = 1024, kMaxChosen = 64, kMaxGroups = 64;
 constexpr int64_t kMaxTokens = INT32_MAX;
+constexpr int kCopies = 16;
 
 struct RouteArgs {
     const char* logits;
     const float* bias;
     int32_t* experts_out;
     char* weights;
-    int32_t* counts;
+    int32_t *counts, *copies;
     int64_t tokens, stride;
-    int32_t experts, chosen, groups, kept, top, score, renormalise, weights_type;
+    int32_t experts, chosen, groups, kept, top, score, renormalise, weights_type, accumulate;
     int32_t log2_lanes, each, log2_group, listed;    // of a team: lanes, experts a lane, lanes a group, candidates
     int32_t room;                                    // keys (or a lane's sorted words) in LDS for each wave
     float scale;
@@ -51,17 +53,29 @@ __device__ __forceinline__ float wave_max(float x) {
     for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
     return x;
 }
+template <int CTRL>
+__device__ __forceinline__ double lane_moved(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b), CTRL, 0xF, 0xF, true));
+    const uint32_t hi = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b >> 32), CTRL, 0xF, 0xF, true));
+    return __builtin_bit_cast(double, static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ __forceinline__ double wave_max(double x) {
+    x = fmax(x, lane_moved<0xB1>(x));                // quad_perm: 1 0 3 2
+    x = fmax(x, lane_moved<0x4E>(x));                // quad_perm: 2 3 0 1
+    x = fmax(x, lane_moved<0x141>(x));               // row_half_mirror
+    x = fmax(x, lane_moved<0x140>(x));               // row_mirror
+    x = fmax(x, __shfl_xor(x, 16));
+    return fmax(x, __shfl_xor(x, 32));
+}
 // The largest key and the lowest index that has it.
 __device__ __forceinline__ void wave_best(double& key, int& at) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const double k = __shfl_xor(key, d);
-        const int i = __shfl_xor(at, d);
-        if (k > key || (k == key && i < at)) {
-            key = k;
-            at = i;
-        }
-    }
+    const double top = wave_max(key);
+    uint64_t here = __ballot(key == top);
+    key = top;
+    int lowest = __builtin_amdgcn_readlane(at, __ffsll(static_cast<unsigned long long>(here)) - 1);
+    for (here &= here - 1; here != 0; here &= here - 1) lowest = min(lowest, __builtin_amdgcn_readlane(at, __ffsll(static_cast<unsigned long long>(here)) - 1));
+    at = lowest;
 }
 __device__ __forceinline__ void store_weight(char* p, int type, int64_t at, float x) {
     if (type == DDP_FP32) store_one<DDP_FP32>(p + at * 4, x);
@@ -82,84 +96,88 @@ constexpr float kMasked = -__builtin_huge_valf();
 
 // ---- a token by a wave, in binary64 ----
 
-// Score and key of an expert from its logit; `largest` and `sum` are the softmax's.
-__device__ __forceinline__ double score64(int score, float x, float largest, double sum) {
-    if (score == DDP_SCORE_SIGMOID) return 1.0 / (1.0 + exp(-static_cast<double>(x)));
-    return x == kMasked ? 0.0 : exp(static_cast<double>(x) - largest) / sum;
-}
-__device__ __forceinline__ double key64(float x, double s, double bias) {
-    const double key = s + bias;
-    return x != kMasked && key > kNone ? key : kNone;            // (NaN is not above)
-}
-
 // keys: of the experts, in LDS.
 template <int LT>
-__device__ void route_token(const RouteArgs& a, int64_t t, double* keys, int32_t* counts) {
+__device__ __forceinline__ void route_token(const RouteArgs& a, int64_t t, double* keys, int32_t* counts) {
     const int lane = threadIdx.x & 63, per_group = a.experts / a.groups;
     const char* row = a.logits + t * a.stride * ElemBytes<LT>::value;
     auto logit = [&](int e) { return load_one<LT>(row + e * ElemBytes<LT>::value); };
-    float largest = kMasked;
-    double sum = 0.0;
-    if (a.score == DDP_SCORE_SOFTMAX) {
+    const bool softmax = a.score == DDP_SCORE_SOFTMAX;
+    float largest = 0.0f;
+    double sum = 1.0;
+    if (softmax) {
+        largest = kMasked;
         for (int e = lane; e < a.experts; e += 64) largest = fmaxf(largest, logit(e));
         largest = wave_max(largest);
-        for (int e = lane; e < a.experts; e += 64) sum += logit(e) == kMasked ? 0.0 : exp(static_cast<double>(logit(e)) - largest);
-        sum = wave_sum(sum);
+        sum = 0.0;
     }
-    for (int e = lane; e < a.experts; e += 64) keys[e] = key64(logit(e), score64(a.score, logit(e), largest, sum), a.bias != nullptr ? static_cast<double>(a.bias[e]) : 0.0);
+    // exp(x - largest) of a softmax, 1 + exp(-x) of a sigmoid
+    auto part = [&](float x) { return softmax ? (x == kMasked ? 0.0 : exp(static_cast<double>(x) - largest)) : 1.0 + exp(-static_cast<double>(x)); };
+    auto score = [&](double part) { return softmax ? part / sum : 1.0 / part; };
+#pragma unroll 1
+    for (int e = lane; e < a.experts; e += 64) {
+        keys[e] = part(logit(e));
+        if (softmax) sum += keys[e];
+    }
+    if (softmax) sum = wave_sum(sum);
+    for (int e = lane; e < a.experts; e += 64) {
+        const double key = score(keys[e]) + (a.bias != nullptr ? static_cast<double>(a.bias[e]) : 0.0);
+        keys[e] = logit(e) != kMasked && key > kNone ? key : kNone;       // (NaN is not above)
+    }
     wave_meets();
-    auto best = [&](auto open, double& k, int& at) {
-        k = kNone;
-        at = kMaxExperts;
-        for (int e = lane; e < a.experts; e += 64)
-            if (keys[e] > k && open(e)) {
-                k = keys[e];
-                at = e;
-            }
-        wave_best(k, at);
-    };
     uint64_t open = ~uint64_t(0);
     if (a.kept < a.groups) {
-        double rank = kNone;                         // lane g: of group g
-        for (int g = 0; g < a.groups; ++g) {
-            double total, k;
-            int first, second;
-            best([&](int e) { return e / per_group == g; }, total, first);
-            if (a.top == 2) {
-                best([&](int e) { return e / per_group == g && e != first; }, k, second);
-                if (k > kNone) total += k;
+        double first = kNone, second = kNone;        // lane g: of group g
+        if (lane < a.groups) {
+#pragma unroll 4
+            for (int i = 0; i < per_group; ++i) {
+                const double k = keys[lane * per_group + i];
+                second = fmax(fmin(first, k), second);
+                first = fmax(first, k);
             }
-            if (lane == g) rank = total;
+            if (a.top == 2 && second > kNone) first += second;
         }
         open = 0;
         for (int n = 0; n < a.kept; ++n) {
-            double k = rank;
+            double k = first;
             int at = lane;
             wave_best(k, at);
             if (!(k > kNone)) break;
             open |= uint64_t(1) << at;
-            if (lane == at) rank = kNone;
+            if (lane == at) first = kNone;
         }
+        for (int e = lane; e < a.experts; e += 64)
+            if (!(open >> (e / per_group) & 1)) keys[e] = kNone;
     }
-    double mine = 0.0, all = 0.0;                    // lane n: of the n-th choice
-    int expert = -1;
+    double best = kNone;                             // of the lane's keys
+    int best_at = kMaxExperts;
+    auto find = [&]() {
+        best = kNone;
+        best_at = kMaxExperts;
+#pragma unroll 4
+        for (int e = lane; e < a.experts; e += 64)
+            if (keys[e] > best) {
+                best = keys[e];
+                best_at = e;
+            }
+    };
+    find();
+    int expert = -1;                                 // lane n: the n-th choice
     for (int n = 0; n < a.chosen; ++n) {
-        double k;
-        int at;
-        best([&](int e) { return (open >> (e / per_group) & 1) != 0; }, k, at);
+        double k = best;
+        int at = best_at;
+        wave_best(k, at);
         if (!(k > kNone)) break;
-        const double w = score64(a.score, logit(at), largest, sum);
-        all += w;
-        if (lane == n) {
-            mine = w;
-            expert = at;
+        if (lane == n) expert = at;
+        if (at == best_at) {
+            keys[at] = kNone;
+            find();
         }
-        wave_meets();
-        if (lane == 0) keys[at] = kNone;
-        wave_meets();
     }
+    double w = lane < a.chosen && expert >= 0 ? score(part(logit(expert))) : 0.0;
+    const double all = wave_sum(w);
     if (lane < a.chosen) {
-        double w = mine * a.scale;
+        w *= a.scale;
         if (a.renormalise) w = all > 0.0 ? w / all : 0.0;
         a.experts_out[t * a.chosen + lane] = expert;
         store_weight(a.weights, a.weights_type, t * a.chosen + lane, static_cast<float>(w));
@@ -173,23 +191,41 @@ __device__ __forceinline__ void clear_counts(const RouteArgs& a, int32_t* counts
     for (int e = threadIdx.x; e < a.experts; e += kThreads) counts[e] = 0;
     __syncthreads();
 }
+// A block alone writes the counts.  More blocks add theirs to copies, which count_kernel sums: 2048 blocks of 256 experts at
+// one copy took 30 us longer.
+template <bool ALONE>
 __device__ __forceinline__ void add_counts(const RouteArgs& a, const int32_t* counts) {
     if (a.counts == nullptr) return;
     __syncthreads();
+    if (ALONE && gridDim.x == 1) {
+        for (int e = threadIdx.x; e < a.experts; e += kThreads) a.counts[e] = counts[e] + (a.accumulate ? a.counts[e] : 0);
+        return;
+    }
+    int32_t* to = a.copies + blockIdx.x % kCopies * a.experts;
     for (int e = threadIdx.x; e < a.experts; e += kThreads)
-        if (counts[e] != 0) atomicAdd(a.counts + e, counts[e]);
+        if (counts[e] != 0) atomicAdd(to + e, counts[e]);
 }
 
-// Groups that no team's lanes divide into.
-template <int LT>
+// All tokens (where no team's lanes divide into the groups), or those that teams have left.
+constexpr int32_t kAgain = -2;
+constexpr int kLooked = 16;                      // tokens that a wave looks through at a time
+template <int LT, bool ALL>
 __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     extern __shared__ double keys[];                 // [kWaves][experts], then the counts
     int32_t* counts = reinterpret_cast<int32_t*>(keys + kWaves * a.experts);
     clear_counts(a, counts);
-    const int wave = threadIdx.x >> 6;
-    for (int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + wave; t < a.tokens; t += static_cast<int64_t>(gridDim.x) * kWaves)
-        route_token<LT>(a, t, keys + wave * a.experts, counts);
-    add_counts(a, counts);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    double* mine = keys + wave * a.experts;
+    if constexpr (ALL) {
+        for (int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + wave; t < a.tokens; t += static_cast<int64_t>(gridDim.x) * kWaves) route_token<LT>(a, t, mine, counts);
+    } else {
+        for (int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kWaves + wave) * kLooked; t0 < a.tokens; t0 += static_cast<int64_t>(gridDim.x) * kWaves * kLooked) {
+            const bool left = lane < kLooked && t0 + lane < a.tokens && a.experts_out[(t0 + lane) * a.chosen] == kAgain;
+            for (uint64_t some = __ballot(left); some != 0; some &= some - 1)
+                route_token<LT>(a, t0 + __ffsll(static_cast<unsigned long long>(some)) - 1, mine, counts);
+        }
+    }
+    add_counts<ALL>(a, counts);
 }
 
 // ---- a token by a team ----
@@ -197,13 +233,15 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 // A team of 1 to 64 lanes has up to kEach neighbouring experts a lane.  Keys in binary32 become words that sort as they do, with the place
 // in the lane for their last four bits; a lane sorts its own, and the team takes the largest head, as often as there are candidates: two more than
 // are chosen.  Where the candidates' keys are all further apart than the error of a binary32 key, their order is that of binary64.
-// Where not, the candidates alone (or the groups) are put in order in binary64.  And where that leaves open whether all that belong are among them, a wave
-// does the token over: one token in some thousands of 16-bit logits, hardly any other.
+// Where not, the candidates are ordered again by whole binary32 keys, equal logits with equal biases by their index.  Where that too leaves it open, or the
+// groups' scores come near each other, a wave does the token over in binary64: of 256 normal logits in eight groups, one token in 400.
 
 constexpr int kEach = 16, kSpare = 2;
 // A key's error in parts of 2^-24 of the largest score and bias: exp, sum and quotient of a softmax over 1024 under 30, the key's
-// rounding 1, the bits given to the place 32: two keys 126.
+// rounding and the lift's 6 (a lifted key is up to twice as large), the bits given to the place 64: two keys 200.
 constexpr float kApart = 0x1p-16f;
+// The same of whole keys: 30 and 3 each of a softmax, 5 of a sigmoid.
+constexpr float kNearSoftmax = 0x1p-17f, kNearSigmoid = 0x1p-20f;
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t lane_moved(uint32_t x) {
@@ -234,15 +272,15 @@ __device__ __forceinline__ uint32_t team_max(int log2, uint32_t x) {
     return x;
 }
 
-// Words that sort as the floats do; 0 is below all of them.
-__device__ __forceinline__ uint32_t sortable(float x) {
-    const uint32_t b = as_bits(x);
-    return b ^ (static_cast<uint32_t>(static_cast<int32_t>(b) >> 31) | 0x80000000u);
+// The first lane of a team that is in the mask (one is).
+__device__ __forceinline__ int first_lane(uint64_t mask, int log2_lanes, int of_team0) {
+    if (log2_lanes == 6) return __ffsll(static_cast<unsigned long long>(mask)) - 1;
+    const uint32_t half = of_team0 & 32 ? static_cast<uint32_t>(mask >> 32) : static_cast<uint32_t>(mask);
+    return __ffs(static_cast<int>(half >> (of_team0 & 31))) - 1;
 }
-__device__ __forceinline__ float key_of(uint32_t word) {
-    const uint32_t w = word & ~15u;
-    return as_float(w >> 31 ? w ^ 0x80000000u : ~w);
-}
+
+// A key as a word: positive floats sort as their bits do, so `lift` makes the key positive; 0: no key.
+__device__ __forceinline__ float key_of(uint32_t word, float lift) { return as_float(word & ~15u) - lift; }
 
 // Descending, by odd-even merges.
 template <int N>
@@ -264,16 +302,18 @@ __device__ __forceinline__ void sort_words(uint32_t (&w)[N]) {
 
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
-// EACH: the lane's experts, a.each of them used.
-template <int LT, int EACH>
+// EACH: the lane's experts, a.each of them used.  LANES: the logarithm of a team's lanes, if it is known (the steps of a meeting need no branches then:
+// 65536 tokens of 256 experts 47 us without).
+template <int LT, int EACH, bool HERE, int LANES>
 __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
     extern __shared__ double keys[];                 // [kWaves][room], then candidates and counts
-    const int lanes = 1 << a.log2_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> a.log2_lanes, teams = kThreads >> a.log2_lanes;
+    const int log2_lanes = LANES >= 0 ? LANES : a.log2_lanes, lanes = 1 << log2_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> log2_lanes, teams = kThreads >> log2_lanes;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     char* behind = reinterpret_cast<char*>(keys + kWaves * a.room);
     uint32_t* word = reinterpret_cast<uint32_t*>(behind) + team * a.listed;          // of each candidate: its key, then its weight
     int32_t* at = reinterpret_cast<int32_t*>(behind) + (teams + team) * a.listed;    // its expert, or -1
-    int32_t* counts = reinterpret_cast<int32_t*>(behind) + 2 * teams * a.listed;
+    int32_t* place = reinterpret_cast<int32_t*>(behind) + (2 * teams + team) * a.listed;      // its rank, once ordered
+    int32_t* counts = reinterpret_cast<int32_t*>(behind) + 3 * teams * a.listed;
     uint32_t* sorted = reinterpret_cast<uint32_t*>(keys + wave * a.room) + lane;     // the lane's words, 64 apart
     clear_counts(a, counts);
     const int e0 = l * a.each, mine = max(min(a.experts - e0, a.each), 0);
@@ -283,7 +323,10 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
         bias[i] = a.bias != nullptr && i < mine ? a.bias[e0 + i] : 0.0f;
         of_bias = fmaxf(of_bias, fabsf(bias[i]) < __builtin_huge_valf() ? fabsf(bias[i]) : 0.0f);
     }
-    of_bias = team_max(a.log2_lanes, of_bias);
+    of_bias = team_max(log2_lanes, of_bias);
+    const float lift = of_bias * (1.0f + 0x1p-20f) + 0x1p-60f;       // (above every -bias)
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) bias[i] = i < mine ? bias[i] + lift : kMasked;
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * teams; base < a.tokens; base += static_cast<int64_t>(gridDim.x) * teams) {
         const int64_t t = base + team;
         const bool live = t < a.tokens;
@@ -305,13 +348,13 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
             largest = x[0];
 #pragma unroll
             for (int i = 1; i < EACH; ++i) largest = fmaxf(largest, x[i]);
-            largest = team_max(a.log2_lanes, largest);
+            largest = team_max(log2_lanes, largest);
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
                 s[i] = x[i] == kMasked ? 0.0f : fast_exp(x[i] - largest);
                 sum += s[i];
             }
-            sum = team_sum(a.log2_lanes, sum);
+            sum = team_sum(log2_lanes, sum);
             most = 1.0f / sum;
 #pragma unroll
             for (int i = 0; i < EACH; ++i) s[i] *= most;
@@ -324,20 +367,14 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const float key = s[i] + bias[i];
-            w[i] = x[i] != kMasked && key > kMasked ? (sortable(key) & ~15u) | static_cast<uint32_t>(15 - i) : 0u;
+            w[i] = x[i] != kMasked && key > 0.0f ? (as_bits(key) & ~15u) | static_cast<uint32_t>(15 - i) : 0u;
         }
         sort_words<EACH>(w);
         bool again = false;                          // the token is for a wave
         const int of_team0 = lane & ~(lanes - 1);
-        double sum64 = 0.0;                          // of the softmax, where it is asked for
-        auto take_sum64 = [&]() {
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) sum64 += x[i] == kMasked ? 0.0 : exp(static_cast<double>(x[i]) - largest);
-            for (int d = 1; d < lanes; d <<= 1) sum64 += __shfl_xor(sum64, d);
-        };
         if (a.kept < a.groups) {
-            float first = w[0] != 0 ? key_of(w[0]) : kMasked, second = kMasked;
-            if constexpr (EACH > 1) second = w[1] != 0 ? key_of(w[1]) : kMasked;
+            float first = w[0] != 0 ? key_of(w[0], lift) : kMasked, second = kMasked;
+            if constexpr (EACH > 1) second = w[1] != 0 ? key_of(w[1], lift) : kMasked;
             meet_lanes(a.log2_group, [&](auto move) {
                 const float f = as_float(move(as_bits(first))), g = as_float(move(as_bits(second)));
                 second = fmaxf(fminf(first, f), fmaxf(second, g));
@@ -350,38 +387,9 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
                 const float r = __shfl(rank, of_team0 + (g << a.log2_group));
                 before += r > rank || (r == rank && g < group);
             }
-            const float worst = -team_max(a.log2_lanes, before < a.kept && group < a.groups ? -rank : kMasked);
-            const float next = team_max(a.log2_lanes, before >= a.kept && group < a.groups ? rank : kMasked);
-            const bool close = live && next > kMasked && !(worst - next > 2.0f * apart);
-            if (__ballot(close) != 0) {
-                if (a.score == DDP_SCORE_SOFTMAX) take_sum64();
-                double first64 = kNone, second64 = kNone;
-#pragma unroll 1
-                for (int i = 0; i < EACH; ++i) {
-                    float v = kMasked, of_v = 0.0f;
-#pragma unroll
-                    for (int j = 0; j < EACH; ++j)
-                        if (j == i) {
-                            v = x[j];
-                            of_v = bias[j];
-                        }
-                    const double key = key64(v, score64(a.score, v, largest, sum64), static_cast<double>(of_v));
-                    second64 = fmax(fmin(first64, key), second64);
-                    first64 = fmax(first64, key);
-                }
-                for (int d = 1; d < 1 << a.log2_group; d <<= 1) {
-                    const double f = __shfl_xor(first64, d), g = __shfl_xor(second64, d);
-                    second64 = fmax(fmin(first64, f), fmax(second64, g));
-                    first64 = fmax(first64, f);
-                }
-                const double rank64 = a.top == 2 && second64 > kNone ? first64 + second64 : first64;
-                int before64 = 0;
-                for (int g = 0; g < a.groups; ++g) {
-                    const double r = __shfl(rank64, of_team0 + (g << a.log2_group));
-                    before64 += r > rank64 || (r == rank64 && g < group);
-                }
-                if (close) before = before64;
-            }
+            const float worst = -team_max(log2_lanes, before < a.kept && group < a.groups ? -rank : kMasked);
+            const float next = team_max(log2_lanes, before >= a.kept && group < a.groups ? rank : kMasked);
+            again = next > kMasked && !(worst - next > 2.0f * apart);
             if (before >= a.kept) {
 #pragma unroll
                 for (int i = 0; i < EACH; ++i) w[i] = 0;
@@ -392,13 +400,12 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
         float left = kMasked;                        // the largest key behind the candidates
         int taken = 0;
         for (int n = 0; n <= a.listed; ++n) {
-            const uint32_t head = w[0] >> 4, top = team_max(a.log2_lanes, head);
+            const uint32_t head = w[0] >> 4, top = team_max(log2_lanes, head);
             if (n == a.listed) {
-                if (top != 0) left = key_of(top << 4);
+                if (top != 0) left = key_of(top << 4, lift);
                 break;
             }
-            const uint64_t same = __ballot(head == top) >> of_team0;
-            if (__ffsll(static_cast<unsigned long long>(same)) - 1 == l) {
+            if (first_lane(__ballot(head == top), log2_lanes, of_team0) == l) {
                 word[n] = w[0];
                 at[n] = top != 0 ? e0 + 15 - static_cast<int>(w[0] & 15u) : -1;
                 ++taken;
@@ -411,52 +418,46 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
         for (int n = l; n < a.chosen; n += lanes) {
             const uint32_t here = word[n], behind = n + 1 < a.listed ? word[n + 1] : 0u;
             if (here != 0 && (behind != 0 || n + 1 >= a.listed)) {
-                const float k = key_of(here), b = n + 1 < a.listed ? key_of(behind) : left;
+                const float k = key_of(here, lift), b = n + 1 < a.listed ? key_of(behind, lift) : left;
                 near |= b > kMasked && !(k - b > apart);
             }
         }
         const uint64_t of_team = lanes == 64 ? ~uint64_t(0) : (uint64_t(1) << lanes) - 1;
         const bool close = (__ballot(near) >> of_team0 & of_team) != 0;
-        bool order64 = false;
-        if (__ballot(close && live) != 0) {
-            order64 = close;
-            if (a.score == DDP_SCORE_SOFTMAX && a.bias != nullptr && sum64 == 0.0) take_sum64();
-            if (a.bias == nullptr) sum64 = 1.0;
-            // the wave's room for keys holds the candidates'
-            double* exact = keys + wave * a.room + (team & ((64 >> a.log2_lanes) - 1)) * a.listed;
+        const bool ordered = __ballot(close && live && !again) != 0;
+        auto logit = [&](int e) { return load_one<LT>(row + e * ElemBytes<LT>::value); };
+        auto score = [&](float x) { return a.score == DDP_SCORE_SOFTMAX ? expf(x - largest) * most : 1.0f / (1.0f + expf(-x)); };
+        auto bias_of = [&](int e) { return a.bias != nullptr ? a.bias[e] : 0.0f; };
+        if (ordered) {                               // the candidates once more, by whole keys
+            for (int n = l; n < a.listed; n += lanes)
+                if (at[n] >= 0) word[n] = as_bits(score(logit(at[n])) + bias_of(at[n]));
+            wave_meets();
+            const float same = (a.score == DDP_SCORE_SOFTMAX ? kNearSoftmax : kNearSigmoid) * (most + of_bias);
             for (int n = l; n < a.listed; n += lanes) {
                 const int e = at[n];
-                const float v = e >= 0 && live ? load_one<LT>(row + e * ElemBytes<LT>::value) : kMasked;
-                exact[n] = e >= 0 ? key64(v, score64(a.score, v, largest, sum64), a.bias != nullptr ? static_cast<double>(a.bias[e]) : 0.0) : kNone;
-            }
-            wave_meets();
-            if (order64) {
-                double last = __builtin_huge_val();  // the lowest key that is chosen
-                for (int n = l; n < a.listed; n += lanes) {
-                    int rank = n;
-                    if (at[n] >= 0) {
-                        rank = 0;
-                        for (int m = 0; m < a.listed; ++m) rank += at[m] >= 0 && (exact[m] > exact[n] || (exact[m] == exact[n] && (at[m] & 0xFFFF) < (at[n] & 0xFFFF)));
-                        if (rank < a.chosen) last = fmin(last, exact[n]);
-                    }
-                    word[n] = static_cast<uint32_t>(rank);
+                if (e < 0) continue;
+                const float key = as_float(word[n]);
+                int rank = 0;
+                for (int m = 0; m < a.listed; ++m) {
+                    const int o = at[m] & 0xFFFF;
+                    if (at[m] < 0 || m == n) continue;
+                    const float other = as_float(word[m]);
+                    rank += other > key || (other == key && o < e);
+                    // equal for certain where logit and bias are
+                    if (!(fabsf(other - key) > same)) again |= logit(o) != logit(e) || bias_of(o) != bias_of(e);
                 }
-                float scale64 = 1.0f;                // (keys of a softmax without a bias are not divided by its sum)
-                if (a.score == DDP_SCORE_SOFTMAX && a.bias == nullptr) scale64 = most;
-                again = left > kMasked && !(static_cast<float>(last * scale64) - left > apart);
+                if (rank < a.chosen) again |= left > kMasked && !(key - left > apart);
+                place[n] = rank;
             }
-            // one lane of a team decides for all
             again = (__ballot(again) >> of_team0 & of_team) != 0;
         }
-        wave_meets();
         if (live && !again) {
             float all = 0.0f;
             for (int n = l; n < a.listed; n += lanes) {
-                const int rank = order64 ? static_cast<int>(word[n]) : n, e = at[n];
+                const int e = at[n], rank = ordered && e >= 0 ? place[n] : n;
                 float v = 0.0f;
                 if (rank < a.chosen && e >= 0) {
-                    const float logit = load_one<LT>(row + e * ElemBytes<LT>::value);
-                    v = a.score == DDP_SCORE_SOFTMAX ? expf(logit - largest) * most : 1.0f / (1.0f + expf(-logit));
+                    v = score(logit(e));
                 }
                 all += v;
                 word[n] = as_bits(v);
@@ -466,7 +467,7 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
                     store_weight(a.weights, a.weights_type, t * a.chosen + rank, 0.0f);
                 }
             }
-            all = team_sum(a.log2_lanes, all);
+            all = team_sum(log2_lanes, all);
             const float factor = !a.renormalise ? a.scale : all > 0.0f ? a.scale / all : 0.0f;
             for (int n = l; n < a.listed; n += lanes) {
                 if (at[n] < 0) continue;
@@ -476,18 +477,34 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
                 if (a.counts != nullptr) atomicAdd(&counts[e], 1);
             }
         }
-        for (uint64_t left_over = __ballot(live && again && l == 0); left_over != 0; left_over &= left_over - 1) {
-            const int which = __ffsll(static_cast<unsigned long long>(left_over)) - 1;
-            wave_meets();
-            route_token<LT>(a, base + ((static_cast<int>(threadIdx.x & ~63u) + which) >> a.log2_lanes), keys + wave * a.room, counts);
+        if constexpr (HERE) {
+            for (uint64_t left_over = __ballot(live && again && l == 0); left_over != 0; left_over &= left_over - 1) {
+                const int which = __ffsll(static_cast<unsigned long long>(left_over)) - 1;
+                wave_meets();
+                route_token<LT>(a, base + ((static_cast<int>(threadIdx.x & ~63u) + which) >> log2_lanes), keys + wave * a.room, counts);
+            }
+        } else {
+            if (live && again && l == 0) a.experts_out[t * a.chosen] = kAgain;
         }
         wave_meets();
     }
-    add_counts(a, counts);
+    add_counts<HERE>(a, counts);
 }
 
-__global__ __launch_bounds__(kThreads) void clear_kernel(int32_t* counts, int n) {
-    for (int e = threadIdx.x; e < n; e += kThreads) counts[e] = 0;
+// The copies' sum, and zeros in them for the next call.  A thread an expert.
+__global__ __launch_bounds__(64) void count_kernel(int32_t* copies, int32_t* counts, int experts, int accumulate) {
+    const int e = blockIdx.x * 64 + threadIdx.x;
+    if (e >= experts) return;
+    int32_t sum = accumulate ? counts[e] : 0;
+    int32_t x[kCopies];
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) x[c] = copies[c * experts + e];
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+        sum += x[c];
+        if (x[c] != 0) copies[c * experts + e] = 0;
+    }
+    counts[e] = sum;
 }
 
 // A token's gradient by a team of lanes with EACH neighbouring experts each.  What the chosen experts get is put together in a row in LDS, which is zeros
@@ -602,15 +619,16 @@ __global__ __launch_bounds__(kMaxExperts) void balance_kernel(const int32_t* cou
 
 // ---- host ----
 
-constexpr int64_t kBlocks = 2048;
+constexpr int64_t kBlocks = 2048, kFewLanes = 65536, kFewBlocks = 512;
 
-// The team of a token: a.each experts a lane, the most that divide into its groups.  False: none.
-bool find_team(RouteArgs& a) {
+// The team of a token: a.each experts a lane, up to `most`, so that groups have a power of two of lanes.  False: none.
+bool team_of(RouteArgs& a, int most) {
     const int per_group = a.experts / a.groups;
+    a.log2_lanes = a.log2_group = 0;
     if (a.kept >= a.groups) {
-        a.each = std::min({kEach, (a.experts + 3) / 4, 256 / a.chosen + 4});     // (many candidates take more lanes: their LDS is a team's)
+        a.each = std::max(std::min(most, 256 / a.chosen + 4), (a.experts + 63) / 64);        // (many candidates take more lanes: their LDS is a team's)
     } else {
-        for (a.each = std::min(kEach, per_group); a.each > 0; --a.each) {
+        for (a.each = std::min(most, per_group); a.each > 0; --a.each) {
             const int lanes = per_group / a.each;
             if (per_group % a.each == 0 && (lanes & (lanes - 1)) == 0) break;
         }
@@ -618,28 +636,55 @@ bool find_team(RouteArgs& a) {
         while (a.each << a.log2_group < per_group) ++a.log2_group;
     }
     while (a.each << a.log2_lanes < a.experts) ++a.log2_lanes;
+    if (a.each > 8) a.log2_lanes = std::max(a.log2_lanes, 2);
     if (a.log2_lanes > 6) return false;
     a.listed = std::min(a.chosen + kSpare, a.experts);
-    a.room = std::max({a.experts, (64 >> a.log2_lanes) * a.listed, 32 * (a.each > 8 ? 16 : a.each > 4 ? 8 : a.each > 2 ? 4 : a.each)});
+    a.room = std::max({a.experts, 32 * (a.each > 8 ? 16 : a.each > 4 ? 8 : a.each > 2 ? 4 : a.each)});
+    return true;
+}
+// Four lanes at least, and where tokens are few as many as find work.
+bool find_team(RouteArgs& a) {
+    const int64_t lanes = std::max<int64_t>(4, std::min<int64_t>(64, kFewLanes / a.tokens));
+    return team_of(a, static_cast<int>(std::min<int64_t>(kEach, (a.experts + lanes - 1) / lanes))) || team_of(a, kEach);
+}
+// Returns whether counts are left in the copies.
+template <int LT, int EACH>
+bool launch_team(ddp_router* h, const RouteArgs& a, int64_t blocks, size_t bytes) {
+    if (blocks <= kFewBlocks) {
+        hipLaunchKernelGGL((route_team_kernel<LT, EACH, true, -1>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), bytes, h->stream, a);
+        return blocks > 1;
+    }
+    const dim3 grid(static_cast<unsigned>(std::min(blocks, kBlocks))), threads(kThreads);
+    auto launch = [&](auto lanes) { hipLaunchKernelGGL((route_team_kernel<LT, EACH, false, lanes.value>), grid, threads, bytes, h->stream, a); };
+    if constexpr (EACH == 16) {
+        if (a.log2_lanes <= 2) launch(std::integral_constant<int, 2>());
+        else if (a.log2_lanes == 3) launch(std::integral_constant<int, 3>());
+        else if (a.log2_lanes == 4) launch(std::integral_constant<int, 4>());
+        else if (a.log2_lanes == 5) launch(std::integral_constant<int, 5>());
+        else launch(std::integral_constant<int, 6>());
+    } else {
+        launch(std::integral_constant<int, -1>());
+    }
+    const int64_t looks = (a.tokens + kWaves * kLooked - 1) / (kWaves * kLooked);
+    hipLaunchKernelGGL((route_kernel<LT, false>), dim3(static_cast<unsigned>(std::min(looks, kBlocks))), dim3(kThreads),
+                       static_cast<size_t>(kWaves * 8 + 4) * a.experts, h->stream, a);
     return true;
 }
 template <int LT>
-hipError_t launch_route(ddp_router* h, RouteArgs a) {
-    const size_t counts = static_cast<size_t>(a.experts) * 4;
+bool launch_route(ddp_router* h, RouteArgs a) {
     if (!find_team(a)) {
         const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((a.tokens + kWaves - 1) / kWaves, kBlocks));
-        hipLaunchKernelGGL((route_kernel<LT>), dim3(blocks), dim3(kThreads), static_cast<size_t>(kWaves) * a.experts * 8 + counts, h->stream, a);
-        return hipGetLastError();
+        hipLaunchKernelGGL((route_kernel<LT, true>), dim3(blocks), dim3(kThreads), static_cast<size_t>(kWaves * 8 + 4) * a.experts, h->stream, a);
+        return blocks > 1;
     }
     const int teams = kThreads >> a.log2_lanes;
-    const dim3 blocks(static_cast<unsigned>(std::min<int64_t>((a.tokens + teams - 1) / teams, kBlocks))), threads(kThreads);
-    const size_t bytes = static_cast<size_t>(kWaves) * a.room * 8 + static_cast<size_t>(teams) * a.listed * 8 + counts;
-    if (a.each > 8) hipLaunchKernelGGL((route_team_kernel<LT, 16>), blocks, threads, bytes, h->stream, a);
-    else if (a.each > 4) hipLaunchKernelGGL((route_team_kernel<LT, 8>), blocks, threads, bytes, h->stream, a);
-    else if (a.each > 2) hipLaunchKernelGGL((route_team_kernel<LT, 4>), blocks, threads, bytes, h->stream, a);
-    else if (a.each > 1) hipLaunchKernelGGL((route_team_kernel<LT, 2>), blocks, threads, bytes, h->stream, a);
-    else hipLaunchKernelGGL((route_team_kernel<LT, 1>), blocks, threads, bytes, h->stream, a);
-    return hipGetLastError();
+    const int64_t blocks = (a.tokens + teams - 1) / teams;
+    const size_t bytes = static_cast<size_t>(kWaves) * a.room * 8 + static_cast<size_t>(teams) * a.listed * 12 + static_cast<size_t>(a.experts) * 4;
+    if (a.each > 8) return launch_team<LT, 16>(h, a, blocks, bytes);
+    if (a.each > 4) return launch_team<LT, 8>(h, a, blocks, bytes);
+    if (a.each > 2) return launch_team<LT, 4>(h, a, blocks, bytes);
+    if (a.each > 1) return launch_team<LT, 2>(h, a, blocks, bytes);
+    return launch_team<LT, 1>(h, a, blocks, bytes);
 }
 template <int LT>
 hipError_t launch_grad(ddp_router* h, RouteGradArgs a) {
@@ -651,6 +696,12 @@ hipError_t launch_grad(ddp_router* h, RouteGradArgs a) {
     if (each == 16) hipLaunchKernelGGL((route_grad_kernel<LT, 16>), blocks, threads, bytes, h->stream, a);
     else hipLaunchKernelGGL((route_grad_kernel<LT, 4>), blocks, threads, bytes, h->stream, a);
     return hipGetLastError();
+}
+
+int32_t sum_copies(ddp_router* h, int32_t* counts, int32_t accumulate) {
+    hipLaunchKernelGGL(count_kernel, dim3(static_cast<unsigned>((h->experts + 63) / 64)), dim3(64), 0, h->stream, h->copies, counts, h->experts, accumulate);
+    LAYER_HIP(h, hipGetLastError());
+    return DDP_OK;
 }
 
 int32_t check_tokens(ddp_router* h, int64_t tokens, int32_t dtype, int32_t weights_dtype, int64_t stride) {
@@ -692,6 +743,21 @@ int32_t ddp_router_create(ddp_router** out, int32_t device, void* stream, int32_
     h->score = score;
     h->renormalise = renormalise != 0;
     h->scale = scale;
+    if (device != DDP_DEVICE_NONE) {
+        const int64_t bytes = static_cast<int64_t>(kCopies) * experts * 4;
+        hipError_t err = layer_alloc(h, bytes);
+        if (err == hipSuccess) {
+            OnDevice on(device);
+            err = taken(hipMemset(h->mem, 0, static_cast<size_t>(bytes)));
+            if (err == hipSuccess) err = taken(hipStreamSynchronize(nullptr));
+            if (err != hipSuccess) (void)taken(hipFree(h->mem));
+        }
+        if (err != hipSuccess) {
+            delete h;
+            return layer_fail(nullptr, DDP_ERR_HIP, hipGetErrorString(err));
+        }
+        h->copies = reinterpret_cast<int32_t*>(h->mem);
+    }
     *out = h;
     return DDP_OK;
 }
@@ -715,11 +781,10 @@ int32_t ddp_router_route(ddp_router* h, int64_t tokens, const void* logits, int3
     if (h->device == DDP_DEVICE_NONE) return layer_fail(h, DDP_ERR_NO_DEVICE, "ddp_router_route without a device");
     OnDevice on(h->device);
     LAYER_HIP(h, on.err);
-    if (counts && !accumulate) {
-        hipLaunchKernelGGL(clear_kernel, dim3(1), dim3(kThreads), 0, h->stream, counts, h->experts);
-        LAYER_HIP(h, hipGetLastError());
+    if (tokens == 0) {
+        if (!counts || accumulate) return DDP_OK;
+        return sum_copies(h, counts, 0);
     }
-    if (tokens == 0) return DDP_OK;
     RouteArgs a{};
     a.logits = static_cast<const char*>(logits);
     a.bias = bias;
@@ -737,8 +802,11 @@ int32_t ddp_router_route(ddp_router* h, int64_t tokens, const void* logits, int3
     a.renormalise = h->renormalise;
     a.weights_type = weights_dtype;
     a.scale = h->scale;
-    LAYER_HIP(h, dtype == DDP_FP32 ? launch_route<DDP_FP32>(h, a) : dtype == DDP_FP16 ? launch_route<DDP_FP16>(h, a) : launch_route<DDP_BF16>(h, a));
-    return DDP_OK;
+    a.copies = h->copies;
+    a.accumulate = accumulate != 0;
+    const bool copies = dtype == DDP_FP32 ? launch_route<DDP_FP32>(h, a) : dtype == DDP_FP16 ? launch_route<DDP_FP16>(h, a) : launch_route<DDP_BF16>(h, a);
+    LAYER_HIP(h, hipGetLastError());
+    return counts && copies ? sum_copies(h, counts, accumulate) : DDP_OK;
 }
 
 int32_t ddp_router_grad(ddp_router* h, int64_t tokens, const void* logits, int32_t dtype, int64_t stride, const int32_t* experts_in,
