@@ -311,6 +311,9 @@ _fast.bind_around(*(C.cast(f, _vp).value for f in (_lib.ddp_embedding_lookup, _l
                                                    _lib.ddp_opt_grad_norm, _lib.ddp_opt_adamw_step)))
 _fast_lookup, _fast_grad = _fast.embedding_lookup, _fast.embedding_grad
 _fast_norm, _fast_step = _fast.opt_grad_norm, _fast.opt_adamw_step
+_fast.bind_layer(*(C.cast(f, _vp).value for f in (
+    _lib.ddp_layernorm_forward, _lib.ddp_layernorm_backward, _lib.ddp_position_bias_apply, _lib.ddp_position_bias_grad,
+    _lib.ddp_router_route, _lib.ddp_router_grad, _lib.ddp_router_balance)))
 
 
 def _address(ctx):
@@ -629,21 +632,29 @@ def ddp_layernorm_destroy(norm) -> None:
 def ddp_layernorm_forward(norm, rows: int, x: int, x_dtype: int, x_stride: int, residual: int, residual_stride: int, gamma: int, beta: int,
                           param_dtype: int, eps: float, sum_: int, sum_stride: int, y: int, y_dtype: int, y_stride: int, mean: int = 0,
                           rstd: int = 0) -> None:
-    status = _lib.ddp_layernorm_forward(norm, _index(rows), _pointer(x), _index(x_dtype), _index(x_stride), _pointer(residual),
-                                        _index(residual_stride), _pointer(gamma), _pointer(beta), _index(param_dtype), float(eps),
-                                        _pointer(sum_), _index(sum_stride), _pointer(y), _index(y_dtype), _index(y_stride),
-                                        _pointer(mean), _pointer(rstd))
-    _check_layer(ddp_layernorm_last_error, norm, status)
+    status = _fast.layernorm_forward(_address(norm), rows, x, x_dtype, x_stride, residual, residual_stride, gamma, beta, param_dtype,
+                                     eps, sum_, sum_stride, y, y_dtype, y_stride, mean, rstd)
+    if status is None:
+        status = _lib.ddp_layernorm_forward(norm, _index(rows), _pointer(x), _index(x_dtype), _index(x_stride), _pointer(residual),
+                                            _index(residual_stride), _pointer(gamma), _pointer(beta), _index(param_dtype), float(eps),
+                                            _pointer(sum_), _index(sum_stride), _pointer(y), _index(y_dtype), _index(y_stride),
+                                            _pointer(mean), _pointer(rstd))
+    if status < 0:
+        _check_layer(ddp_layernorm_last_error, norm, status)
 
 
 def ddp_layernorm_backward(norm, rows: int, dy: int, dy_dtype: int, dy_stride: int, x: int, x_dtype: int, x_stride: int, mean: int, rstd: int,
                            gamma: int, param_dtype: int, dsum: int, dsum_stride: int, dx: int, dx_stride: int, accumulate: bool,
                            dgamma: int, dbeta: int, grad_dtype: int) -> None:
-    status = _lib.ddp_layernorm_backward(norm, _index(rows), _pointer(dy), _index(dy_dtype), _index(dy_stride), _pointer(x),
-                                         _index(x_dtype), _index(x_stride), _pointer(mean), _pointer(rstd), _pointer(gamma),
-                                         _index(param_dtype), _pointer(dsum), _index(dsum_stride), _pointer(dx), _index(dx_stride),
-                                         1 if accumulate else 0, _pointer(dgamma), _pointer(dbeta), _index(grad_dtype))
-    _check_layer(ddp_layernorm_last_error, norm, status)
+    status = _fast.layernorm_backward(_address(norm), rows, dy, dy_dtype, dy_stride, x, x_dtype, x_stride, mean, rstd, gamma,
+                                      param_dtype, dsum, dsum_stride, dx, dx_stride, accumulate, dgamma, dbeta, grad_dtype)
+    if status is None:
+        status = _lib.ddp_layernorm_backward(norm, _index(rows), _pointer(dy), _index(dy_dtype), _index(dy_stride), _pointer(x),
+                                             _index(x_dtype), _index(x_stride), _pointer(mean), _pointer(rstd), _pointer(gamma),
+                                             _index(param_dtype), _pointer(dsum), _index(dsum_stride), _pointer(dx), _index(dx_stride),
+                                             1 if accumulate else 0, _pointer(dgamma), _pointer(dbeta), _index(grad_dtype))
+    if status < 0:
+        _check_layer(ddp_layernorm_last_error, norm, status)
 
 
 def ddp_position_bias_last_error(bias) -> str:
@@ -673,21 +684,31 @@ def ddp_position_bias_buckets(bias) -> np.ndarray:
 def ddp_position_bias_apply(bias, batch: int, queries: int, keys: int, offset: int, table: int, table_dtype: int, table_stride: int,
                             scale: float, key_lengths: int, causal: bool, masked: float, accumulate: bool, out: int, out_dtype: int,
                             batch_stride: int, head_stride: int, query_stride: int) -> None:
-    status = _lib.ddp_position_bias_apply(bias, _index(batch), _index(queries), _index(keys), _index(offset), _pointer(table),
-                                          _index(table_dtype), _index(table_stride), float(scale), _pointer(key_lengths),
-                                          1 if causal else 0, float(masked), 1 if accumulate else 0, _pointer(out), _index(out_dtype),
-                                          _index(batch_stride), _index(head_stride), _index(query_stride))
-    _check_layer(ddp_position_bias_last_error, bias, status)
+    status = _fast.position_bias_apply(_address(bias), batch, queries, keys, offset, table, table_dtype, table_stride, scale,
+                                       key_lengths, causal, masked, accumulate, out, out_dtype, batch_stride, head_stride,
+                                       query_stride)
+    if status is None:
+        status = _lib.ddp_position_bias_apply(bias, _index(batch), _index(queries), _index(keys), _index(offset), _pointer(table),
+                                              _index(table_dtype), _index(table_stride), float(scale), _pointer(key_lengths),
+                                              1 if causal else 0, float(masked), 1 if accumulate else 0, _pointer(out), _index(out_dtype),
+                                              _index(batch_stride), _index(head_stride), _index(query_stride))
+    if status < 0:
+        _check_layer(ddp_position_bias_last_error, bias, status)
 
 
 def ddp_position_bias_grad(bias, batch: int, queries: int, keys: int, offset: int, dscores: int, dtype: int, batch_stride: int,
                            head_stride: int, query_stride: int, scale: float, key_lengths: int, query_lengths: int, causal: bool,
                            accumulate: bool, grad: int, grad_dtype: int, grad_stride: int) -> None:
-    status = _lib.ddp_position_bias_grad(bias, _index(batch), _index(queries), _index(keys), _index(offset), _pointer(dscores),
-                                         _index(dtype), _index(batch_stride), _index(head_stride), _index(query_stride), float(scale),
-                                         _pointer(key_lengths), _pointer(query_lengths), 1 if causal else 0, 1 if accumulate else 0,
-                                         _pointer(grad), _index(grad_dtype), _index(grad_stride))
-    _check_layer(ddp_position_bias_last_error, bias, status)
+    status = _fast.position_bias_grad(_address(bias), batch, queries, keys, offset, dscores, dtype, batch_stride, head_stride,
+                                      query_stride, scale, key_lengths, query_lengths, causal, accumulate, grad, grad_dtype,
+                                      grad_stride)
+    if status is None:
+        status = _lib.ddp_position_bias_grad(bias, _index(batch), _index(queries), _index(keys), _index(offset), _pointer(dscores),
+                                             _index(dtype), _index(batch_stride), _index(head_stride), _index(query_stride), float(scale),
+                                             _pointer(key_lengths), _pointer(query_lengths), 1 if causal else 0, 1 if accumulate else 0,
+                                             _pointer(grad), _index(grad_dtype), _index(grad_stride))
+    if status < 0:
+        _check_layer(ddp_position_bias_last_error, bias, status)
 
 
 def ddp_router_last_error(router) -> str:
@@ -710,19 +731,30 @@ def ddp_router_destroy(router) -> None:
 
 def ddp_router_route(router, tokens: int, logits: int, dtype: int, stride: int, bias: int, experts_out: int, weights: int,
                      weights_dtype: int, counts: int = 0, accumulate: bool = False) -> None:
-    status = _lib.ddp_router_route(router, _index(tokens), _pointer(logits), _index(dtype), _index(stride), _pointer(bias),
-                                   _pointer(experts_out), _pointer(weights), _index(weights_dtype), _pointer(counts),
-                                   1 if accumulate else 0)
-    _check_layer(ddp_router_last_error, router, status)
+    status = _fast.router_route(_address(router), tokens, logits, dtype, stride, bias, experts_out, weights, weights_dtype, counts,
+                                accumulate)
+    if status is None:
+        status = _lib.ddp_router_route(router, _index(tokens), _pointer(logits), _index(dtype), _index(stride), _pointer(bias),
+                                       _pointer(experts_out), _pointer(weights), _index(weights_dtype), _pointer(counts),
+                                       1 if accumulate else 0)
+    if status < 0:
+        _check_layer(ddp_router_last_error, router, status)
 
 
 def ddp_router_grad(router, tokens: int, logits: int, dtype: int, stride: int, experts_in: int, dweights: int, dweights_dtype: int,
                     dlogits: int, dlogits_stride: int) -> None:
-    status = _lib.ddp_router_grad(router, _index(tokens), _pointer(logits), _index(dtype), _index(stride), _pointer(experts_in),
-                                  _pointer(dweights), _index(dweights_dtype), _pointer(dlogits), _index(dlogits_stride))
-    _check_layer(ddp_router_last_error, router, status)
+    status = _fast.router_grad(_address(router), tokens, logits, dtype, stride, experts_in, dweights, dweights_dtype, dlogits,
+                               dlogits_stride)
+    if status is None:
+        status = _lib.ddp_router_grad(router, _index(tokens), _pointer(logits), _index(dtype), _index(stride), _pointer(experts_in),
+                                      _pointer(dweights), _index(dweights_dtype), _pointer(dlogits), _index(dlogits_stride))
+    if status < 0:
+        _check_layer(ddp_router_last_error, router, status)
 
 
 def ddp_router_balance(router, replicas: int, counts: int, rate: float, bias: int, bias_out: int) -> None:
-    status = _lib.ddp_router_balance(router, _index(replicas), _pointer(counts), float(rate), _pointer(bias), _pointer(bias_out))
-    _check_layer(ddp_router_last_error, router, status)
+    status = _fast.router_balance(_address(router), replicas, counts, rate, bias, bias_out)
+    if status is None:
+        status = _lib.ddp_router_balance(router, _index(replicas), _pointer(counts), float(rate), _pointer(bias), _pointer(bias_out))
+    if status < 0:
+        _check_layer(ddp_router_last_error, router, status)

@@ -424,7 +424,108 @@ static PyObject* opt_adamw_step(PyObject* self, PyObject* const* a, Py_ssize_t n
     return PyLong_FromLong((long)g_step(o, x[0], x[1], x[2], x[3], x[4], x[5], x[6], skip != 0, NULL));
 }
 
+typedef int32_t (*ln_forward_fn)(void*, int64_t, const void*, int32_t, int64_t, const void*, int64_t, const void*, const void*, int32_t, float, void*,
+                                 int64_t, void*, int32_t, int64_t, float*, float*);
+typedef int32_t (*ln_backward_fn)(void*, int64_t, const void*, int32_t, int64_t, const void*, int32_t, int64_t, const float*, const float*, const void*,
+                                  int32_t, const void*, int64_t, void*, int64_t, int32_t, void*, void*, int32_t);
+typedef int32_t (*bias_apply_fn)(void*, int64_t, int64_t, int64_t, int64_t, const void*, int32_t, int64_t, float, const int32_t*, int32_t, float, int32_t,
+                                 void*, int32_t, int64_t, int64_t, int64_t);
+typedef int32_t (*bias_grad_fn)(void*, int64_t, int64_t, int64_t, int64_t, const void*, int32_t, int64_t, int64_t, int64_t, float, const int32_t*,
+                                const int32_t*, int32_t, int32_t, void*, int32_t, int64_t);
+typedef int32_t (*route_fn)(void*, int64_t, const void*, int32_t, int64_t, const float*, int32_t*, void*, int32_t, int32_t*, int32_t);
+typedef int32_t (*route_grad_fn)(void*, int64_t, const void*, int32_t, int64_t, const int32_t*, const void*, int32_t, void*, int64_t);
+typedef int32_t (*balance_fn)(void*, int32_t, const int32_t*, float, const float*, float*);
+
+static ln_forward_fn g_ln_forward = NULL;
+static ln_backward_fn g_ln_backward = NULL;
+static bias_apply_fn g_bias_apply = NULL;
+static bias_grad_fn g_bias_grad = NULL;
+static route_fn g_route = NULL;
+static route_grad_fn g_route_grad = NULL;
+static balance_fn g_balance = NULL;
+
+/* bind_layer(layernorm_forward, layernorm_backward, position_bias_apply, position_bias_grad, router_route, router_grad, router_balance) */
+static PyObject* bind_layer(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 7) {
+        PyErr_SetString(PyExc_TypeError, "bind_layer: seven addresses");
+        return NULL;
+    }
+    void* a[7];
+    for (Py_ssize_t i = 0; i < 7; ++i) {
+        a[i] = PyLong_AsVoidPtr(args[i]);
+        if (a[i] == NULL && PyErr_Occurred()) return NULL;
+    }
+    g_ln_forward = (ln_forward_fn)a[0];
+    g_ln_backward = (ln_backward_fn)a[1];
+    g_bias_apply = (bias_apply_fn)a[2];
+    g_bias_grad = (bias_grad_fn)a[3];
+    g_route = (route_fn)a[4];
+    g_route_grad = (route_grad_fn)a[5];
+    g_balance = (balance_fn)a[6];
+    Py_RETURN_NONE;
+}
+
+/* The functions below take the C functions' arguments one by one: p a pointer, l and i integers of 64 and 32 bits, f a float. */
+typedef union { void* p; int64_t l; int32_t i; double f; } arg_t;
+static int plain_args(PyObject* const* a, Py_ssize_t nargs, const char* kinds, arg_t* v) {
+    for (Py_ssize_t k = 0; k < nargs; ++k) {
+        const char kind = kinds[k];
+        if (kind == 'p' ? !plain_ptr(a[k], &v[k].p) : kind == 'l' ? !plain_i64(a[k], &v[k].l) : kind == 'i' ? !plain_i32(a[k], &v[k].i) : kind == 'f' ? !plain_f64(a[k], &v[k].f) : 1)
+            return 0;
+    }
+    return kinds[nargs] == 0;
+}
+static int32_t truth(arg_t v) { return v.i != 0; }
+
+static PyObject* layernorm_forward(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    arg_t v[18];
+    if (nargs != 18 || g_ln_forward == NULL || !plain_args(a, nargs, "plpilplppifplpilpp", v)) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_ln_forward(v[0].p, v[1].l, v[2].p, v[3].i, v[4].l, v[5].p, v[6].l, v[7].p, v[8].p, v[9].i, (float)v[10].f, v[11].p,
+                                              v[12].l, v[13].p, v[14].i, v[15].l, (float*)v[16].p, (float*)v[17].p));
+}
+static PyObject* layernorm_backward(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    arg_t v[20];
+    if (nargs != 20 || g_ln_backward == NULL || !plain_args(a, nargs, "plpilpilpppiplplippi", v)) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_ln_backward(v[0].p, v[1].l, v[2].p, v[3].i, v[4].l, v[5].p, v[6].i, v[7].l, (float*)v[8].p, (float*)v[9].p, v[10].p,
+                                               v[11].i, v[12].p, v[13].l, v[14].p, v[15].l, truth(v[16]), v[17].p, v[18].p, v[19].i));
+}
+static PyObject* position_bias_apply(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    arg_t v[18];
+    if (nargs != 18 || g_bias_apply == NULL || !plain_args(a, nargs, "pllllpilfpifipilll", v)) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_bias_apply(v[0].p, v[1].l, v[2].l, v[3].l, v[4].l, v[5].p, v[6].i, v[7].l, (float)v[8].f, (int32_t*)v[9].p, truth(v[10]),
+                                              (float)v[11].f, truth(v[12]), v[13].p, v[14].i, v[15].l, v[16].l, v[17].l));
+}
+static PyObject* position_bias_grad(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    arg_t v[18];
+    if (nargs != 18 || g_bias_grad == NULL || !plain_args(a, nargs, "pllllpilllfppiipil", v)) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_bias_grad(v[0].p, v[1].l, v[2].l, v[3].l, v[4].l, v[5].p, v[6].i, v[7].l, v[8].l, v[9].l, (float)v[10].f, (int32_t*)v[11].p,
+                                             (int32_t*)v[12].p, truth(v[13]), truth(v[14]), v[15].p, v[16].i, v[17].l));
+}
+static PyObject* router_route(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    arg_t v[11];
+    if (nargs != 11 || g_route == NULL || !plain_args(a, nargs, "plpilpppipi", v)) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_route(v[0].p, v[1].l, v[2].p, v[3].i, v[4].l, (float*)v[5].p, (int32_t*)v[6].p, v[7].p, v[8].i, (int32_t*)v[9].p, truth(v[10])));
+}
+static PyObject* router_grad(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    arg_t v[10];
+    if (nargs != 10 || g_route_grad == NULL || !plain_args(a, nargs, "plpilppipl", v)) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_route_grad(v[0].p, v[1].l, v[2].p, v[3].i, v[4].l, (int32_t*)v[5].p, v[6].p, v[7].i, v[8].p, v[9].l));
+}
+static PyObject* router_balance(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+    arg_t v[6];
+    if (nargs != 6 || g_balance == NULL || !plain_args(a, nargs, "pipfpp", v)) Py_RETURN_NONE;
+    return PyLong_FromLong((long)g_balance(v[0].p, v[1].i, (int32_t*)v[2].p, (float)v[3].f, (float*)v[4].p, (float*)v[5].p));
+}
+
 static PyMethodDef methods[] = {
+    {"bind_layer", (PyCFunction)(void (*)(void))bind_layer, METH_FASTCALL, "set the C entry points of the operators inside a layer"},
+    {"layernorm_forward", (PyCFunction)(void (*)(void))layernorm_forward, METH_FASTCALL, "ddp_layernorm_forward"},
+    {"layernorm_backward", (PyCFunction)(void (*)(void))layernorm_backward, METH_FASTCALL, "ddp_layernorm_backward"},
+    {"position_bias_apply", (PyCFunction)(void (*)(void))position_bias_apply, METH_FASTCALL, "ddp_position_bias_apply"},
+    {"position_bias_grad", (PyCFunction)(void (*)(void))position_bias_grad, METH_FASTCALL, "ddp_position_bias_grad"},
+    {"router_route", (PyCFunction)(void (*)(void))router_route, METH_FASTCALL, "ddp_router_route"},
+    {"router_grad", (PyCFunction)(void (*)(void))router_grad, METH_FASTCALL, "ddp_router_grad"},
+    {"router_balance", (PyCFunction)(void (*)(void))router_balance, METH_FASTCALL, "ddp_router_balance"},
     {"bind_around", (PyCFunction)(void (*)(void))bind_around, METH_FASTCALL, "set the C entry points of embedding and optimizer"},
     {"embedding_lookup", (PyCFunction)(void (*)(void))embedding_lookup, METH_FASTCALL, "ddp_embedding_lookup"},
     {"embedding_grad", (PyCFunction)(void (*)(void))embedding_grad, METH_FASTCALL, "ddp_embedding_grad"},
