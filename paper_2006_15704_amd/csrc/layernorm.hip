@@ -74,12 +74,12 @@ __device__ __forceinline__ float block_sum(float x, float* part) {
 // A team is LANES neighbouring lanes or WAVES waves, an element kEach times: a row is read once, in whole 16-byte vectors that are all on
 // the way together, and its sums are taken in registers.  Vector v of lane l is at column (v lanes + l) N; the one that would reach over the
 // end of the row is moved back to end with it, and what it shares with the vector in front of it counts there.
-constexpr int kEach = 16;
+constexpr int kMostEach = 16;
 
-template <int XT, int YT, int LANES_, int WAVES_, int THREADS_>
+template <int XT, int YT, int LANES_, int WAVES_, int THREADS_, int EACH_>
 struct Team {
-    static constexpr int LANES = LANES_, WAVES = WAVES_, THREADS = THREADS_;
-    static constexpr int N = XT == DDP_FP32 ? 4 : 8, V = kEach / N, SIZE = LANES * WAVES, TEAMS = THREADS / SIZE;
+    static constexpr int LANES = LANES_, WAVES = WAVES_, THREADS = THREADS_, EACH = EACH_;
+    static constexpr int N = XT == DDP_FP32 ? 4 : 8, V = EACH / N, SIZE = LANES * WAVES, TEAMS = THREADS / SIZE;
     static_assert(LANES == 64 || WAVES == 1, "a team of several waves has whole ones");
     int at[V], own[V];                               // own: elements from here on are the vector's; N: nothing here
     bool ragged;
@@ -93,8 +93,13 @@ struct Team {
             at[v] = c + N <= width ? c : width - N;
             own[v] = c >= width ? N : c - at[v];
         }
-        ragged = width != SIZE * kEach;
+        ragged = width != SIZE * EACH;
 #endif
+    }
+    // The block's team that a thread belongs to; where that is a wave's, its rows' addresses are scalars.
+    __device__ __forceinline__ static int mine() {
+        const int team = static_cast<int>(threadIdx.x) / SIZE;
+        return LANES == 64 ? __builtin_amdgcn_readfirstlane(team) : team;
     }
     // Elements that are another vector's, as zeros.
     __device__ __forceinline__ void clear_shared(float (&x)[V][N]) const {
@@ -108,7 +113,7 @@ struct Team {
     __device__ __forceinline__ void load(const char* row, bool live, Parts<DT, N> (&raw)[V]) const {
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (live && own[v] < N) raw[v] = load_parts<DT, N>(row + at[v] * ElemBytes<DT>::value);
+            if (live && own[v] < N) raw[v] = load_parts<DT, N>(row + static_cast<unsigned>(at[v]) * ElemBytes<DT>::value);
             else raw[v] = Parts<DT, N>{};
     }
     template <int DT>
@@ -116,7 +121,7 @@ struct Team {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live || own[v] == N) continue;
-            char* to = row + at[v] * ElemBytes<DT>::value;
+            char* to = row + static_cast<unsigned>(at[v]) * ElemBytes<DT>::value;
             if (own[v] == 0) {
                 store_some<DT, N>(to, N, x[v]);
             } else {
@@ -175,7 +180,7 @@ __global__ __launch_bounds__(T::THREADS) void forward_team_kernel(ForwardArgs a)
     team.params(a.beta, a.param, 0.0f, beta);
     const float each = 1.0f / a.width;
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * T::TEAMS; base < a.rows; base += static_cast<int64_t>(gridDim.x) * T::TEAMS) {
-        const int64_t row = base + threadIdx.x / T::SIZE;
+        const int64_t row = base + T::mine();
         const bool live = row < a.rows;
         Parts<XT, N> x[V], r[V];
         team.template load<XT>(a.x + row * a.x_stride * ElemBytes<XT>::value, live, x);
@@ -231,14 +236,14 @@ __global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs 
     constexpr bool WIDE = T::LANES == 64;            // narrower teams meet within their wave first
     constexpr int MEET = WIDE ? T::TEAMS : T::THREADS / 64;
     __shared__ float meet[2][T::THREADS / 64 * 2];
-    __shared__ float part[MEET > 1 ? MEET / 2 : 1][2][MEET > 1 ? T::SIZE * kEach : 1];
+    __shared__ float part[MEET > 1 ? MEET / 2 : 1][2][MEET > 1 ? T::SIZE * T::EACH : 1];
     const T team(a.width);
     float gamma[V][N], dgamma[V][N] = {}, dbeta[V][N] = {};
     team.params(a.gamma, a.param, 1.0f, gamma);
     const float each = 1.0f / a.width;
     int turn = 0;
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * T::TEAMS; base < a.rows; base += static_cast<int64_t>(gridDim.x) * T::TEAMS) {
-        const int64_t row = base + threadIdx.x / T::SIZE;
+        const int64_t row = base + T::mine();
         const bool live = row < a.rows;
         Parts<XT, N> x[V], more[V];
         Parts<YT, N> dy[V];
@@ -494,26 +499,27 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
 
 constexpr int kRowBlocks = 1 << 16;
 
-constexpr int kForwardThreads = 256, kForwardBlocks = 2048, kBackwardThreads = 512;
+constexpr int kForwardThreads = 256, kForwardBlocks = 2048, kBackwardThreads = 512, kForwardEach = 16, kBackwardEach = 8;
 
 // The team of a width, as a type; false: rows are too short for a vector, or too long for a team.
-template <int XT, int YT, int THREADS, typename F>
+template <int XT, int YT, int THREADS, int EACH, typename F>
 bool with_team(int64_t width, F f) {
     constexpr int N = XT == DDP_FP32 ? 4 : 8;
-    if (width < N || width > 16 * 64 * kEach) return false;
-    if (width <= 8 * kEach) f(Team<XT, YT, 8, 1, THREADS>(0));
-    else if (width <= 32 * kEach) f(Team<XT, YT, 32, 1, THREADS>(0));
-    else if (width <= 64 * kEach) f(Team<XT, YT, 64, 1, THREADS>(0));
-    else if (width <= 2 * 64 * kEach) f(Team<XT, YT, 64, 2, THREADS>(0));
-    else if (width <= 4 * 64 * kEach) f(Team<XT, YT, 64, 4, THREADS>(0));
-    else if (width <= 8 * 64 * kEach) f(Team<XT, YT, 64, 8, std::max(512, THREADS)>(0));
-    else f(Team<XT, YT, 64, 16, 1024>(0));
+    if (width < N || width > 16 * 64 * kMostEach) return false;
+    if (width <= 8 * EACH) f(Team<XT, YT, 8, 1, THREADS, EACH>(0));
+    else if (width <= 32 * EACH) f(Team<XT, YT, 32, 1, THREADS, EACH>(0));
+    else if (width <= 64 * EACH) f(Team<XT, YT, 64, 1, THREADS, EACH>(0));
+    else if (width <= 2 * 64 * EACH) f(Team<XT, YT, 64, 2, THREADS, EACH>(0));
+    else if (width <= 4 * 64 * EACH) f(Team<XT, YT, 64, 4, THREADS, EACH>(0));
+    else if (width <= 8 * 64 * EACH) f(Team<XT, YT, 64, 8, std::max(512, THREADS), EACH>(0));
+    else if (width <= 16 * 64 * EACH) f(Team<XT, YT, 64, 16, 1024, EACH>(0));
+    else f(Team<XT, YT, 64, 16, 1024, kMostEach>(0));
     return true;
 }
 
 template <int XT, int YT>
 hipError_t launch_forward(ddp_layernorm* h, const ForwardArgs& a) {
-    const bool team = with_team<XT, YT, kForwardThreads>(a.width, [&](auto t) {
+    const bool team = with_team<XT, YT, kForwardThreads, kForwardEach>(a.width, [&](auto t) {
         typedef decltype(t) T;
         const int64_t blocks = std::min<int64_t>((a.rows + T::TEAMS - 1) / T::TEAMS, kForwardBlocks);
         hipLaunchKernelGGL((forward_team_kernel<XT, YT, T>), dim3(static_cast<unsigned>(blocks)), dim3(T::THREADS), 0, h->stream, a);
@@ -526,7 +532,7 @@ hipError_t launch_forward(ddp_layernorm* h, const ForwardArgs& a) {
 template <int XT, int YT>
 int32_t launch_backward(ddp_layernorm* h, BackwardArgs a) {
     int32_t chunks = a.chunks;
-    const bool team = with_team<XT, YT, kBackwardThreads>(a.width, [&](auto t) {
+    const bool team = with_team<XT, YT, kBackwardThreads, kBackwardEach>(a.width, [&](auto t) {
         typedef decltype(t) T;
         chunks = static_cast<int32_t>(std::min<int64_t>((a.rows + T::TEAMS - 1) / T::TEAMS, h->chunks));
         hipLaunchKernelGGL((backward_team_kernel<XT, YT, T>), dim3(static_cast<unsigned>(chunks)), dim3(T::THREADS), 0, h->stream, a);
