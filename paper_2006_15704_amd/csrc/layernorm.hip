@@ -101,20 +101,19 @@ struct Team {
         const int team = static_cast<int>(threadIdx.x) / SIZE;
         return LANES == 64 ? __builtin_amdgcn_readfirstlane(team) : team;
     }
-    // Elements that are another vector's, as zeros.
-    __device__ __forceinline__ void clear_shared(float (&x)[V][N]) const {
-        if (!ragged) return;
+    // Elements that are another vector's, or of no row, as zeros.
+    __device__ __forceinline__ void clear_shared(bool live, float (&x)[V][N]) const {
+        if (!ragged && live) return;
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[v][i] = i >= own[v] ? x[v][i] : 0.0f;
+            for (int i = 0; i < N; ++i) x[v][i] = live && i >= own[v] ? x[v][i] : 0.0f;
     }
+    // (No condition, or each load would be waited for before the next: a vector that has nothing reads the row's end.)
     template <int DT>
-    __device__ __forceinline__ void load(const char* row, bool live, Parts<DT, N> (&raw)[V]) const {
+    __device__ __forceinline__ void load(const char* row, Parts<DT, N> (&raw)[V]) const {
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (live && own[v] < N) raw[v] = load_parts<DT, N>(row + static_cast<unsigned>(at[v]) * ElemBytes<DT>::value);
-            else raw[v] = Parts<DT, N>{};
+        for (int v = 0; v < V; ++v) raw[v] = load_parts<DT, N>(row + static_cast<unsigned>(at[v]) * ElemBytes<DT>::value);
     }
     template <int DT>
     __device__ __forceinline__ void store(char* row, bool live, const float (&x)[V][N]) const {
@@ -182,9 +181,10 @@ __global__ __launch_bounds__(T::THREADS) void forward_team_kernel(ForwardArgs a)
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * T::TEAMS; base < a.rows; base += static_cast<int64_t>(gridDim.x) * T::TEAMS) {
         const int64_t row = base + T::mine();
         const bool live = row < a.rows;
+        const int64_t from = live ? row : a.rows - 1;
         Parts<XT, N> x[V], r[V];
-        team.template load<XT>(a.x + row * a.x_stride * ElemBytes<XT>::value, live, x);
-        if (a.residual != nullptr) team.template load<XT>(a.residual + row * a.residual_stride * ElemBytes<XT>::value, live, r);
+        team.template load<XT>(a.x + from * a.x_stride * ElemBytes<XT>::value, x);
+        if (a.residual != nullptr) team.template load<XT>(a.residual + from * a.residual_stride * ElemBytes<XT>::value, r);
         float s[V][N], sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) widen<XT, N>(x[v], s[v]);
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(T::THREADS) void forward_team_kernel(ForwardArgs a)
             }
         }
         if (a.sum != nullptr) team.template store<XT>(a.sum + row * a.sum_stride * ElemBytes<XT>::value, live, s);
-        team.clear_shared(s);
+        team.clear_shared(live, s);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(T::THREADS) void forward_team_kernel(ForwardArgs a)
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < N; ++i) s[v][i] -= mean;
-        team.clear_shared(s);
+        team.clear_shared(live, s);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -245,12 +245,13 @@ __global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs 
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * T::TEAMS; base < a.rows; base += static_cast<int64_t>(gridDim.x) * T::TEAMS) {
         const int64_t row = base + T::mine();
         const bool live = row < a.rows;
+        const int64_t from = live ? row : a.rows - 1;
         Parts<XT, N> x[V], more[V];
         Parts<YT, N> dy[V];
-        team.template load<YT>(a.dy + row * a.dy_stride * ElemBytes<YT>::value, live, dy);
-        team.template load<XT>(a.x + row * a.x_stride * ElemBytes<XT>::value, live, x);
-        if (a.dsum != nullptr && a.dx != nullptr) team.template load<XT>(a.dsum + row * a.dsum_stride * ElemBytes<XT>::value, live, more);
-        const float mean = live ? a.mean[row] : 0.0f, rstd = live ? a.rstd[row] : 0.0f;
+        team.template load<YT>(a.dy + from * a.dy_stride * ElemBytes<YT>::value, dy);
+        team.template load<XT>(a.x + from * a.x_stride * ElemBytes<XT>::value, x);
+        if (a.dsum != nullptr && a.dx != nullptr) team.template load<XT>(a.dsum + from * a.dsum_stride * ElemBytes<XT>::value, more);
+        const float mean = a.mean[from], rstd = a.rstd[from];
         float g[V][N], xh[V][N], of_g = 0.0f, of_gx = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -259,8 +260,8 @@ __global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs 
 #pragma unroll
             for (int i = 0; i < N; ++i) xh[v][i] = (xh[v][i] - mean) * rstd;
         }
-        team.clear_shared(g);
-        team.clear_shared(xh);
+        team.clear_shared(live, g);
+        team.clear_shared(live, xh);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -467,7 +468,7 @@ struct JoinArgs {
     int32_t width, chunks, grad, add;
 };
 // blockIdx.y: dgamma, dbeta.  A wave has 64 columns of a share of the chunks, kJoinWaves of them meet in LDS.
-constexpr int kJoinWaves = 16;
+constexpr int kJoinWaves = 16, kJoinDeep = 16;
 __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
     __shared__ double part[kJoinWaves][64];
     char* out = blockIdx.y == 0 ? a.dgamma : a.dbeta;
@@ -476,12 +477,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
     double sum = 0.0;
     if (c < a.width) {
         const float* from = a.partial + static_cast<int64_t>(blockIdx.y) * a.width + c;
-        for (int k = wave; k < a.chunks; k += kJoinWaves * 8) {
-            float x[8];
+        for (int k = wave; k < a.chunks; k += kJoinWaves * kJoinDeep) {
+            float x[kJoinDeep];                      // (no condition on a load: it would be waited for before the next)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = k + u * kJoinWaves < a.chunks ? from[static_cast<int64_t>(k + u * kJoinWaves) * 2 * a.width] : 0.0f;
+            for (int u = 0; u < kJoinDeep; ++u) x[u] = from[static_cast<int64_t>(min(k + u * kJoinWaves, a.chunks - 1)) * 2 * a.width];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) sum += x[u];
+            for (int u = 0; u < kJoinDeep; ++u) sum += k + u * kJoinWaves < a.chunks ? x[u] : 0.0f;
         }
     }
     part[wave][lane] = sum;

@@ -295,18 +295,18 @@ struct JoinArgs {
     float scale;
 };
 // A wave has 64 sums of a share of the parts, kJoinWaves of them meet in LDS.
-constexpr int kJoinWaves = 16;
+constexpr int kJoinWaves = 16, kJoinDeep = 16;
 __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
     __shared__ double meet[kJoinWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = blockIdx.x * 64 + lane, all = a.heads * a.buckets;
     double sum = 0.0;
     if (at < all) {
-        for (int p = wave; p < a.parts; p += kJoinWaves * 8) {
-            float x[8];
+        for (int p = wave; p < a.parts; p += kJoinWaves * kJoinDeep) {
+            float x[kJoinDeep];                      // (no condition on a load: it would be waited for before the next)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = p + u * kJoinWaves < a.parts ? a.partial[static_cast<int64_t>(p + u * kJoinWaves) * all + at] : 0.0f;
+            for (int u = 0; u < kJoinDeep; ++u) x[u] = a.partial[static_cast<int64_t>(min(p + u * kJoinWaves, a.parts - 1)) * all + at];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) sum += x[u];
+            for (int u = 0; u < kJoinDeep; ++u) sum += p + u * kJoinWaves < a.parts ? x[u] : 0.0f;
         }
     }
     meet[wave][lane] = sum;
