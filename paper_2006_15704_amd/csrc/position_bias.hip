@@ -190,13 +190,13 @@ __device__ __forceinline__ void range_of(const int32_t* first, const BiasArgs& a
     hi = behind ? to : side == 0 && !a.both ? kFar : -from;
 }
 
-template <int ST>
+template <int ST, bool NT>
 __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
     constexpr int N = ST == DDP_FP32 ? 4 : 8, DIAGONALS = Band<N>::diagonals;
     __shared__ float diagonal[kWaves][DIAGONALS + 1];
     __shared__ int32_t first[kMaxBuckets];
     extern __shared__ double sums[];                 // of the buckets
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     for (int k = threadIdx.x; k < a.sides; k += kThreads) first[k] = a.first[k];
     for (int k = threadIdx.x; k < a.buckets; k += kThreads) sums[k] = 0.0;
     const int64_t h = blockIdx.x % a.heads;
@@ -204,24 +204,27 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
     const int64_t groups = (a.queries + N - 1) / N, vectors = (a.keys + N - 1) / N;
     const char* scores = a.scores + h * a.s_head * ElemBytes<ST>::value;
     for (int64_t strip = part / a.shares; strip < a.strips; strip += a.strip_blocks) {
-        const int64_t t0 = a.band0 + strip * 64, t = t0 + lane;
-        // the row groups in which some lane has a column
-        const int64_t g_from = max(int64_t(0), -(t0 + 63)), g_to = min(groups, vectors - t0);
-        const int64_t steps = max(g_to - g_from, int64_t(0)), turns = static_cast<int64_t>(a.shares) * kWaves;
-        const int64_t each = (steps + turns - 1) / turns, turn = static_cast<int64_t>(share) * kWaves + wave;
-        const int64_t mine_from = g_from + min(turn * each, steps), mine_to = g_from + min(turn * each + each, steps);
+        const int64_t t0 = a.band0 + strip * 64;
+        // the row groups in which some lane has a column, of all sequences, in equal parts for all waves of the shares
+        const int64_t g_from = max(int64_t(0), -(t0 + 63)), steps = max(min(groups, vectors - t0) - g_from, int64_t(0));
+        const int64_t units = steps * a.batch, turns = static_cast<int64_t>(a.shares) * kWaves;
+        const int64_t each = (units + turns - 1) / turns, mine = (static_cast<int64_t>(share) * kWaves + wave) * each;
+        int64_t left = min(each, units - mine);
         float acc[2 * N - 1] = {};
-        for (int64_t b = 0; b < a.batch; ++b) {
+        for (int64_t b = left > 0 ? mine / steps : 0, g = g_from + (left > 0 ? mine % steps : 0); left > 0; ++b, g = g_from) {
             const int64_t keys = length_of(a.key_lengths, b, a.keys), queries = length_of(a.query_lengths, b, a.queries);
+            const int64_t here = min(left, g_from + steps - g), end = min(g + here, (queries + N - 1) / N);
+            left -= here;
             const char* s = scores + b * a.s_batch * ElemBytes<ST>::value;
-            for (int64_t g = mine_from; g < mine_to; ++g) {
-                const int64_t c = (g + t) * N, i = g * N;
-                if (c < 0 || c >= keys || i >= queries) continue;
-                const char* at = s + (i * a.s_query + c) * ElemBytes<ST>::value;
+            for (; g < end; ++g) {
+                const int64_t i = g * N;
+                const int c = static_cast<int>(g + t0 + lane) * N;
+                const unsigned at = static_cast<unsigned>(c) * ElemBytes<ST>::value;
+                if (c < 0 || c >= keys) continue;
                 if (c + N <= keys && i + N <= queries) {
                     Parts<ST, N> v[N];
 #pragma unroll
-                    for (int x = 0; x < N; ++x) v[x] = load_parts<ST, N, true>(at + x * a.s_query * ElemBytes<ST>::value);
+                    for (int x = 0; x < N; ++x) v[x] = load_parts<ST, N, NT>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at);
 #pragma unroll
                     for (int x = 0; x < N; ++x) {
                         float e[N];
@@ -230,12 +233,20 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
                         for (int k = 0; k < N; ++k) acc[k - x + N - 1] += e[k];
                     }
                 } else {
+                    // element by element, where a row or a sequence ends: the sums go round instead of the rows being unrolled
+                    const int have = static_cast<int>(min(keys - c, int64_t(N)));
+#pragma unroll 1
+                    for (int x = 0; x < 2 * N - 1; ++x) {
+                        if (x < N && i + x < queries) {
+                            float e[N];
+                            load_some<ST, N>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at, have, e);
 #pragma unroll
-                    for (int x = 0; x < N; ++x) {
-                        float e[N];
-                        load_some<ST, N>(at + x * a.s_query * ElemBytes<ST>::value, i + x < queries ? static_cast<int>(min(keys - c, int64_t(N))) : 0, e);
+                            for (int k = 0; k < N; ++k) acc[k + N - 1] += e[k];
+                        }
+                        const float last = acc[2 * N - 2];
 #pragma unroll
-                        for (int k = 0; k < N; ++k) acc[k - x + N - 1] += e[k];
+                        for (int k = 2 * N - 2; k > 0; --k) acc[k] = acc[k - 1];
+                        acc[0] = last;
                     }
                 }
             }
@@ -326,7 +337,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
 
 constexpr int64_t kMaxTiles = int64_t(1) << 20, kTiles = 2048;
 constexpr int kTileRows = 64;
-constexpr int64_t kGradBlocks = 2048, kGradSteps = 4;
+constexpr int64_t kGradBlocks = 2048, kGradSteps = 4, kStreamBytes = int64_t(1) << 28;
 constexpr int64_t kPartBytes = int64_t(1) << 24;     // of the workspace, if 64 parts do not take more
 
 template <int TT, int OT>
@@ -541,9 +552,15 @@ int32_t ddp_position_bias_grad(ddp_position_bias* h, int64_t batch, int64_t quer
             parts = static_cast<int64_t>(a.strip_blocks) * a.shares;
             const dim3 grid(static_cast<unsigned>(parts * h->heads));
             const size_t bytes = static_cast<size_t>(a.buckets) * 8;
-            if (dtype == DDP_FP32) hipLaunchKernelGGL((diagonal_kernel<DDP_FP32>), grid, dim3(kThreads), bytes, h->stream, a);
-            else if (dtype == DDP_FP16) hipLaunchKernelGGL((diagonal_kernel<DDP_FP16>), grid, dim3(kThreads), bytes, h->stream, a);
-            else hipLaunchKernelGGL((diagonal_kernel<DDP_BF16>), grid, dim3(kThreads), bytes, h->stream, a);
+            const bool stream = batch * h->heads * queries * keys * elem_bytes(dtype) >= kStreamBytes;
+            auto launch = [&](auto st, auto nt) { hipLaunchKernelGGL((diagonal_kernel<st.value, nt.value>), grid, dim3(kThreads), bytes, h->stream, a); };
+            auto typed = [&](auto nt) {
+                if (dtype == DDP_FP32) launch(std::integral_constant<int, DDP_FP32>(), nt);
+                else if (dtype == DDP_FP16) launch(std::integral_constant<int, DDP_FP16>(), nt);
+                else launch(std::integral_constant<int, DDP_BF16>(), nt);
+            };
+            if (stream) typed(std::true_type());
+            else typed(std::false_type());
         }
         LAYER_HIP(h, hipGetLastError());
     } else if (accumulate) {
