@@ -697,7 +697,7 @@ int32_t ddp_position_bias_apply(ddp_position_bias* bias, int64_t batch, int64_t 
 
 /* grad[k][h] = scale * sum of dscores[b, h, i, j] over the visible places of bucket k (zeros where there are none; accumulate != 0:
  * added to what grad holds).  Places are visible as above, and only queries i < query_lengths[b] (NULL: all) take part.  Strides of dscores
- * may be anything from 0 on (0: the same scores for all).  Sums in binary32 along a diagonal and binary64 across, in an order that depends on the sizes
+ * may be anything from 0 on (0: the same scores for all); what lies between its rows is memory that can be read.  Sums in binary32 along a diagonal and binary64 across, in an order that depends on the sizes
  * alone (repeated calls give the same bits), rounded once. */
 int32_t ddp_position_bias_grad(ddp_position_bias* bias, int64_t batch, int64_t queries, int64_t keys, int64_t offset, const void* dscores,
                                int32_t dtype, int64_t batch_stride, int64_t head_stride, int64_t query_stride, float scale,

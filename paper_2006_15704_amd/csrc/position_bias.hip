@@ -216,15 +216,28 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
             const int64_t here = min(left, g_from + steps - g), end = min(g + here, (queries + N - 1) / N);
             left -= here;
             const char* s = scores + b * a.s_batch * ElemBytes<ST>::value;
+            const int64_t room = (a.batch - 1 - b) * a.s_batch + (a.heads - 1 - h) * a.s_head + (a.queries - 1) * a.s_query + a.keys;
             for (; g < end; ++g) {
                 const int64_t i = g * N;
                 const int c = static_cast<int>(g + t0 + lane) * N;
                 const unsigned at = static_cast<unsigned>(c) * ElemBytes<ST>::value;
                 if (c < 0 || c >= keys) continue;
-                if (c + N <= keys && i + N <= queries) {
+                // (what follows a row's keys is read with them, as far as the tensor reaches, and not used)
+                if ((i + N - 1) * a.s_query + c + N <= room) {
                     Parts<ST, N> v[N];
 #pragma unroll
                     for (int x = 0; x < N; ++x) v[x] = load_parts<ST, N, NT>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at);
+                    const bool partial = c + N > keys || i + N > queries;
+                    const int have = static_cast<int>(min(keys - c, int64_t(N))), rows = static_cast<int>(min(queries - i, int64_t(N)));
+                    if (__ballot(partial) != 0) {
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const int in = have * ElemBytes<ST>::value - 4 * w;          // bytes of this word
+                            const uint32_t keep = in >= 4 ? ~0u : in == 2 ? 0xFFFFu : 0u;
+#pragma unroll
+                            for (int x = 0; x < N; ++x) v[x].part[0].w[w] &= x < rows ? keep : 0u;
+                        }
+                    }
 #pragma unroll
                     for (int x = 0; x < N; ++x) {
                         float e[N];
@@ -233,7 +246,7 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
                         for (int k = 0; k < N; ++k) acc[k - x + N - 1] += e[k];
                     }
                 } else {
-                    // element by element, where a row or a sequence ends: the sums go round instead of the rows being unrolled
+                    // element by element in the tensor's last rows: the sums go round instead of the rows being unrolled
                     const int have = static_cast<int>(min(keys - c, int64_t(N)));
 #pragma unroll 1
                     for (int x = 0; x < 2 * N - 1; ++x) {
