@@ -3,6 +3,7 @@ lookup, backward pass, embedding gradient, bucketed synchronization, global
 norm, AdamW.
 
     python -m paper_2006_15704_amd.train --replicas 4 --bits 8
+    python -m paper_2006_15704_amd.train --layer --replicas 4
 
 The model predicts the next token from the last one: logits = x W^T + b with
 x = scale * table[token].  Its tokens follow a fixed random successor nine times out
@@ -10,6 +11,11 @@ of ten, so the loss falls from log(vocabulary) towards the entropy of that.
 R replicas (the R training processes) draw their own batches; the library averages their
 gradients and steps replica 0's parameters, which all replicas read.  The products and the
 softmax in between are PyTorch's.
+
+With --layer a transformer layer stands between the two: attention with a learned relative position bias and experts chosen by a
+router, behind layer norms (`layer.py`).  A replica's count of tokens for an expert says whether it takes part in that expert's
+gradients; parameters of experts that no replica used keep their values; and the counts of all replicas move the router's
+balance bias.
 """
 from __future__ import annotations
 
@@ -21,8 +27,10 @@ import torch
 
 from . import binding as B
 from . import harness
+from . import layer
 
 LR, BETA1, BETA2, EPS, DECAY, MAX_NORM = 0.02, 0.9, 0.99, 1e-8, 0.01, 1.0
+LAYER_LR, BALANCE = 5e-3, 1e-3
 
 
 class Task:
@@ -109,6 +117,70 @@ def run(replicas: int = 2, vocabulary: int = 512, width: int = 64, tokens: int =
     return losses
 
 
+def sequences(task: Task, s: layer.Sizes, seed: int):
+    """(tokens, their successors, lengths): sequences of half to all of the length, -1 behind them."""
+    gen = torch.Generator().manual_seed(seed)
+    lengths = torch.randint(s.length // 2, s.length + 1, (s.sequences,), generator=gen)
+    now, then = (x.view(s.sequences, s.length) for x in task.batch(s.sequences * s.length, seed))
+    behind = torch.arange(s.length)[None, :] >= lengths[:, None]
+    return now.masked_fill(behind, -1), then, lengths.int()
+
+
+def run_layer(replicas: int = 2, steps: int = 40, bits: int = 32, sizes: layer.Sizes = layer.Sizes(), seed: int = 0, log=print) -> List[float]:
+    """Trains the model with a layer; returns the mean loss over the replicas at every step."""
+    device = harness.require_gpu()
+    task = Task(sizes.vocabulary, seed)
+    params = {k: v.to(device) for k, v in layer.initial(sizes, seed).items()}
+    keys = list(params)
+    numel = [params[k].numel() for k in keys]
+    n = len(keys)
+    grads = harness.DeviceGrads(numel, [B.DDP_FP32] * n, replicas, fill=0)
+    grad = [{k: grads.view(r, i).view(torch.float32).view(params[k].shape) for i, k in enumerate(keys)} for r in range(replicas)]
+    losses = []
+    with harness.Session(grads, 64 * 1024, B.DDP_PIPELINE_FUSED) as s:
+        B.ddp_set_option(s.ctx, B.DDP_OPT_FIND_UNUSED, 1)
+        stream = s.backward_stream.cuda_stream
+        opt = B.ddp_opt_create(0, stream)
+        kind = B.DDP_STATE_8BIT if bits == 8 else B.DDP_STATE_FP32
+        _, layout = B.ddp_opt_state_layout(numel, kind)
+        state = torch.zeros(layout["bytes"], dtype=torch.uint8, device=device)
+        norm = torch.zeros(1, device=device)
+        B.ddp_opt_register(opt, numel, [B.DDP_FP32] * n, [params[k].data_ptr() for k in keys], [B.DDP_FP32] * n, [grads.ptr(0, i) for i in range(n)])
+        B.ddp_opt_set_groups(opt, None, [0.0 if params[k].dim() == 1 else 1.0 for k in keys])
+        B.ddp_opt_set_state(opt, kind, state.data_ptr(), layout["bytes"])
+        counts = torch.zeros((replicas, sizes.experts), dtype=torch.int32, device=device)
+        balance = torch.zeros(sizes.experts, device=device)
+        torch.cuda.synchronize()
+        model = layer.Layer(sizes, stream)
+        with torch.cuda.stream(s.backward_stream):
+            for step in range(steps):
+                total, load = torch.zeros((), device=device), []
+                for r in range(replicas):
+                    batch = [x.to(device) for x in sequences(task, sizes, (seed * 100003 + step) * 64 + r)]
+                    loss, counted = model.step(params, grad[r], balance, *batch, counts[r])
+                    total += loss / replicas
+                    load.append(counted)
+                for i in reversed(range(n)):
+                    expert = layer.expert_of(keys[i])
+                    if expert >= 0:                                  # takes part where tokens have reached it
+                        B.ddp_mark_ready_local(s.ctx, i, [c[expert] > 0 for c in load])
+                    else:
+                        B.ddp_mark_ready(s.ctx, i)
+                B.ddp_finalize_backward(s.ctx)
+                used = B.ddp_get_global_used(s.ctx, n)
+                B.ddp_opt_grad_norm(opt, 1.0, norm.data_ptr(), used)
+                B.ddp_opt_adamw_step(opt, LAYER_LR, BETA1, BETA2, EPS, DECAY, 1.0, MAX_NORM, True, used)
+                B.ddp_router_balance(model.router, replicas, counts.data_ptr(), BALANCE, balance.data_ptr(), balance.data_ptr())
+                losses.append(total.item())
+                if log and (step % 10 == 0 or step + 1 == steps):
+                    log(f"step {step:3d}  loss {losses[-1]:.4f}  gradient norm {norm.item():.4f}  tokens of an expert "
+                        f"{min(map(sum, zip(*load)))} to {max(map(sum, zip(*load)))}", flush=True)
+        torch.cuda.synchronize()
+        model.close()
+        B.ddp_opt_destroy(opt)
+    return losses
+
+
 def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--replicas", type=int, default=2)
@@ -117,8 +189,9 @@ def main() -> None:
     ap.add_argument("--tokens", type=int, default=1024, help="per replica and step")
     ap.add_argument("--steps", type=int, default=40)
     ap.add_argument("--bits", type=int, choices=(32, 8), default=32, help="of an element of the optimizer's state")
+    ap.add_argument("--layer", action="store_true", help="with a transformer layer (vocabulary and width are its own then)")
     a = ap.parse_args()
-    losses = run(a.replicas, a.vocabulary, a.width, a.tokens, a.steps, a.bits)
+    losses = run_layer(a.replicas, a.steps, a.bits) if a.layer else run(a.replicas, a.vocabulary, a.width, a.tokens, a.steps, a.bits)
     print(f"loss {losses[0]:.4f} -> {losses[-1]:.4f} in {a.steps} steps")
 
 
