@@ -81,7 +81,7 @@ inline void layer_release(LayerHandle* h) {
 
 #if defined(__HIPCC__)
 
-// Sums over the LANES (8, 16, 32 or 64) neighbours of a lane, the same bits in all of them: neighbours within 16 by the VALU's lane
+// Sums over the LANES (4, 8, 16, 32 or 64) neighbours of a lane, the same bits in all of them: neighbours within 16 by the VALU's lane
 // moves, further ones by swaps of rows.  (A shuffle is an LDS access: six of them one after the other take some 0.4 us of a wave.)
 template <int CTRL>
 __device__ __forceinline__ float lane_moved(float x) {
@@ -101,7 +101,7 @@ template <int LANES>
 __device__ __forceinline__ float lanes_sum(float x) {
     x += lane_moved<0xB1>(x);                        // quad_perm: 1 0 3 2
     x += lane_moved<0x4E>(x);                        // quad_perm: 2 3 0 1
-    x += lane_moved<0x141>(x);                       // row_half_mirror
+    if constexpr (LANES >= 8) x += lane_moved<0x141>(x);        // row_half_mirror
     if constexpr (LANES >= 16) x += lane_moved<0x140>(x);       // row_mirror
     if constexpr (LANES >= 32) x = rows_of_16_summed(x);
     if constexpr (LANES >= 64) x = halves_summed(x);

@@ -238,8 +238,22 @@ __global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs 
     __shared__ float meet[2][T::THREADS / 64 * 2];
     __shared__ float part[MEET > 1 ? MEET / 2 : 1][2][MEET > 1 ? T::SIZE * T::EACH : 1];
     const T team(a.width);
+    // of the widest rows a lane's sums of the parameters' gradients are in LDS, which registers do not suffice for
+    constexpr bool IN_LDS = T::WAVES == 16 && T::EACH == kMostEach;
+    __shared__ __attribute__((aligned(16))) float held[IN_LDS ? 2 * V : 1][IN_LDS ? T::SIZE : 1][N];
     float gamma[V][N], dgamma[V][N] = {}, dbeta[V][N] = {};
     team.params(a.gamma, a.param, 1.0f, gamma);
+    auto hold = [&](int at, float (&x)[N], bool add) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) held[at][threadIdx.x][i] = add ? held[at][threadIdx.x][i] + x[i] : x[i];
+    };
+    if constexpr (IN_LDS) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            hold(v, dgamma[v], false);
+            hold(V + v, dbeta[v], false);
+        }
+    }
     const float each = 1.0f / a.width;
     int turn = 0;
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * T::TEAMS; base < a.rows; base += static_cast<int64_t>(gridDim.x) * T::TEAMS) {
@@ -262,12 +276,28 @@ __global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs 
         }
         team.clear_shared(live, g);
         team.clear_shared(live, xh);
+        if constexpr (IN_LDS) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float x[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = g[v][i] * xh[v][i];
+                hold(v, x, true);
+                hold(V + v, g[v], true);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    dgamma[v][i] += g[v][i] * xh[v][i];
+                    dbeta[v][i] += g[v][i];
+                }
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                dgamma[v][i] += g[v][i] * xh[v][i];
-                dbeta[v][i] += g[v][i];
                 g[v][i] *= gamma[v][i];
                 of_g += g[v][i];
                 of_gx += g[v][i] * xh[v][i];
@@ -292,6 +322,15 @@ __global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs 
         team.template store<XT>(a.dx + row * a.dx_stride * ElemBytes<XT>::value, live, g);
     }
     if (a.partial == nullptr) return;
+    if constexpr (IN_LDS) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                dgamma[v][i] = held[v][threadIdx.x][i];
+                dbeta[v][i] = held[V + v][threadIdx.x][i];
+            }
+    }
     if constexpr (!WIDE) {
 #pragma unroll
         for (int d = T::LANES; d < 64; d <<= 1)
@@ -507,7 +546,9 @@ template <int XT, int YT, int THREADS, int EACH, typename F>
 bool with_team(int64_t width, F f) {
     constexpr int N = XT == DDP_FP32 ? 4 : 8;
     if (width < N || width > 16 * 64 * kMostEach) return false;
-    if (width <= 8 * EACH) f(Team<XT, YT, 8, 1, THREADS, EACH>(0));
+    if (width <= 4 * N) f(Team<XT, YT, 4, 1, THREADS, N>(0));
+    else if (width <= 8 * N) f(Team<XT, YT, 8, 1, THREADS, N>(0));
+    else if (width <= 8 * EACH) f(Team<XT, YT, 8, 1, THREADS, EACH>(0));
     else if (width <= 32 * EACH) f(Team<XT, YT, 32, 1, THREADS, EACH>(0));
     else if (width <= 64 * EACH) f(Team<XT, YT, 64, 1, THREADS, EACH>(0));
     else if (width <= 2 * 64 * EACH) f(Team<XT, YT, 64, 2, THREADS, EACH>(0));

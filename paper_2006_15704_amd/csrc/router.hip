@@ -254,8 +254,14 @@ __device__ __forceinline__ void meet_lanes(int log2, F f) {
     if (log2 > 1) f([](uint32_t x) { return lane_moved<0x4E>(x); });         // quad_perm: 2 3 0 1
     if (log2 > 2) f([](uint32_t x) { return lane_moved<0x141>(x); });        // row_half_mirror
     if (log2 > 3) f([](uint32_t x) { return lane_moved<0x140>(x); });        // row_mirror
-    if (log2 > 4) f([](uint32_t x) { return static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 16)); });
-    if (log2 > 5) f([](uint32_t x) { return static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), 32)); });
+    if (log2 > 4) f([](uint32_t x) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    });
+    if (log2 > 5) f([](uint32_t x) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    });
 }
 __device__ __forceinline__ float as_float(uint32_t x) { return __builtin_bit_cast(float, x); }
 __device__ __forceinline__ uint32_t as_bits(float x) { return __builtin_bit_cast(uint32_t, x); }
