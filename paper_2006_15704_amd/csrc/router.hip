@@ -208,7 +208,6 @@ __device__ __forceinline__ void add_counts(const RouteArgs& a, const int32_t* co
 
 // All tokens (where no team's lanes divide into the groups), or those that teams have left.
 constexpr int32_t kAgain = -2;
-constexpr int kLooked = 16;                      // tokens that a wave looks through at a time
 template <int LT, bool ALL>
 __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     extern __shared__ double keys[];                 // [kWaves][experts], then the counts
@@ -219,10 +218,12 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     if constexpr (ALL) {
         for (int64_t t = static_cast<int64_t>(blockIdx.x) * kWaves + wave; t < a.tokens; t += static_cast<int64_t>(gridDim.x) * kWaves) route_token<LT>(a, t, mine, counts);
     } else {
-        for (int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kWaves + wave) * kLooked; t0 < a.tokens; t0 += static_cast<int64_t>(gridDim.x) * kWaves * kLooked) {
-            const bool left = lane < kLooked && t0 + lane < a.tokens && a.experts_out[(t0 + lane) * a.chosen] == kAgain;
-            for (uint64_t some = __ballot(left); some != 0; some &= some - 1)
-                route_token<LT>(a, t0 + __ffsll(static_cast<unsigned long long>(some)) - 1, mine, counts);
+        for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * 64; t0 < a.tokens; t0 += static_cast<int64_t>(gridDim.x) * 64) {
+            const bool left = t0 + lane < a.tokens && a.experts_out[(t0 + lane) * a.chosen] == kAgain;
+            __syncthreads();                         // (all waves look before one of them is done with a token)
+            int n = 0;
+            for (uint64_t some = __ballot(left); some != 0; some &= some - 1, ++n)
+                if (n % kWaves == wave) route_token<LT>(a, t0 + __ffsll(static_cast<unsigned long long>(some)) - 1, mine, counts);
         }
     }
     add_counts<ALL>(a, counts);
@@ -240,8 +241,8 @@ constexpr int kEach = 16, kSpare = 2;
 // A key's error in parts of 2^-24 of the largest score and bias: exp, sum and quotient of a softmax over 1024 under 30, the key's
 // rounding and the lift's 6 (a lifted key is up to twice as large), the bits given to the place 64: two keys 200.
 constexpr float kApart = 0x1p-16f;
-// The same of whole keys: 30 and 3 each of a softmax, 5 of a sigmoid.
-constexpr float kNearSoftmax = 0x1p-17f, kNearSigmoid = 0x1p-20f;
+// The same of whole keys: 30 of the largest score and 3 of score and bias each of a softmax, 5 of a sigmoid.
+constexpr float kNearSoftmax = 0x1p-18f, kNearKey = 0x1p-20f;
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t lane_moved(uint32_t x) {
@@ -438,7 +439,7 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
             for (int n = l; n < a.listed; n += lanes)
                 if (at[n] >= 0) word[n] = as_bits(score(logit(at[n])) + bias_of(at[n]));
             wave_meets();
-            const float same = (a.score == DDP_SCORE_SOFTMAX ? kNearSoftmax : kNearSigmoid) * (most + of_bias);
+            const float same = (a.score == DDP_SCORE_SOFTMAX ? kNearSoftmax * most : 0.0f) + kNearKey * (most + of_bias);
             for (int n = l; n < a.listed; n += lanes) {
                 const int e = at[n];
                 if (e < 0) continue;
@@ -671,7 +672,7 @@ bool launch_team(ddp_router* h, const RouteArgs& a, int64_t blocks, size_t bytes
     } else {
         launch(std::integral_constant<int, -1>());
     }
-    const int64_t looks = (a.tokens + kWaves * kLooked - 1) / (kWaves * kLooked);
+    const int64_t looks = (a.tokens + 63) / 64;      // tokens that a block looks through at a time
     hipLaunchKernelGGL((route_kernel<LT, false>), dim3(static_cast<unsigned>(std::min(looks, kBlocks))), dim3(kThreads),
                        static_cast<size_t>(kWaves * 8 + 4) * a.experts, h->stream, a);
     return true;
