@@ -320,20 +320,29 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
     uint32_t* word = reinterpret_cast<uint32_t*>(behind) + team * a.listed;          // of each candidate: its key, then its weight
     int32_t* at = reinterpret_cast<int32_t*>(behind) + (teams + team) * a.listed;    // its expert, or -1
     int32_t* place = reinterpret_cast<int32_t*>(behind) + (2 * teams + team) * a.listed;      // its rank, once ordered
-    int32_t* counts = reinterpret_cast<int32_t*>(behind) + 3 * teams * a.listed;
+    float* lifted = reinterpret_cast<float*>(behind) + 3 * teams * a.listed;
+    int32_t* counts = reinterpret_cast<int32_t*>(behind) + 3 * teams * a.listed + max(EACH << log2_lanes, kWaves);
     uint32_t* sorted = reinterpret_cast<uint32_t*>(keys + wave * a.room) + lane;     // the lane's words, 64 apart
     clear_counts(a, counts);
     const int e0 = l * a.each, mine = max(min(a.experts - e0, a.each), 0);
-    float bias[EACH], of_bias = 0.0f;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        bias[i] = a.bias != nullptr && i < mine ? a.bias[e0 + i] : 0.0f;
-        of_bias = fmaxf(of_bias, fabsf(bias[i]) < __builtin_huge_valf() ? fabsf(bias[i]) : 0.0f);
+    // biases, lifted, in LDS: the i-th of a team's lanes side by side (in registers they would cost a wave in six)
+    float of_bias = 0.0f;
+    for (int e = threadIdx.x; a.bias != nullptr && e < a.experts; e += kThreads) {
+        const float x = fabsf(a.bias[e]);
+        of_bias = fmaxf(of_bias, x < __builtin_huge_valf() ? x : 0.0f);
     }
-    of_bias = team_max(log2_lanes, of_bias);
+    of_bias = team_max(6, of_bias);
+    if (lane == 0) lifted[wave] = of_bias;
+    __syncthreads();
+    of_bias = fmaxf(fmaxf(lifted[0], lifted[1]), fmaxf(lifted[2], lifted[3]));
+    static_assert(kWaves == 4, "");
     const float lift = of_bias * (1.0f + 0x1p-20f) + 0x1p-60f;       // (above every -bias)
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) bias[i] = i < mine ? bias[i] + lift : kMasked;
+    __syncthreads();
+    for (int i = threadIdx.x; i < EACH << log2_lanes; i += kThreads) {
+        const int of = i & (lanes - 1), k = i >> log2_lanes, e = of * a.each + k;
+        lifted[i] = k < a.each && e < a.experts ? (a.bias != nullptr ? a.bias[e] : 0.0f) + lift : kMasked;
+    }
+    __syncthreads();
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * teams; base < a.tokens; base += static_cast<int64_t>(gridDim.x) * teams) {
         const int64_t t = base + team;
         const bool live = t < a.tokens;
@@ -373,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
         uint32_t w[EACH];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const float key = s[i] + bias[i];
+            const float key = s[i] + lifted[(i << log2_lanes) + l];
             w[i] = x[i] != kMasked && key > 0.0f ? (as_bits(key) & ~15u) | static_cast<uint32_t>(15 - i) : 0u;
         }
         sort_words<EACH>(w);
@@ -686,7 +695,9 @@ bool launch_route(ddp_router* h, RouteArgs a) {
     }
     const int teams = kThreads >> a.log2_lanes;
     const int64_t blocks = (a.tokens + teams - 1) / teams;
-    const size_t bytes = static_cast<size_t>(kWaves) * a.room * 8 + static_cast<size_t>(teams) * a.listed * 12 + static_cast<size_t>(a.experts) * 4;
+    const int each = a.each > 8 ? 16 : a.each > 4 ? 8 : a.each > 2 ? 4 : a.each;
+    const size_t bytes = static_cast<size_t>(kWaves) * a.room * 8 + static_cast<size_t>(teams) * a.listed * 12 + static_cast<size_t>(a.experts) * 4 +
+                         (std::max(each << a.log2_lanes, kWaves)) * size_t(4);
     if (a.each > 8) return launch_team<LT, 16>(h, a, blocks, bytes);
     if (a.each > 4) return launch_team<LT, 8>(h, a, blocks, bytes);
     if (a.each > 2) return launch_team<LT, 4>(h, a, blocks, bytes);
