@@ -19,13 +19,14 @@ using namespace ddp;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int64_t kMaxWidth = int64_t(1) << 20, kMaxRows = INT32_MAX;
+constexpr int64_t kStreamBytes = int64_t(4) << 20;
 
 struct ForwardArgs {
     const char *x, *residual, *gamma, *beta;
     char *sum, *y;
     float *mean, *rstd;
     int64_t rows, x_stride, residual_stride, sum_stride, y_stride;
-    int32_t width, param;
+    int32_t width, param, stream;
     float eps;
 };
 struct BackwardArgs {
@@ -34,7 +35,7 @@ struct BackwardArgs {
     char *dx;
     float* partial;
     int64_t rows, dy_stride, x_stride, dsum_stride, dx_stride, rows_per_chunk;
-    int32_t width, param, chunks;
+    int32_t width, param, chunks, stream;
 };
 
 // gamma or beta: `none` where there is none.
@@ -115,14 +116,14 @@ struct Team {
 #pragma unroll
         for (int v = 0; v < V; ++v) raw[v] = load_parts<DT, N>(row + static_cast<unsigned>(at[v]) * ElemBytes<DT>::value);
     }
-    template <int DT>
+    template <int DT, bool NT = false>
     __device__ __forceinline__ void store(char* row, bool live, const float (&x)[V][N]) const {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live || own[v] == N) continue;
             char* to = row + static_cast<unsigned>(at[v]) * ElemBytes<DT>::value;
             if (own[v] == 0) {
-                store_some<DT, N>(to, N, x[v]);
+                store_some<DT, N, NT>(to, N, x[v]);
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
@@ -169,6 +170,12 @@ struct Team {
     }
 };
 
+template <typename T, int DT>
+__device__ __forceinline__ void put(const T& team, int stream, char* row, bool live, const float (&x)[T::V][T::N]) {
+    if (stream) team.template store<DT, true>(row, live, x);
+    else team.template store<DT>(row, live, x);
+}
+
 template <int XT, int YT, typename T>
 __global__ __launch_bounds__(T::THREADS) void forward_team_kernel(ForwardArgs a) {
     constexpr int N = T::N, V = T::V;
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(T::THREADS) void forward_team_kernel(ForwardArgs a)
                 for (int i = 0; i < N; ++i) s[v][i] += more[i];
             }
         }
-        if (a.sum != nullptr) team.template store<XT>(a.sum + row * a.sum_stride * ElemBytes<XT>::value, live, s);
+        if (a.sum != nullptr) put<T, XT>(team, a.stream, a.sum + row * a.sum_stride * ElemBytes<XT>::value, live, s);
         team.clear_shared(live, s);
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -221,7 +228,7 @@ __global__ __launch_bounds__(T::THREADS) void forward_team_kernel(ForwardArgs a)
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < N; ++i) s[v][i] = s[v][i] * rstd * gamma[v][i] + beta[v][i];
-        team.template store<YT>(a.y + row * a.y_stride * ElemBytes<YT>::value, live, s);
+        put<T, YT>(team, a.stream, a.y + row * a.y_stride * ElemBytes<YT>::value, live, s);
         if (live && threadIdx.x % T::SIZE == 0) {
             if (a.mean != nullptr) a.mean[row] = mean;
             if (a.rstd != nullptr) a.rstd[row] = rstd;
@@ -319,7 +326,7 @@ __global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs 
                 for (int i = 0; i < N; ++i) g[v][i] += m[i];
             }
         }
-        team.template store<XT>(a.dx + row * a.dx_stride * ElemBytes<XT>::value, live, g);
+        put<T, XT>(team, a.stream, a.dx + row * a.dx_stride * ElemBytes<XT>::value, live, g);
     }
     if (a.partial == nullptr) return;
     if constexpr (IN_LDS) {
@@ -625,7 +632,8 @@ int32_t ddp_layernorm_create(ddp_layernorm** out, int32_t device, void* stream, 
     h->device = device;
     h->stream = static_cast<hipStream_t>(stream);
     h->width = width;
-    h->chunks = static_cast<int32_t>(std::max<int64_t>(16, std::min<int64_t>(512, (int64_t(1) << 22) / width)));
+    // two blocks a compute unit, one of the widest teams
+    h->chunks = static_cast<int32_t>(std::max<int64_t>(16, std::min<int64_t>(width <= 8 * 1024 ? 512 : 256, (int64_t(1) << 22) / width)));
     if (device != DDP_DEVICE_NONE) {
         const hipError_t err = layer_alloc(h, static_cast<int64_t>(h->chunks) * 2 * width * 4);
         if (err != hipSuccess) {
@@ -681,6 +689,7 @@ int32_t ddp_layernorm_forward(ddp_layernorm* h, int64_t rows, const void* x, int
     a.width = static_cast<int32_t>(h->width);
     a.param = param_dtype;
     a.eps = eps;
+    a.stream = rows * h->width * elem_bytes(y_dtype) >= kStreamBytes;
     LAYER_HIP(h, with_types(x_dtype, y_dtype, [&](auto xt, auto yt) { return launch_forward<xt.value, yt.value>(h, a); }));
     return DDP_OK;
 }
@@ -723,6 +732,7 @@ int32_t ddp_layernorm_backward(ddp_layernorm* h, int64_t rows, const void* dy, i
     a.chunks = static_cast<int32_t>((rows + a.rows_per_chunk - 1) / a.rows_per_chunk);
     a.width = static_cast<int32_t>(h->width);
     a.param = param_dtype;
+    a.stream = rows * h->width * elem_bytes(x_dtype) >= kStreamBytes;
     int32_t chunks = 0;
     if (rows > 0) {
         chunks = with_types(x_dtype, dy_dtype, [&](auto xt, auto yt) { return launch_backward<xt.value, yt.value>(h, a); });

@@ -73,7 +73,7 @@ struct BiasArgs {
     char* scores;                                // dscores in the gradient
     float* partial;
     int64_t batch, queries, keys, offset, table_stride, s_batch, s_head, s_query;
-    int64_t band0, strips;                       // of the gradient: the first lane of the first strip
+    int64_t band0, strips, center;               // of the gradient: the first lane of the first strip
     int64_t tiles, plane_tiles, col_tiles;       // of the bias
     int32_t heads, buckets, sides, both, causal, strip_blocks, shares, rows, cols, log2_cols;
     float scale, masked;
@@ -190,6 +190,13 @@ __device__ __forceinline__ void range_of(const int32_t* first, const BiasArgs& a
     hi = behind ? to : side == 0 && !a.both ? kFar : -from;
 }
 
+// Strips of the longest diagonals come first, so that the short ones fill in at the end: from `center` to both sides, then what is left of one.
+__device__ __forceinline__ int64_t strip_of(const BiasArgs& a, int64_t turn) {
+    const int64_t below = a.center, above = a.strips - 1 - a.center, both = below < above ? below : above;
+    if (turn <= 2 * both) return a.center + ((turn & 1) ? (turn + 1) / 2 : -(turn / 2));
+    return below < above ? turn : a.strips - 1 - turn;
+}
+
 template <int ST, bool NT>
 __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
     constexpr int N = ST == DDP_FP32 ? 4 : 8, DIAGONALS = Band<N>::diagonals;
@@ -203,8 +210,8 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
     const int part = blockIdx.x / a.heads, share = part % a.shares;
     const int64_t groups = (a.queries + N - 1) / N, vectors = (a.keys + N - 1) / N;
     const char* scores = a.scores + h * a.s_head * ElemBytes<ST>::value;
-    for (int64_t strip = part / a.shares; strip < a.strips; strip += a.strip_blocks) {
-        const int64_t t0 = a.band0 + strip * 64;
+    for (int64_t turn = part / a.shares; turn < a.strips; turn += a.strip_blocks) {
+        const int64_t t0 = a.band0 + strip_of(a, turn) * 64;
         // the row groups in which some lane has a column, of all sequences, in equal parts for all waves of the shares
         const int64_t g_from = max(int64_t(0), -(t0 + 63)), steps = max(min(groups, vectors - t0) - g_from, int64_t(0));
         const int64_t units = steps * a.batch, turns = static_cast<int64_t>(a.shares) * kWaves;
@@ -350,7 +357,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
 
 constexpr int64_t kMaxTiles = int64_t(1) << 20, kTiles = 2048;
 constexpr int kTileRows = 64;
-constexpr int64_t kGradBlocks = 2048, kGradSteps = 1, kStreamBytes = int64_t(1) << 28;
+constexpr int64_t kGradBlocks = 2048, kGradSteps = 4, kComputeUnits = 256, kStreamBytes = int64_t(1) << 28;
 constexpr int64_t kPartBytes = int64_t(1) << 24;     // of the workspace, if 64 parts do not take more
 
 template <int TT, int OT>
@@ -559,9 +566,12 @@ int32_t ddp_position_bias_grad(ddp_position_bias* h, int64_t batch, int64_t quer
         a.band0 = 1 - groups;
         a.strips = (last - a.band0 + 1 + 63) / 64;
         if (a.strips > 0) {
+            a.center = std::max<int64_t>(0, std::min(a.strips - 1, (((keys + n - 1) / n - groups) / 2 - a.band0) / 64));
             a.strip_blocks = static_cast<int32_t>(std::min<int64_t>(a.strips, h->parts));
             const int64_t blocks = static_cast<int64_t>(a.strip_blocks) * h->heads, steps = batch * std::min(groups, last - a.band0 + 1);
-            a.shares = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({kGradBlocks / blocks, h->parts / a.strip_blocks, steps / (kWaves * kGradSteps)})));
+            // kGradSteps row groups a wave, or fewer to have a block for each compute unit
+            const int64_t shares = std::max(steps / (kWaves * kGradSteps), std::min(steps / kWaves, kComputeUnits / blocks));
+            a.shares = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>({kGradBlocks / blocks, h->parts / a.strip_blocks, shares})));
             parts = static_cast<int64_t>(a.strip_blocks) * a.shares;
             const dim3 grid(static_cast<unsigned>(parts * h->heads));
             const size_t bytes = static_cast<size_t>(a.buckets) * 8;

@@ -191,7 +191,7 @@ __device__ __forceinline__ void clear_counts(const RouteArgs& a, int32_t* counts
     for (int e = threadIdx.x; e < a.experts; e += kThreads) counts[e] = 0;
     __syncthreads();
 }
-// A block alone writes the counts.  More blocks add theirs to copies, which count_kernel sums: 2048 blocks of 256 experts at
+// A block alone writes the counts.  More blocks add theirs to copies, which the next kernel sums: 2048 blocks of 256 experts at
 // one copy took 30 us longer.
 template <bool ALONE>
 __device__ __forceinline__ void add_counts(const RouteArgs& a, const int32_t* counts) {
@@ -204,6 +204,18 @@ __device__ __forceinline__ void add_counts(const RouteArgs& a, const int32_t* co
     int32_t* to = a.copies + blockIdx.x % kCopies * a.experts;
     for (int e = threadIdx.x; e < a.experts; e += kThreads)
         if (counts[e] != 0) atomicAdd(to + e, counts[e]);
+}
+// The sum of an expert's copies, and zeros in them for the next call.
+__device__ __forceinline__ int32_t take_copies(int32_t* copies, int experts, int e) {
+    int32_t x[kCopies], sum = 0;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) x[c] = copies[c * experts + e];
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+        sum += x[c];
+        if (x[c] != 0) copies[c * experts + e] = 0;
+    }
+    return sum;
 }
 
 // All tokens (where no team's lanes divide into the groups), or those that teams have left.
@@ -226,7 +238,15 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
                 if (n % kWaves == wave) route_token<LT>(a, t0 + __ffsll(static_cast<unsigned long long>(some)) - 1, mine, counts);
         }
     }
-    add_counts<ALL>(a, counts);
+    if constexpr (ALL) {
+        add_counts<true>(a, counts);
+    } else if (a.counts != nullptr) {                // the teams' kernel has cleared the counts, where they are not added to
+        __syncthreads();
+        for (int e = threadIdx.x; e < a.experts; e += kThreads) {
+            const int32_t n = counts[e] + (e % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x) ? take_copies(a.copies, a.experts, e) : 0);
+            if (n != 0) atomicAdd(a.counts + e, n);
+        }
+    }
 }
 
 // ---- a token by a team ----
@@ -325,6 +345,8 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
     uint32_t* sorted = reinterpret_cast<uint32_t*>(keys + wave * a.room) + lane;     // the lane's words, 64 apart
     clear_counts(a, counts);
     const int e0 = l * a.each, mine = max(min(a.experts - e0, a.each), 0);
+    if (!HERE && a.counts != nullptr && !a.accumulate && blockIdx.x == 0)
+        for (int e = threadIdx.x; e < a.experts; e += kThreads) a.counts[e] = 0;
     // biases, lifted, in LDS: the i-th of a team's lanes side by side (in registers they would cost a wave in six)
     float of_bias = 0.0f;
     for (int e = threadIdx.x; a.bias != nullptr && e < a.experts; e += kThreads) {
@@ -507,20 +529,9 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
     add_counts<HERE>(a, counts);
 }
 
-// The copies' sum, and zeros in them for the next call.  A thread an expert.
 __global__ __launch_bounds__(64) void count_kernel(int32_t* copies, int32_t* counts, int experts, int accumulate) {
     const int e = blockIdx.x * 64 + threadIdx.x;
-    if (e >= experts) return;
-    int32_t sum = accumulate ? counts[e] : 0;
-    int32_t x[kCopies];
-#pragma unroll
-    for (int c = 0; c < kCopies; ++c) x[c] = copies[c * experts + e];
-#pragma unroll
-    for (int c = 0; c < kCopies; ++c) {
-        sum += x[c];
-        if (x[c] != 0) copies[c * experts + e] = 0;
-    }
-    counts[e] = sum;
+    if (e < experts) counts[e] = take_copies(copies, experts, e) + (accumulate ? counts[e] : 0);
 }
 
 // A token's gradient by a team of lanes with EACH neighbouring experts each.  What the chosen experts get is put together in a row in LDS, which is zeros
@@ -684,7 +695,7 @@ bool launch_team(ddp_router* h, const RouteArgs& a, int64_t blocks, size_t bytes
     const int64_t looks = (a.tokens + 63) / 64;      // tokens that a block looks through at a time
     hipLaunchKernelGGL((route_kernel<LT, false>), dim3(static_cast<unsigned>(std::min(looks, kBlocks))), dim3(kThreads),
                        static_cast<size_t>(kWaves * 8 + 4) * a.experts, h->stream, a);
-    return true;
+    return false;
 }
 template <int LT>
 bool launch_route(ddp_router* h, RouteArgs a) {
@@ -696,6 +707,7 @@ bool launch_route(ddp_router* h, RouteArgs a) {
     const int teams = kThreads >> a.log2_lanes;
     const int64_t blocks = (a.tokens + teams - 1) / teams;
     const int each = a.each > 8 ? 16 : a.each > 4 ? 8 : a.each > 2 ? 4 : a.each;
+    if (blocks > kFewBlocks) a.room = 32 * each;     // (no token is done over there)
     const size_t bytes = static_cast<size_t>(kWaves) * a.room * 8 + static_cast<size_t>(teams) * a.listed * 12 + static_cast<size_t>(a.experts) * 4 +
                          (std::max(each << a.log2_lanes, kWaves)) * size_t(4);
     if (a.each > 8) return launch_team<LT, 16>(h, a, blocks, bytes);
