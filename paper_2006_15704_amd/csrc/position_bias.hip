@@ -82,6 +82,7 @@ struct BiasArgs {
 __device__ __forceinline__ int bucket_of(const int32_t* first, const BiasArgs& a, int64_t r) {
     const int64_t d = a.both ? (r < 0 ? -r : r) : (r < 0 ? -r : 0);
     int lo = 0, hi = a.sides;                        // first[lo] <= d < first[hi]
+    if (d >= first[hi - 1]) lo = hi - 1;             // (most diagonals of long scores)
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (first[mid] <= d) lo = mid;
@@ -109,6 +110,7 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
     constexpr int N = VectorOf<OT>::value;
     __shared__ __attribute__((aligned(16))) float of[kTileDiagonals];
     __shared__ int32_t first[kMaxBuckets];
+    __shared__ float value[kMaxBuckets];             // of the head's buckets
     for (int k = threadIdx.x; k < a.sides; k += kThreads) first[k] = a.first[k];
     const int x = threadIdx.x & (a.cols - 1), y = threadIdx.x >> a.log2_cols;
     const int high = (kThreads >> a.log2_cols) * a.rows, wide = a.cols * N;
@@ -119,11 +121,12 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
         // of[d]: of the diagonal that ends in the tile's first column d - high + 1 rows from its first row
         const int64_t r0 = c0 - i0 - (high - 1) - a.offset;
         __syncthreads();
+        for (int k = threadIdx.x; k < a.buckets; k += kThreads)
+            value[k] = load_one<TT>(a.table + (k * a.table_stride + h) * ElemBytes<TT>::value) * a.scale;
+        __syncthreads();
         for (int d = high - rows_here + threadIdx.x; d < high - 1 + cols_here; d += kThreads) {
             const int64_t r = r0 + d;
-            float v = load_one<TT>(a.table + (bucket_of(first, a, r) * a.table_stride + h) * ElemBytes<TT>::value) * a.scale;
-            if (!ADD && a.causal && r > 0) v = a.masked;
-            of[d] = v;
+            of[d] = !ADD && a.causal && r > 0 ? a.masked : value[bucket_of(first, a, r)];
         }
         __syncthreads();
         const int64_t c = c0 + x * N;
@@ -141,9 +144,10 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
             // causal: element e of row k is visible where e - k <= edge
             const int64_t behind = i_first + g + a.offset - c;
             const int edge = a.causal ? static_cast<int>(max(min(behind, int64_t(N)), int64_t(-N))) : N;
-            Parts<OT, N> there[N];                                   // all on the way together
+            Parts<OT, N> there[N] = {};                              // all on the way together
+            const bool some = seen > 0 && edge > -N;                 // (what is masked is not read)
             if constexpr (ADD) {
-                if (have == N) {
+                if (have == N && some) {
 #pragma unroll
                     for (int k = 0; k < N; ++k)
                         if (k < rows) there[k] = load_parts<OT, N>(out + static_cast<int64_t>(g + k) * a.s_query * ElemBytes<OT>::value);
@@ -156,14 +160,14 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
                 float v[N];
                 if constexpr (ADD) {
                     if (have == N) widen<OT, N>(there[k], v);
-                    else load_some<OT, N>(to, have, v);
+                    else load_some<OT, N>(to, some ? have : 0, v);
                 }
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     if constexpr (ADD) v[e] = e < seen && e - k <= edge ? window[e - k + N - 1] + v[e] : a.masked;
                     else v[e] = e < seen ? window[e - k + N - 1] : a.masked;
                 }
-                store_some<OT, N, !ADD>(to, have, v);
+                store_some<OT, N>(to, have, v);
             }
         }
     }
@@ -356,7 +360,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
 // ---- host ----
 
 constexpr int64_t kMaxTiles = int64_t(1) << 20, kTiles = 2048;
-constexpr int kTileRows = 64;
+constexpr int kTileRows = 16;
 constexpr int64_t kGradBlocks = 2048, kGradSteps = 4, kComputeUnits = 256, kStreamBytes = int64_t(1) << 28;
 constexpr int64_t kPartBytes = int64_t(1) << 24;     // of the workspace, if 64 parts do not take more
 
