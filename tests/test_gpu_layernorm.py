@@ -325,3 +325,48 @@ def test_on_another_stream_and_replayed():
                 assert torch.equal(t, w)
     torch.cuda.synchronize()
     d.ddp_layernorm_destroy(h)
+
+
+@pytest.mark.parametrize("xt,yt", [(FP32, FP32), (FP32, BF16), (BF16, BF16)])
+@pytest.mark.parametrize("rows,width", [(9000, 1024), (9001, 515), (40001, 64), (150001, 16), (2500, 2100), (3001, 4000), (600, 8100)])
+def test_forward_of_many_rows(xt, yt, rows, width):
+    """More rows than the launch has teams, results that go past the caches."""
+    check_forward(rows, width, xt, yt, residual=True)
+
+
+@pytest.mark.parametrize("xt,yt", [(FP32, FP32), (FP32, FP16), (BF16, BF16)])
+@pytest.mark.parametrize("rows,width", [(300, 16), (301, 24), (99, 32), (50, 48), (70, 300), (70, 512), (41, 1500), (41, 2048), (9, 4096), (5, 6000), (5, 16384),
+                                        (3, 16385)])
+def test_both_ways_of_every_team(xt, yt, rows, width):
+    check_forward(rows, width, xt, yt, residual=True, gaps=(1, 0, 3, 2))
+    check_backward(rows, width, xt, yt, dsum=True, gaps=(0, 3, 1, 2))
+
+
+@pytest.mark.parametrize("rows,width", [(5000, 1500), (70000, 24), (900, 10048)])
+def test_backward_of_more_rows_than_teams(rows, width):
+    check_backward(rows, width, BF16, BF16, dsum=True, add=True)
+    check_backward(rows, width, FP32, BF16, wanted="gb")
+
+
+def test_two_handles_at_once():
+    """Handles on two streams, their calls in turn: workspaces of their own."""
+    torch, d = lib()
+    rows, width = 4000, 1024
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    handles = [d.ddp_layernorm_create(0, s.cuda_stream, width) for s in streams]
+    gen = torch.Generator("cuda").manual_seed(3)
+    x, dy = (torch.randn((2, rows, width), generator=gen, device="cuda") for _ in range(2))
+    mean, rstd = x.mean(2), x.var(2, unbiased=False).rsqrt()
+    out = torch.zeros((8, 2, 2, width), device="cuda")
+    torch.cuda.synchronize()
+    for turn in range(8):
+        for k in range(2):
+            d.ddp_layernorm_backward(handles[k], rows, dy[k].data_ptr(), FP32, width, x[k].data_ptr(), FP32, width, mean[k].data_ptr(), rstd[k].data_ptr(), 0,
+                                     FP32, 0, 0, 0, 0, False, out[turn, k, 0].data_ptr(), out[turn, k, 1].data_ptr(), FP32)
+    torch.cuda.synchronize()
+    assert (out == out[0]).all()
+    for k in range(2):
+        want = (dy[k].double() * ((x[k].double() - mean[k].double()[:, None]) * rstd[k].double()[:, None])).sum(0)
+        assert (out[0, k, 0].double() - want).abs().max() < 1e-3
+    for h in handles:
+        d.ddp_layernorm_destroy(h)

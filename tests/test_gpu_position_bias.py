@@ -289,3 +289,54 @@ def test_on_another_stream_and_replayed():
             assert torch.equal(s, want[0]) and torch.equal(grad, want[1])
     torch.cuda.synchronize()
     d.ddp_position_bias_destroy(h)
+
+
+@pytest.mark.parametrize("batch,queries,keys,offset,causal", [(1, 5000, 5000, 0, True), (2, 3001, 2999, 0, False), (3, 300, 4100, 3800, True), (70, 64, 64, 0, True),
+                                                              (2, 4100, 17, -4083, True), (1, 20000, 600, 0, False)])
+@pytest.mark.parametrize("dt", [FP32, BF16])
+def test_grad_of_small_whole_numbers(batch, queries, keys, offset, causal, dt):
+    """Sums of whole numbers are exact at every size: all the ways that strips and row groups are dealt out count every place once."""
+    torch, d = lib()
+    H, kind = 2, (32, 8, 700, True)
+    gen = torch.Generator("cuda").manual_seed(queries)
+    ds = torch.randint(-1, 2, (batch, H, queries, keys), generator=gen, device="cuda").to(torch_type(dt))
+    lengths = torch.randint(0, queries + 1, (batch,), generator=gen, device="cuda", dtype=torch.int32)
+    grad = torch.full((32, H), GUARD, device="cuda")
+    h = d.ddp_position_bias_create(0, 0, H, *kind)
+    first = torch.from_numpy(d.ddp_position_bias_buckets(h)).cuda().long()
+    torch.cuda.synchronize()
+    d.ddp_position_bias_grad(h, batch, queries, keys, offset, ds.data_ptr(), dt, *ds.stride()[:3], 1.0, 0, lengths.data_ptr(), causal, False, grad.data_ptr(),
+                             FP32, H)
+    torch.cuda.synchronize()
+    i, j = torch.arange(queries, device="cuda")[:, None], torch.arange(keys, device="cuda")[None]
+    r = j - i - offset
+    bucket = torch.bucketize(r.abs(), first, right=True) - 1 + (r > 0) * 16
+    want = torch.zeros((32, H), device="cuda", dtype=torch.float64)
+    for b in range(batch):
+        seen = i < lengths[b]
+        if causal:
+            seen = seen & (r <= 0)
+        for n in range(H):
+            want[:, n] += torch.bincount(bucket[seen.expand_as(r)], weights=ds[b, n][seen.expand_as(r)].double(), minlength=32)
+    assert torch.equal(grad.double(), want)
+    d.ddp_position_bias_destroy(h)
+
+
+@pytest.mark.parametrize("queries,keys,gap,shift", [(1, 1, 0, 3), (9, 3, 0, 1), (40, 61, 0, 5), (7, 64, 0, 0), (64, 7, 1, 2)])
+@pytest.mark.parametrize("dt", [FP32, BF16])
+def test_grad_at_the_end_of_its_memory(queries, keys, gap, shift, dt):
+    """Scores that end with their allocation: nothing behind it is read (what would be is NaN here, and would show)."""
+    torch, d = lib()
+    B, H, kind = 2, 3, (8, 4, 32, False)
+    n = B * H * queries * (keys + gap) - gap
+    mem = torch.full((shift + n + 64,), float("nan"), dtype=torch_type(dt), device="cuda")
+    view = mem[shift:shift + n].as_strided((B, H, queries, keys), (H * queries * (keys + gap), queries * (keys + gap), keys + gap, 1))
+    view.copy_(torch.randint(-3, 4, (B, H, queries, keys), generator=torch.Generator("cuda").manual_seed(keys), device="cuda"))
+    grad = torch.zeros((8, H), device="cuda")
+    h = d.ddp_position_bias_create(0, 0, H, *kind)
+    torch.cuda.synchronize()
+    d.ddp_position_bias_grad(h, B, queries, keys, 0, view.data_ptr(), dt, *view.stride()[:3], 1.0, 0, 0, False, False, grad.data_ptr(), FP32, H)
+    torch.cuda.synchronize()
+    want, _ = ops.bias_grad(view.double().cpu().numpy(), ops.visible(B, queries, keys, 0), ops.bucket_places(queries, keys, 0, *kind), 8)
+    assert (grad.double().cpu().numpy() == want).all()
+    d.ddp_position_bias_destroy(h)

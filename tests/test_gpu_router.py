@@ -268,3 +268,68 @@ def test_on_another_stream_and_replayed():
                 assert torch.equal(t, w)
     torch.cuda.synchronize()
     d.ddp_router_destroy(h)
+
+
+BIG = [(256, 8, 8, 4, 2, SIGMOID, FP32, True), (256, 8, 1, 1, 1, SOFTMAX, BF16, False), (64, 2, 1, 1, 1, SOFTMAX, BF16, True), (60, 4, 1, 1, 1, SIGMOID, FP16, True),
+       (1000, 16, 1, 1, 1, SOFTMAX, FP32, True), (8, 3, 2, 1, 2, SIGMOID, BF16, False), (160, 6, 8, 3, 1, SOFTMAX, FP32, True), (130, 40, 1, 1, 1, SIGMOID, BF16, True),
+       (24, 2, 12, 6, 2, SIGMOID, FP32, True), (512, 4, 64, 8, 2, SOFTMAX, BF16, False)]
+
+
+@pytest.mark.parametrize("E,k,groups,kept,top,score,dt,biased", BIG)
+def test_many_tokens_as_few(E, k, groups, kept, top, score, dt, biased):
+    """Long calls leave the tokens whose keys come near each other to a second kernel: they choose what short calls do (which are
+    compared with the oracle above), and count the same, at every call."""
+    torch, d = lib()
+    T, some = 70000, 700
+    gen = torch.Generator("cuda").manual_seed(E)
+    x = (torch.randn((T, E), generator=gen, device="cuda") * 1.5).to(torch_type(dt))
+    x[::97, ::2] = x[::97, 1::2]                          # pairs of equal logits
+    x[5::101] = (x[5::101].float() * 1e-3).to(x.dtype)    # many that are nearly equal
+    x[7::103, : E // 2] = -float("inf")
+    bias = (torch.randint(-40, 41, (E,), generator=gen, device="cuda") * 1e-3) if biased else None
+    h = d.ddp_router_create(0, 0, E, k, groups, kept, top, score, True, 2.5)
+    big, small = ((torch.zeros((T, k), dtype=torch.int32, device="cuda"), torch.zeros((T, k), device="cuda"),
+                   torch.full((E,), 5, dtype=torch.int32, device="cuda")) for _ in range(2))
+    torch.cuda.synchronize()
+
+    def route(out, a, n, add):
+        d.ddp_router_route(h, n, x[a:a + n].data_ptr(), dt, E, bias.data_ptr() if biased else 0, out[0][a:].data_ptr(), out[1][a:].data_ptr(), FP32,
+                           out[2].data_ptr(), add)
+    for a in range(0, T, some):
+        route(small, a, some, a > 0)
+    for add in (False, False, True):
+        big[0].fill_(-2)
+        route(big, 0, T, add)
+    torch.cuda.synchronize()
+    assert torch.equal(big[0], small[0])
+    assert ((big[1] - small[1]).abs() <= 2 * (2 * 20 + E / 16 + 40) * U * small[1]).all()
+    load = torch.bincount(small[0][small[0] >= 0], minlength=E)
+    assert torch.equal(small[2].long(), load) and torch.equal(big[2].long(), 2 * load)
+    d.ddp_router_destroy(h)
+
+
+@pytest.mark.parametrize("experts,chosen", [(143, 14), (64, 2), (1024, 8), (20, 20), (6, 1)])
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+def test_grad_of_many_tokens_as_few(experts, chosen, score):
+    torch, d = lib()
+    T, some = 60000, 1500
+    gen = torch.Generator("cuda").manual_seed(experts)
+    x = torch.randn((T, experts), generator=gen, device="cuda").bfloat16()
+    at = torch.rand((T, experts), generator=gen, device="cuda").topk(chosen, dim=1).indices.int()
+    at[::7, -1] = -1
+    dw = torch.randn((T, chosen), generator=gen, device="cuda")
+    h = d.ddp_router_create(0, 0, experts, chosen, score=score)
+    big, small = (torch.full((T, experts), GUARD, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    torch.cuda.synchronize()
+
+    def grad(out, a, n):
+        d.ddp_router_grad(h, n, x[a:].data_ptr(), BF16, experts, at[a:].data_ptr(), dw[a:].data_ptr(), FP32, out[a:].data_ptr(), experts)
+    grad(big, 0, T)
+    for a in range(0, T, some):
+        grad(small, a, some)
+    torch.cuda.synchronize()
+    assert torch.equal(big, small)
+    grad(x, 0, T)                                         # over the logits
+    torch.cuda.synchronize()
+    assert torch.equal(big, x)
+    d.ddp_router_destroy(h)
