@@ -652,7 +652,8 @@ const char* ddp_layernorm_last_error(const ddp_layernorm* norm);
  * y = (s - mean) * rstd * gamma + beta, all in binary32 (the variance from the differences to the mean)
  * and rounded once to the types of what is written: sum (s, may be NULL), y, and mean and rstd (one
  * binary32 a row, may be NULL).  x, residual and sum are of x_dtype; y is of x_dtype too, or of any type
- * where x is binary32 (DDP_ERR_UNSUPPORTED otherwise); gamma and beta (NULL: 1 and 0) of param_dtype. */
+ * where x is binary32 (DDP_ERR_UNSUPPORTED otherwise); gamma and beta (NULL: 1 and 0) of param_dtype.  sum may be x or residual
+ * (address and stride). */
 int32_t ddp_layernorm_forward(ddp_layernorm* norm, int64_t rows, const void* x, int32_t x_dtype, int64_t x_stride, const void* residual,
                               int64_t residual_stride, const void* gamma, const void* beta, int32_t param_dtype, float eps, void* sum,
                               int64_t sum_stride, void* y, int32_t y_dtype, int64_t y_stride, float* mean, float* rstd);
@@ -661,7 +662,7 @@ int32_t ddp_layernorm_forward(ddp_layernorm* norm, int64_t rows, const void* x, 
  *   dx = (g - mean(g) - xh * mean(g * xh)) * rstd + dsum
  *   dgamma = sum over the rows of dy * xh      dbeta = sum over the rows of dy
  * dsum (x_dtype, NULL: 0) is what flows back along the sum by itself.  dx is the gradient of x and of the residual alike.
- * dx (x_dtype), dgamma and dbeta (grad_dtype) may be NULL each.  accumulate != 0: dgamma and dbeta are added to what they hold.
+ * dx (x_dtype; may be dsum, address and stride), dgamma and dbeta (grad_dtype) may be NULL each.  accumulate != 0: dgamma and dbeta are added to what they hold.
  * Types as in the forward pass, dy as y.  In binary32, in an order that depends on the sizes alone (repeated calls give the same
  * bits), rounded once. */
 int32_t ddp_layernorm_backward(ddp_layernorm* norm, int64_t rows, const void* dy, int32_t dy_dtype, int64_t dy_stride, const void* x,

@@ -510,9 +510,9 @@ int32_t ddp_position_bias_apply(ddp_position_bias* h, int64_t batch, int64_t que
     a.keys = keys;
     a.offset = offset;
     a.table_stride = table_stride;
-    a.s_batch = batch_stride;
-    a.s_head = head_stride;
-    a.s_query = query_stride;
+    a.s_batch = batch > 1 ? batch_stride : 0;        // (of one, the stride may be anything)
+    a.s_head = h->heads > 1 ? head_stride : 0;
+    a.s_query = queries > 1 ? query_stride : 0;
     a.heads = h->heads;
     a.buckets = h->buckets;
     a.sides = h->sides;
@@ -554,9 +554,9 @@ int32_t ddp_position_bias_grad(ddp_position_bias* h, int64_t batch, int64_t quer
         a.queries = queries;
         a.keys = keys;
         a.offset = offset;
-        a.s_batch = batch_stride;
-        a.s_head = head_stride;
-        a.s_query = query_stride;
+        a.s_batch = batch > 1 ? batch_stride : 0;    // (of one, the stride may be anything)
+        a.s_head = h->heads > 1 ? head_stride : 0;
+        a.s_query = queries > 1 ? query_stride : 0;
         a.heads = h->heads;
         a.buckets = h->buckets;
         a.sides = h->sides;

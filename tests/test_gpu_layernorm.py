@@ -370,3 +370,39 @@ def test_two_handles_at_once():
         assert (out[0, k, 0].double() - want).abs().max() < 1e-3
     for h in handles:
         d.ddp_layernorm_destroy(h)
+
+
+@pytest.mark.parametrize("width", [5, 24, 70, 515, 1024, 1500, 3001, 6000, 10001, 17000])
+@pytest.mark.parametrize("dt", [FP32, BF16])
+def test_in_place(width, dt):
+    """The sum over x or over the residual, dx over what flows along the sum: the same bits as apart."""
+    torch, d = lib()
+    rows = 50
+    gen = torch.Generator("cuda").manual_seed(width)
+    x, r, dy = (torch.randn((rows, width), generator=gen, device="cuda").to(torch_type(dt)) for _ in range(3))
+    gamma, beta = (torch.randn(width, generator=gen, device="cuda") for _ in range(2))
+    h = d.ddp_layernorm_create(0, 0, width)
+
+    def forward(x, r, total):
+        y, mean, rstd = torch.zeros_like(x), torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+        d.ddp_layernorm_forward(h, rows, x.data_ptr(), dt, width, r.data_ptr(), width, gamma.data_ptr(), beta.data_ptr(), FP32, EPS, total.data_ptr(), width,
+                                y.data_ptr(), dt, width, mean.data_ptr(), rstd.data_ptr())
+        return y, mean, rstd, total
+
+    def backward(along, dx):
+        dgamma, dbeta = torch.zeros(width, device="cuda"), torch.zeros(width, device="cuda")
+        d.ddp_layernorm_backward(h, rows, dy.data_ptr(), dt, width, x.data_ptr(), dt, width, mean.data_ptr(), rstd.data_ptr(), gamma.data_ptr(), FP32,
+                                 along.data_ptr(), width, dx.data_ptr(), width, False, dgamma.data_ptr(), dbeta.data_ptr(), FP32)
+        return dx, dgamma, dbeta
+    torch.cuda.synchronize()
+    apart = forward(x, r, torch.zeros_like(x))
+    _, mean, rstd, _ = apart
+    for which in (0, 1):
+        ins = [x.clone(), r.clone()]
+        for a, b in zip(forward(*ins, ins[which]), apart):
+            assert torch.equal(a, b)
+    want = backward(r, torch.zeros_like(x))
+    along = r.clone()
+    for a, b in zip(backward(along, along), want):
+        assert torch.equal(a, b)
+    d.ddp_layernorm_destroy(h)

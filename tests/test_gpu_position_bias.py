@@ -340,3 +340,22 @@ def test_grad_at_the_end_of_its_memory(queries, keys, gap, shift, dt):
     want, _ = ops.bias_grad(view.double().cpu().numpy(), ops.visible(B, queries, keys, 0), ops.bucket_places(queries, keys, 0, *kind), 8)
     assert (grad.double().cpu().numpy() == want).all()
     d.ddp_position_bias_destroy(h)
+
+
+def test_strides_of_single_entries_may_be_anything():
+    torch, d = lib()
+    K, kind = 37, (32, 16, 128, False)
+    h = d.ddp_position_bias_create(0, 0, 1, *kind)
+    table = torch.randn((32, 1), device="cuda")
+    out, grad = torch.zeros(K, device="cuda"), torch.zeros((32, 1), device="cuda")
+    far = 1 << 62
+    torch.cuda.synchronize()
+    d.ddp_position_bias_apply(h, 1, 1, K, K - 1, table.data_ptr(), FP32, 1, 1.0, 0, True, 0.0, False, out.data_ptr(), FP32, far, -far, far + 1)
+    out_of = out.cpu()
+    d.ddp_position_bias_grad(h, 1, 1, K, K - 1, out.data_ptr(), FP32, far, far, far, 1.0, 0, 0, True, False, grad.data_ptr(), FP32, 1)
+    torch.cuda.synchronize()
+    places = ops.bucket_places(1, K, K - 1, *kind)[0]
+    assert torch.equal(out_of, table[:, 0].cpu()[places])
+    want = np.bincount(places, weights=out_of.double().numpy(), minlength=32)
+    assert np.allclose(grad[:, 0].double().cpu().numpy(), want, rtol=1e-6, atol=1e-6)
+    d.ddp_position_bias_destroy(h)
