@@ -534,43 +534,52 @@ __global__ __launch_bounds__(64) void count_kernel(int32_t* copies, int32_t* cou
     if (e < experts) counts[e] = take_copies(copies, experts, e) + (accumulate ? counts[e] : 0);
 }
 
-// A token's gradient by a team of lanes with EACH neighbouring experts each.  What the chosen experts get is put together in a row in LDS, which is zeros
+// A token's gradient by a team of lanes with EACH experts each, in vectors of 16 bytes side by side.  What the chosen experts get is put together in a row in LDS, which is zeros
 // otherwise, and everyone reads what is theirs; of sigmoids nothing else is computed.
 template <int LT, int EACH>
 __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
     extern __shared__ float lds[];                   // [teams]: the row, then of the chosen: gradient, score, expert
     const int lanes = 1 << a.log2_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> a.log2_lanes, teams = kThreads >> a.log2_lanes;
-    constexpr int STEP = EACH + 4;                   // (lanes four words further apart: fewer of them share a bank)
-    float* row = lds + team * (lanes * STEP + 3 * a.chosen);
-    float* of = row + lanes * STEP;
+    constexpr int N = EACH * ElemBytes<LT>::value >= 16 ? 16 / ElemBytes<LT>::value : EACH, V = EACH / N;
+    float* row = lds + team * (lanes * EACH + 3 * a.chosen);
+    float* of = row + lanes * EACH;
     float* score = of + a.chosen;
     int32_t* at = reinterpret_cast<int32_t*>(score + a.chosen);
-    auto place = [](int e) { return e / EACH * STEP + e % EACH; };
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) row[l * STEP + i] = 0.0f;
-    const int e0 = l * EACH, mine = max(min(a.experts - e0, EACH), 0);
+    for (int i = 0; i < EACH; ++i) row[l * EACH + i] = 0.0f;
+    auto first = [&](int v) { return (v * lanes + l) * N; };             // of a vector's experts
+    auto have = [&](int v) { return max(min(a.experts - first(v), N), 0); };
     const int of_team0 = static_cast<int>(threadIdx.x & 63) & ~(lanes - 1);
     const uint64_t of_team = lanes == 64 ? ~uint64_t(0) : (uint64_t(1) << lanes) - 1;
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * teams; base < a.tokens; base += static_cast<int64_t>(gridDim.x) * teams) {
         const int64_t t = base + team;
         const bool live = t < a.tokens;
         const char* from = a.logits + t * a.stride * ElemBytes<LT>::value;
-        float s[EACH], largest = 0.0f, part = 0.0f;
+        float s[V][N], largest = 0.0f, part = 0.0f;
         if (a.score == DDP_SCORE_SOFTMAX) {
-            load_some<LT, EACH>(from + e0 * ElemBytes<LT>::value, live ? mine : 0, s);
+#pragma unroll
+            for (int v = 0; v < V; ++v) load_some<LT, N>(from + first(v) * ElemBytes<LT>::value, live ? have(v) : 0, s[v]);
             largest = kMasked;
 #pragma unroll
-            for (int i = 0; i < EACH; ++i)
-                if (i < mine) largest = fmaxf(largest, s[i]);
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    if (i >= have(v)) s[v][i] = kMasked;
+                    largest = fmaxf(largest, s[v][i]);
+                }
             largest = team_max(a.log2_lanes, largest);
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                s[i] = i >= mine || s[i] == kMasked ? 0.0f : expf(s[i] - largest);
-                part += s[i];
-            }
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    s[v][i] = s[v][i] == kMasked ? 0.0f : expf(s[v][i] - largest);
+                    part += s[v][i];
+                }
             part = 1.0f / team_sum(a.log2_lanes, part);
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) s[i] *= part;
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[v][i] *= part;
         }
         // the chosen go round the lanes
         bool any = false;
@@ -614,19 +623,22 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
                 const float x = load_one<LT>(from + e * ElemBytes<LT>::value);
                 sum *= score[n] * (1.0f / (1.0f + expf(x)));     // 1 - s, without the difference
             }
-            row[place(e)] = sum;
+            row[e] = sum;
         }
         wave_meets();
-        float d[EACH];
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            d[i] = row[l * STEP + i];
-            if (a.score == DDP_SCORE_SOFTMAX) d[i] = any ? s[i] * (d[i] - dot) : 0.0f;
+        for (int v = 0; v < V; ++v) {
+            float d[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                d[i] = row[first(v) + i];
+                if (a.score == DDP_SCORE_SOFTMAX) d[i] = any ? s[v][i] * (d[i] - dot) : 0.0f;
+            }
+            if (live && have(v) > 0) store_some<LT, N>(a.dlogits + (t * a.dstride + first(v)) * ElemBytes<LT>::value, have(v), d);
         }
-        if (live && mine > 0) store_some<LT, EACH>(a.dlogits + (t * a.dstride + e0) * ElemBytes<LT>::value, mine, d);
         wave_meets();
         for (int n = l; n < a.chosen; n += lanes)
-            if (at[n] >= 0) row[place(at[n])] = 0.0f;
+            if (at[n] >= 0) row[at[n]] = 0.0f;
     }
 }
 
@@ -722,7 +734,7 @@ hipError_t launch_grad(ddp_router* h, RouteGradArgs a) {
     while (each << a.log2_lanes < a.experts) ++a.log2_lanes;
     const int teams = kThreads >> a.log2_lanes;
     const dim3 blocks(static_cast<unsigned>(std::min<int64_t>((a.tokens + teams - 1) / teams, kBlocks))), threads(kThreads);
-    const size_t bytes = static_cast<size_t>(teams) * (((each + 4) << a.log2_lanes) + 3 * a.chosen) * 4;
+    const size_t bytes = static_cast<size_t>(teams) * ((each << a.log2_lanes) + 3 * a.chosen) * 4;
     if (each == 16) hipLaunchKernelGGL((route_grad_kernel<LT, 16>), blocks, threads, bytes, h->stream, a);
     else hipLaunchKernelGGL((route_grad_kernel<LT, 4>), blocks, threads, bytes, h->stream, a);
     return hipGetLastError();
