@@ -38,7 +38,7 @@ struct RouteGradArgs {
     const int32_t* experts_in;
     char* dlogits;
     int64_t tokens, stride, dstride;
-    int32_t experts, chosen, score, renormalise, dweights_type, log2_lanes;
+    int32_t experts, chosen, score, renormalise, dweights_type, log2_lanes, stream;
     float scale;
 };
 
@@ -634,7 +634,10 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
                 d[i] = row[first(v) + i];
                 if (a.score == DDP_SCORE_SOFTMAX) d[i] = any ? s[v][i] * (d[i] - dot) : 0.0f;
             }
-            if (live && have(v) > 0) store_some<LT, N>(a.dlogits + (t * a.dstride + first(v)) * ElemBytes<LT>::value, have(v), d);
+            char* to = a.dlogits + (t * a.dstride + first(v)) * ElemBytes<LT>::value;
+            if (!live || have(v) == 0) continue;
+            if (a.stream) store_some<LT, N, true>(to, have(v), d);
+            else store_some<LT, N>(to, have(v), d);
         }
         wave_meets();
         for (int n = l; n < a.chosen; n += lanes)
@@ -658,6 +661,7 @@ __global__ __launch_bounds__(kMaxExperts) void balance_kernel(const int32_t* cou
 
 // ---- host ----
 
+constexpr int64_t kStreamBytes = int64_t(4) << 20;
 constexpr int64_t kBlocks = 2048, kFewLanes = 65536, kFewBlocks = 512;
 
 // The team of a token: a.each experts a lane, up to `most`, so that groups have a power of two of lanes.  False: none.
@@ -878,6 +882,7 @@ int32_t ddp_router_grad(ddp_router* h, int64_t tokens, const void* logits, int32
     a.score = h->score;
     a.renormalise = h->renormalise;
     a.dweights_type = dweights_dtype;
+    a.stream = tokens * h->experts * elem_bytes(dtype) >= kStreamBytes;
     a.scale = h->scale;
     LAYER_HIP(h, dtype == DDP_FP32 ? launch_grad<DDP_FP32>(h, a) : dtype == DDP_FP16 ? launch_grad<DDP_FP16>(h, a) : launch_grad<DDP_BF16>(h, a));
     return DDP_OK;
