@@ -546,7 +546,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
 
 constexpr int kRowBlocks = 1 << 16;
 
-constexpr int kForwardThreads = 256, kForwardBlocks = 2048, kBackwardThreads = 512, kForwardEach = 16, kBackwardEach = 8;
+constexpr int kForwardThreads = 256, kForwardBlocks = 1 << 20, kForwardWideBlocks = 1536, kBackwardThreads = 512, kForwardEach = 16, kBackwardEach = 8;
 
 // The team of a width, as a type; false: rows are too short for a vector, or too long for a team.
 template <int XT, int YT, int THREADS, int EACH, typename F>
@@ -570,7 +570,7 @@ template <int XT, int YT>
 hipError_t launch_forward(ddp_layernorm* h, const ForwardArgs& a) {
     const bool team = with_team<XT, YT, kForwardThreads, kForwardEach>(a.width, [&](auto t) {
         typedef decltype(t) T;
-        const int64_t blocks = std::min<int64_t>((a.rows + T::TEAMS - 1) / T::TEAMS, kForwardBlocks);
+        const int64_t blocks = std::min<int64_t>((a.rows + T::TEAMS - 1) / T::TEAMS, T::WAVES < 8 ? kForwardBlocks : kForwardWideBlocks);
         hipLaunchKernelGGL((forward_team_kernel<XT, YT, T>), dim3(static_cast<unsigned>(blocks)), dim3(T::THREADS), 0, h->stream, a);
     });
     if (!team)

@@ -551,9 +551,24 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
     auto have = [&](int v) { return max(min(a.experts - first(v), N), 0); };
     const int of_team0 = static_cast<int>(threadIdx.x & 63) & ~(lanes - 1);
     const uint64_t of_team = lanes == 64 ? ~uint64_t(0) : (uint64_t(1) << lanes) - 1;
+    // a lane's first choice of the next token is on the way while this one's logit is
+    int next_expert = -1;
+    float next_weight = 0.0f;
+    auto fetch = [&](int64_t t) {
+        const bool some = t < a.tokens && l < a.chosen;
+        const int64_t from = some ? t * a.chosen + l : 0;
+        next_expert = a.experts_in[from];
+        next_weight = load_weight(a.dweights, a.dweights_type, from);
+        if (!some) next_expert = -1;
+    };
+    fetch(static_cast<int64_t>(blockIdx.x) * teams + team);
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * teams; base < a.tokens; base += static_cast<int64_t>(gridDim.x) * teams) {
         const int64_t t = base + team;
         const bool live = t < a.tokens;
+        const int expert = next_expert;
+        const float weight = next_weight;
+        float logit = 0.0f;
+        fetch(t + static_cast<int64_t>(gridDim.x) * teams);
         const char* from = a.logits + t * a.stride * ElemBytes<LT>::value;
         float s[V][N], largest = 0.0f, part = 0.0f;
         if (a.score == DDP_SCORE_SOFTMAX) {
@@ -585,13 +600,14 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
         bool any = false;
         float all = 0.0f, dot = 0.0f;
         for (int n = l; n < a.chosen; n += lanes) {
-            const int e = live ? a.experts_in[t * a.chosen + n] : -1;
+            const int e = n == l ? expert : live ? a.experts_in[t * a.chosen + n] : -1;
             const bool named = e >= 0 && e < a.experts;
             float w = 0.0f, g = 0.0f;
             if (named) {
                 const float x = load_one<LT>(from + e * ElemBytes<LT>::value);
+                if (n == l) logit = x;
                 w = a.score == DDP_SCORE_SIGMOID ? 1.0f / (1.0f + expf(-x)) : x == kMasked ? 0.0f : expf(x - largest) * part;
-                g = load_weight(a.dweights, a.dweights_type, t * a.chosen + n) * a.scale;
+                g = (n == l ? weight : load_weight(a.dweights, a.dweights_type, t * a.chosen + n)) * a.scale;
             }
             any |= named;
             all += w;
@@ -618,9 +634,12 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
             const int e = at[n];
             if (e < 0) continue;
             float sum = 0.0f;                        // (an expert that is named twice)
-            for (int m = 0; m < a.chosen; ++m) sum += at[m] == e ? of[m] : 0.0f;
+            for (int m = 0; m < a.chosen; ++m) {
+                const float one = of[m];             // (no condition on the read: it would be waited for)
+                sum += at[m] == e ? one : 0.0f;
+            }
             if (a.score == DDP_SCORE_SIGMOID) {
-                const float x = load_one<LT>(from + e * ElemBytes<LT>::value);
+                const float x = n == l ? logit : load_one<LT>(from + e * ElemBytes<LT>::value);
                 sum *= score[n] * (1.0f / (1.0f + expf(x)));     // 1 - s, without the difference
             }
             row[e] = sum;
@@ -662,7 +681,7 @@ __global__ __launch_bounds__(kMaxExperts) void balance_kernel(const int32_t* cou
 // ---- host ----
 
 constexpr int64_t kStreamBytes = int64_t(4) << 20;
-constexpr int64_t kBlocks = 2048, kFewLanes = 65536, kFewBlocks = 512;
+constexpr int64_t kBlocks = 1536, kFewLanes = 65536, kFewBlocks = 512;
 
 // The team of a token: a.each experts a lane, up to `most`, so that groups have a power of two of lanes.  False: none.
 bool team_of(RouteArgs& a, int most) {
