@@ -361,7 +361,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
 
 constexpr int64_t kMaxTiles = int64_t(1) << 20, kTiles = 2048;
 constexpr int kTileRows = 16;
-constexpr int64_t kGradBlocks = 2048, kGradSteps = 4, kComputeUnits = 256, kStreamBytes = int64_t(1) << 28;
+constexpr int64_t kGradBlocks = 1792, kGradSteps = 4, kComputeUnits = 256, kStreamBytes = int64_t(1) << 28;
 constexpr int64_t kPartBytes = int64_t(1) << 24;     // of the workspace, if 64 parts do not take more
 
 template <int TT, int OT>
