@@ -689,8 +689,8 @@ int32_t ddp_position_bias_buckets(const ddp_position_bias* bias, int32_t* first)
 /* out[b, h, i, j] = scale * table[bucket(j - i - offset)][h] (+ out[b, h, i, j] with accumulate != 0) for every batch entry, head,
  * query and key; `masked` (rounded to the type of out; what is there is not used) where the key is not visible: j >= key_lengths[b] (device, NULL: all
  * visible; counts below 0 are 0), or with causal != 0 a key behind the query, j > i + offset.  offset: position of query 0 counted from
- * key 0 (the number of cached keys, where queries follow them).  table: [buckets][heads] with a stride.  out: any three strides with which no two
- * places coincide; keys are adjacent.  In binary32, rounded once. */
+ * key 0 (the number of cached keys, where queries follow them).  table: [buckets][heads] with a stride.  out: the three strides in
+ * any order, each at least what the smaller ones span; keys are adjacent.  In binary32, rounded once. */
 int32_t ddp_position_bias_apply(ddp_position_bias* bias, int64_t batch, int64_t queries, int64_t keys, int64_t offset, const void* table,
                                 int32_t table_dtype, int64_t table_stride, float scale, const int32_t* key_lengths, int32_t causal,
                                 float masked, int32_t accumulate, void* out, int32_t out_dtype, int64_t batch_stride, int64_t head_stride,
@@ -728,7 +728,7 @@ int32_t ddp_router_route(ddp_router* router, int64_t tokens, const void* logits,
                          int32_t* experts_out, void* weights, int32_t weights_dtype, int32_t* counts, int32_t accumulate);
 
 /* dlogits (of dtype) from the gradient of the weights, for the choice that experts_in holds (indices outside [0, experts) take no part;
- * a token without any gets zeros).  The bias has no gradient.  dlogits may be logits (address and stride). */
+ * a token without any gets zeros).  A renormalised softmax is one over the chosen logits: the others get zeros, and are not read.  The bias has no gradient.  dlogits may be logits (address and stride). */
 int32_t ddp_router_grad(ddp_router* router, int64_t tokens, const void* logits, int32_t dtype, int64_t stride, const int32_t* experts_in,
                         const void* dweights, int32_t dweights_dtype, void* dlogits, int64_t dlogits_stride);
 

@@ -263,6 +263,9 @@ constexpr int kEach = 16, kSpare = 2;
 constexpr float kApart = 0x1p-16f;
 // The same of whole keys: 30 of the largest score and 3 of score and bias each of a softmax, 5 of a sigmoid.
 constexpr float kNearSoftmax = 0x1p-18f, kNearKey = 0x1p-20f;
+// Chosen scores whose sum is below this (biases have chosen them, or every logit of a sigmoid is far below 0) are near binary32's end, their
+// quotients not: a wave takes the weights in binary64.
+constexpr float kTiny = 0x1p-100f;
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t lane_moved(uint32_t x) {
@@ -330,9 +333,9 @@ __device__ __forceinline__ void sort_words(uint32_t (&w)[N]) {
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // EACH: the lane's experts, a.each of them used.  LANES: the logarithm of a team's lanes, if it is known (the steps of a meeting need no branches then:
-// 65536 tokens of 256 experts 47 us without).
+// 65536 tokens of 256 experts 47 us without).  Four lanes and 64 are held to the 80 registers of six waves, which the compiler exceeds by one.
 template <int LT, int EACH, bool HERE, int LANES>
-__global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
+__global__ __launch_bounds__(kThreads, LANES == 2 || LANES == 6 ? 6 : 1) void route_team_kernel(RouteArgs a) {
     extern __shared__ double keys[];                 // [kWaves][room], then candidates and counts
     const int log2_lanes = LANES >= 0 ? LANES : a.log2_lanes, lanes = 1 << log2_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> log2_lanes, teams = kThreads >> log2_lanes;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -427,7 +430,7 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
             }
             const float worst = -team_max(log2_lanes, before < a.kept && group < a.groups ? -rank : kMasked);
             const float next = team_max(log2_lanes, before >= a.kept && group < a.groups ? rank : kMasked);
-            again = next > kMasked && !(worst - next > 2.0f * apart);
+            again = (next > kMasked && !(worst - next > 2.0f * apart)) || !(lift < __builtin_huge_valf());
             if (before >= a.kept) {
 #pragma unroll
                 for (int i = 0; i < EACH; ++i) w[i] = 0;
@@ -457,7 +460,7 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
             const uint32_t here = word[n], behind = n + 1 < a.listed ? word[n + 1] : 0u;
             if (here != 0 && (behind != 0 || n + 1 >= a.listed)) {
                 const float k = key_of(here, lift), b = n + 1 < a.listed ? key_of(behind, lift) : left;
-                near |= b > kMasked && !(k - b > apart);
+                near |= b != kMasked && !(k - b > apart);       // (a lift beyond binary32 makes NaN of them)
             }
         }
         const uint64_t of_team = lanes == 64 ? ~uint64_t(0) : (uint64_t(1) << lanes) - 1;
@@ -484,7 +487,7 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
                     // equal for certain where logit and bias are
                     if (!(fabsf(other - key) > same)) again |= logit(o) != logit(e) || bias_of(o) != bias_of(e);
                 }
-                if (rank < a.chosen) again |= left > kMasked && !(key - left > apart);
+                if (rank < a.chosen) again |= left != kMasked && !(key - left > apart);
                 place[n] = rank;
             }
             again = (__ballot(again) >> of_team0 & of_team) != 0;
@@ -494,9 +497,7 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
             for (int n = l; n < a.listed; n += lanes) {
                 const int e = at[n], rank = ordered && e >= 0 ? place[n] : n;
                 float v = 0.0f;
-                if (rank < a.chosen && e >= 0) {
-                    v = score(logit(e));
-                }
+                if (rank < a.chosen && e >= 0) v = score(logit(e));
                 all += v;
                 word[n] = as_bits(v);
                 at[n] = rank < a.chosen ? (e < 0 ? -1 : e | rank << 16) : -2;
@@ -506,9 +507,13 @@ __global__ __launch_bounds__(kThreads) void route_team_kernel(RouteArgs a) {
                 }
             }
             all = team_sum(log2_lanes, all);
+            if (all < kTiny) {
+                wave_meets();
+                again = at[0] != -1;                 // some are chosen
+            }
             const float factor = !a.renormalise ? a.scale : all > 0.0f ? a.scale / all : 0.0f;
             for (int n = l; n < a.listed; n += lanes) {
-                if (at[n] < 0) continue;
+                if (again || at[n] < 0) continue;
                 const int e = at[n] & 0xFFFF, rank = at[n] >> 16;
                 a.experts_out[t * a.chosen + rank] = e;
                 store_weight(a.weights, a.weights_type, t * a.chosen + rank, as_float(word[n]) * factor);
@@ -534,9 +539,14 @@ __global__ __launch_bounds__(64) void count_kernel(int32_t* copies, int32_t* cou
     if (e < experts) counts[e] = take_copies(copies, experts, e) + (accumulate ? counts[e] : 0);
 }
 
+// Below this a sigmoid is 0 in binary64 too, and the weights are.
+constexpr float kNoScore = -745.0f;
+
 // A token's gradient by a team of lanes with EACH experts each, in vectors of 16 bytes side by side.  What the chosen experts get is put together in a row in LDS, which is zeros
-// otherwise, and everyone reads what is theirs; of sigmoids nothing else is computed.
-template <int LT, int EACH>
+// otherwise, and everyone reads what is theirs.  Only a softmax that is not renormalised reads the other logits: renormalised, it is that of the
+// chosen ones, and 64 bits or 32 leave nothing to the rest.  Renormalised scores are taken with a common factor exp(-shift) that makes the largest
+// 1 (a sigmoid's at least 1/2), so that small ones do not leave the range of binary32 before they are divided.
+template <int LT, int EACH, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
     extern __shared__ float lds[];                   // [teams]: the row, then of the chosen: gradient, score, expert
     const int lanes = 1 << a.log2_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> a.log2_lanes, teams = kThreads >> a.log2_lanes;
@@ -551,6 +561,7 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
     auto have = [&](int v) { return max(min(a.experts - first(v), N), 0); };
     const int of_team0 = static_cast<int>(threadIdx.x & 63) & ~(lanes - 1);
     const uint64_t of_team = lanes == 64 ? ~uint64_t(0) : (uint64_t(1) << lanes) - 1;
+    const bool sigmoid = !WHOLE && a.score == DDP_SCORE_SIGMOID, renormalise = !WHOLE && a.renormalise;
     // a lane's first choice of the next token is on the way while this one's logit is
     int next_expert = -1;
     float next_weight = 0.0f;
@@ -571,7 +582,7 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
         fetch(t + static_cast<int64_t>(gridDim.x) * teams);
         const char* from = a.logits + t * a.stride * ElemBytes<LT>::value;
         float s[V][N], largest = 0.0f, part = 0.0f;
-        if (a.score == DDP_SCORE_SOFTMAX) {
+        if constexpr (WHOLE) {
 #pragma unroll
             for (int v = 0; v < V; ++v) load_some<LT, N>(from + first(v) * ElemBytes<LT>::value, live ? have(v) : 0, s[v]);
             largest = kMasked;
@@ -598,37 +609,47 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
         }
         // the chosen go round the lanes
         bool any = false;
-        float all = 0.0f, dot = 0.0f;
+        float most = kMasked, all = 0.0f, dot = 0.0f;
         for (int n = l; n < a.chosen; n += lanes) {
             const int e = n == l ? expert : live ? a.experts_in[t * a.chosen + n] : -1;
             const bool named = e >= 0 && e < a.experts;
-            float w = 0.0f, g = 0.0f;
+            float x = kMasked, g = 0.0f;
             if (named) {
-                const float x = load_one<LT>(from + e * ElemBytes<LT>::value);
+                x = load_one<LT>(from + e * ElemBytes<LT>::value);
                 if (n == l) logit = x;
-                w = a.score == DDP_SCORE_SIGMOID ? 1.0f / (1.0f + expf(-x)) : x == kMasked ? 0.0f : expf(x - largest) * part;
                 g = (n == l ? weight : load_weight(a.dweights, a.dweights_type, t * a.chosen + n)) * a.scale;
             }
             any |= named;
-            all += w;
-            dot += g * w;
+            most = fmaxf(most, x);
             at[n] = named ? e : -1;
             of[n] = g;
+            score[n] = x;
+        }
+        float shift = WHOLE ? largest : 0.0f, factor = WHOLE ? part : 1.0f;
+        if (renormalise) {
+            most = team_max(a.log2_lanes, most);
+            shift = sigmoid ? fminf(most, 0.0f) : most;
+            if (sigmoid && most < kNoScore) factor = 0.0f;
+        }
+        for (int n = l; n < a.chosen; n += lanes) {
+            const float x = score[n];
+            float w = 0.0f;
+            if (x != kMasked) w = sigmoid && x > 0.0f ? 1.0f / (1.0f + expf(-x)) : expf(x - shift) * (sigmoid ? factor / (1.0f + expf(x)) : factor);
+            all += w;
+            dot += of[n] * w;
             score[n] = w;
         }
-        any = (__ballot(any) >> of_team0 & of_team) != 0;
-        if (a.renormalise) {
+        if (renormalise) {
             all = team_sum(a.log2_lanes, all);
             dot = team_sum(a.log2_lanes, dot);
             const float mean = dot / all;
-            dot = 0.0f;
-            for (int n = l; n < a.chosen; n += lanes) {
-                const float g = at[n] >= 0 && all > 0.0f ? (of[n] - mean) / all : 0.0f;
-                of[n] = g;
-                dot += g * score[n];
-            }
+            for (int n = l; n < a.chosen; n += lanes) of[n] = score[n] != 0.0f ? (of[n] - mean) * (score[n] / all) : 0.0f;
+        } else if (sigmoid) {
+            for (int n = l; n < a.chosen; n += lanes) of[n] *= score[n];
+        } else {
+            any = (__ballot(any) >> of_team0 & of_team) != 0;
+            dot = team_sum(a.log2_lanes, dot);
         }
-        dot = a.score == DDP_SCORE_SOFTMAX ? team_sum(a.log2_lanes, dot) : 0.0f;
         wave_meets();
         for (int n = l; n < a.chosen; n += lanes) {
             const int e = at[n];
@@ -638,9 +659,9 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
                 const float one = of[m];             // (no condition on the read: it would be waited for)
                 sum += at[m] == e ? one : 0.0f;
             }
-            if (a.score == DDP_SCORE_SIGMOID) {
+            if (sigmoid) {
                 const float x = n == l ? logit : load_one<LT>(from + e * ElemBytes<LT>::value);
-                sum *= score[n] * (1.0f / (1.0f + expf(x)));     // 1 - s, without the difference
+                sum *= 1.0f / (1.0f + expf(x));                  // 1 - s, without the difference
             }
             row[e] = sum;
         }
@@ -651,7 +672,7 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 d[i] = row[first(v) + i];
-                if (a.score == DDP_SCORE_SOFTMAX) d[i] = any ? s[v][i] * (d[i] - dot) : 0.0f;
+                if (WHOLE) d[i] = any ? s[v][i] * (d[i] - dot) : 0.0f;
             }
             char* to = a.dlogits + (t * a.dstride + first(v)) * ElemBytes<LT>::value;
             if (!live || have(v) == 0) continue;
@@ -758,8 +779,13 @@ hipError_t launch_grad(ddp_router* h, RouteGradArgs a) {
     const int teams = kThreads >> a.log2_lanes;
     const dim3 blocks(static_cast<unsigned>(std::min<int64_t>((a.tokens + teams - 1) / teams, kBlocks))), threads(kThreads);
     const size_t bytes = static_cast<size_t>(teams) * ((each << a.log2_lanes) + 3 * a.chosen) * 4;
-    if (each == 16) hipLaunchKernelGGL((route_grad_kernel<LT, 16>), blocks, threads, bytes, h->stream, a);
-    else hipLaunchKernelGGL((route_grad_kernel<LT, 4>), blocks, threads, bytes, h->stream, a);
+    auto launch = [&](auto each, auto whole) { hipLaunchKernelGGL((route_grad_kernel<LT, each.value, whole.value>), blocks, threads, bytes, h->stream, a); };
+    auto sized = [&](auto whole) {
+        if (each == 16) launch(std::integral_constant<int, 16>(), whole);
+        else launch(std::integral_constant<int, 4>(), whole);
+    };
+    if (a.score == DDP_SCORE_SOFTMAX && !a.renormalise) sized(std::true_type());
+    else sized(std::false_type());
     return hipGetLastError();
 }
 

@@ -23,11 +23,12 @@ def spread(x):
 
 
 def check_route(tokens, kind, score, renormalise, dt=FP32, wt=FP32, scale=2.5, bias=True, gap=0, shift=0, add=False, seed=0, logits=None, stats=True,
-                handle=None):
+                handle=None, times=1):
     torch, d = lib()
     E, k, groups, kept, top = kind
     rng = np.random.default_rng(seed + E)
-    x = Rows(rng.standard_normal((tokens, E)) * 1.5 if logits is None else logits, dt, gap, shift)
+    x = Rows(np.tile(rng.standard_normal((tokens, E)) * 1.5 if logits is None else logits, (times, 1)), dt, gap, shift)
+    few, tokens = tokens, tokens * times
     b = (rng.integers(-40, 41, E) * np.float32(1e-3)).astype(np.float32) if bias is True else bias
     b_on = torch.from_numpy(b).cuda() if b is not None and bias is not False else None
     experts = torch.full((tokens + 1, k), 99, dtype=torch.int32, device="cuda")
@@ -38,7 +39,8 @@ def check_route(tokens, kind, score, renormalise, dt=FP32, wt=FP32, scale=2.5, b
     d.ddp_router_route(h, tokens, x.ptr, dt, x.stride, b_on.data_ptr() if b_on is not None else 0, experts.data_ptr(), weights.data_ptr(), wt,
                        counts.data_ptr() if stats else 0, add)
     torch.cuda.synchronize()
-    want, w = ops.route(x.held, b if b_on is not None else np.zeros(E), k, groups, kept, top, score, renormalise, scale)
+    want, w = ops.route(x.held[:few], b if b_on is not None else np.zeros(E), k, groups, kept, top, score, renormalise, scale)
+    want, w = np.tile(want, (times, 1)), np.tile(w, (times, 1))
     got = experts[:-1].cpu().numpy()
     assert (got == want).all(), (np.argwhere(got != want)[:3].tolist(), got[(got != want).any(1)][:2], want[(got != want).any(1)][:2])
     R = (2 * spread(x.held) + E / 16 + 40)[:, None]
@@ -121,6 +123,39 @@ def test_route_wide_range():
     check_route(50, (96, 8, 1, 1, 1), SIGMOID, True, logits=logits, bias=False)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("times", [1, 1000])
+def test_route_biases_at_the_end_of_binary32(kind, score, times):
+    """As masks (the lowest value), and as what is chosen first."""
+    E, most = kind[0], np.finfo(np.float32).max
+    rng = np.random.default_rng(E)
+    logits = rng.standard_normal((40, E))
+    for values in ([0.0, -most], [0.0, 0.25, most, -most], [most * 0.75, -most * 0.75, -np.inf]):
+        bias = rng.choice(np.array(values, dtype=np.float32), E)
+        check_route(40, kind, score, True, logits=logits, bias=bias, times=times)
+
+
+def far_below(rng, tokens, E):
+    """Logits of which every second one is some hundred below the others, and what makes those the chosen ones."""
+    logits = rng.standard_normal((tokens, E)) * 2.0
+    logits[:, ::2] -= 110.0
+    bias = np.zeros(E, dtype=np.float32)
+    bias[::2] = 8.0 + rng.integers(0, 40, (E + 1) // 2) * 0.125
+    return logits, bias
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("times", [1, 1000])
+def test_route_scores_below_binary32(kind, score, times):
+    """The chosen scores and their sum leave binary32, their quotients do not."""
+    logits, bias = far_below(np.random.default_rng(kind[0]), 40, kind[0])
+    logits[1] -= 100.0
+    check_route(40, kind, score, True, logits=logits, bias=bias, times=times)
+    check_route(40, kind, score, False, logits=logits, bias=bias, times=times)
+
+
 def check_grad(tokens, kind, score, renormalise, dt=FP32, wt=FP32, scale=2.5, gap=0, shift=0, seed=0, experts=None, logits=None):
     torch, d = lib()
     E, k = kind[:2]
@@ -176,6 +211,19 @@ def test_grad_of_places_left_over(score, renormalise):
     logits[::3, 1::2] = -np.inf
     experts[::3, :3] = [0, 2, 4]
     check_grad(40, (70, 5, 1, 1, 1), score, renormalise, experts=experts, logits=logits)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("renormalise", [False, True])
+def test_grad_of_scores_below_binary32(kind, score, renormalise):
+    E, k = kind[:2]
+    rng = np.random.default_rng(E)
+    logits = far_below(rng, 40, E)[0]
+    experts = np.stack([rng.permutation(np.arange(0, E, 2))[:k] for _ in range(40)])
+    experts = np.pad(experts, ((0, 0), (0, k - experts.shape[1])), constant_values=-1)
+    experts[::7, 0] = E - 1 - (E - 1) % 2
+    check_grad(40, kind, score, renormalise, logits=logits, experts=experts)
 
 
 @pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
