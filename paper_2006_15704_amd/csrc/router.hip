@@ -252,12 +252,12 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 // ---- a token by a team ----
 //
 // A team of 1 to 64 lanes has up to kEach neighbouring experts a lane.  Keys in binary32 become words that sort as they do, with the place
-// in the lane for their last four bits; a lane sorts its own, and the team takes the largest head, as often as there are candidates: two more than
+// in the lane for their last four bits; a lane sorts its own, and the team takes the largest head, as often as there are candidates: one more than
 // are chosen.  Where the candidates' keys are all further apart than the error of a binary32 key, their order is that of binary64.
 // Where not, the candidates are ordered again by whole binary32 keys, equal logits with equal biases by their index.  Where that too leaves it open, or the
 // groups' scores come near each other, a wave does the token over in binary64: of 256 normal logits in eight groups, one token in 400.
 
-constexpr int kEach = 16, kSpare = 2;
+constexpr int kEach = 16, kSpare = 1;
 // A key's error in parts of 2^-24 of the largest score and bias: exp, sum and quotient of a softmax over 1024 under 30, the key's
 // rounding and the lift's 6 (a lifted key is up to twice as large), the bits given to the place 64: two keys 200.
 constexpr float kApart = 0x1p-16f;
@@ -335,7 +335,7 @@ __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp
 // EACH: the lane's experts, a.each of them used.  LANES: the logarithm of a team's lanes, if it is known (the steps of a meeting need no branches then:
 // 65536 tokens of 256 experts 47 us without).  Four lanes and 64 are held to the 80 registers of six waves, which the compiler exceeds by one.
 template <int LT, int EACH, bool HERE, int LANES>
-__global__ __launch_bounds__(kThreads, LANES == 2 || LANES == 6 ? 6 : 1) void route_team_kernel(RouteArgs a) {
+__global__ __launch_bounds__(kThreads, !HERE && (LANES == 2 || LANES == 6) ? 6 : 1) void route_team_kernel(RouteArgs a) {
     extern __shared__ double keys[];                 // [kWaves][room], then candidates and counts
     const int log2_lanes = LANES >= 0 ? LANES : a.log2_lanes, lanes = 1 << log2_lanes, l = threadIdx.x & (lanes - 1), team = threadIdx.x >> log2_lanes, teams = kThreads >> log2_lanes;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -436,8 +436,12 @@ __global__ __launch_bounds__(kThreads, LANES == 2 || LANES == 6 ? 6 : 1) void ro
                 for (int i = 0; i < EACH; ++i) w[i] = 0;
             }
         }
+        // what is behind a lane's head: in LDS, or where latency counts and there is little, in registers
+        constexpr bool SHIFT = HERE && EACH <= 8;
+        if constexpr (!SHIFT) {
 #pragma unroll
-        for (int i = 1; i < EACH; ++i) sorted[i * 64] = w[i];
+            for (int i = 1; i < EACH; ++i) sorted[i * 64] = w[i];
+        }
         float left = kMasked;                        // the largest key behind the candidates
         int taken = 0;
         for (int n = 0; n <= a.listed; ++n) {
@@ -449,8 +453,14 @@ __global__ __launch_bounds__(kThreads, LANES == 2 || LANES == 6 ? 6 : 1) void ro
             if (first_lane(__ballot(head == top), log2_lanes, of_team0) == l) {
                 word[n] = w[0];
                 at[n] = top != 0 ? e0 + 15 - static_cast<int>(w[0] & 15u) : -1;
-                ++taken;
-                w[0] = taken < EACH ? sorted[taken * 64] : 0u;
+                if constexpr (SHIFT) {
+#pragma unroll
+                    for (int i = 1; i < EACH; ++i) w[i - 1] = w[i];
+                    w[EACH - 1] = 0u;
+                } else {
+                    ++taken;
+                    w[0] = taken < EACH ? sorted[taken * 64] : 0u;
+                }
             }
         }
         wave_meets();
@@ -734,7 +744,8 @@ bool find_team(RouteArgs& a) {
 template <int LT, int EACH>
 bool launch_team(ddp_router* h, const RouteArgs& a, int64_t blocks, size_t bytes) {
     if (blocks <= kFewBlocks) {
-        hipLaunchKernelGGL((route_team_kernel<LT, EACH, true, -1>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), bytes, h->stream, a);
+        if (a.log2_lanes == 6) hipLaunchKernelGGL((route_team_kernel<LT, EACH, true, 6>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), bytes, h->stream, a);
+        else hipLaunchKernelGGL((route_team_kernel<LT, EACH, true, -1>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), bytes, h->stream, a);
         return blocks > 1;
     }
     const dim3 grid(static_cast<unsigned>(std::min(blocks, kBlocks))), threads(kThreads);
@@ -774,7 +785,11 @@ bool launch_route(ddp_router* h, RouteArgs a) {
 }
 template <int LT>
 hipError_t launch_grad(ddp_router* h, RouteGradArgs a) {
-    const int each = a.experts > 256 || (a.experts > 32 && 4 * a.chosen <= a.experts) ? 16 : 4;      // (many chosen take more lanes: their LDS is a team's)
+    // 16 where tokens are enough for it (60 experts: 20011 tokens 7.7 us with 16 and 6.2 with 4, of 64 65536 5.4 and 9.6); many chosen take more lanes: their LDS is a team's
+    int few = 0;
+    while (16 << few < a.experts) ++few;
+    const bool enough = a.tokens << few >= kFewBlocks * kThreads;
+    const int each = a.experts > 256 || (enough && a.experts > 32 && 4 * a.chosen <= a.experts) ? 16 : 4;
     while (each << a.log2_lanes < a.experts) ++a.log2_lanes;
     const int teams = kThreads >> a.log2_lanes;
     const dim3 blocks(static_cast<unsigned>(std::min<int64_t>((a.tokens + teams - 1) / teams, kBlocks))), threads(kThreads);
