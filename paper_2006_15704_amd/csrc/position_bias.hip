@@ -73,7 +73,7 @@ struct BiasArgs {
     char* scores;                                // dscores in the gradient
     float* partial;
     int64_t batch, queries, keys, offset, table_stride, s_batch, s_head, s_query;
-    int64_t band0, strips, center;               // of the gradient: the first lane of the first strip
+    int64_t band0, last, strips, center;         // of the gradient: the first lane of the first strip, the last that is visible
     int64_t tiles, plane_tiles, col_tiles;       // of the bias
     int32_t heads, buckets, sides, both, causal, strip_blocks, shares, rows, cols, log2_cols;
     float scale, masked;
@@ -201,6 +201,25 @@ __device__ __forceinline__ int64_t strip_of(const BiasArgs& a, int64_t turn) {
     return below < above ? turn : a.strips - 1 - turn;
 }
 
+// A vector's elements from byte `by` on (0 to 15), then anything.
+template <typename P>
+__device__ __forceinline__ void shift_down(P& v, int by) {
+    uint32_t* w = v.part[0].w;
+    if (by & 8) {
+        w[0] = w[2];
+        w[1] = w[3];
+    }
+    if (by & 4) {
+        w[0] = w[1];
+        w[1] = w[2];
+        w[2] = w[3];
+    }
+    if (by & 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = w[i] >> 16 | (i < 3 ? w[i + 1] << 16 : 0u);
+    }
+}
+
 template <int ST, bool NT>
 __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
     constexpr int N = ST == DDP_FP32 ? 4 : 8, DIAGONALS = Band<N>::diagonals;
@@ -217,7 +236,7 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
     for (int64_t turn = part / a.shares; turn < a.strips; turn += a.strip_blocks) {
         const int64_t t0 = a.band0 + strip_of(a, turn) * 64;
         // the row groups in which some lane has a column, of all sequences, in equal parts for all waves of the shares
-        const int64_t g_from = max(int64_t(0), -(t0 + 63)), steps = max(min(groups, vectors - t0) - g_from, int64_t(0));
+        const int64_t g_from = max(int64_t(0), -min(t0 + 63, a.last)), steps = max(min(groups, vectors - t0) - g_from, int64_t(0));
         const int64_t units = steps * a.batch, turns = static_cast<int64_t>(a.shares) * kWaves;
         const int64_t each = (units + turns - 1) / turns, mine = (static_cast<int64_t>(share) * kWaves + wave) * each;
         int64_t left = min(each, units - mine);
@@ -227,12 +246,13 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
             const int64_t here = min(left, g_from + steps - g), end = min(g + here, (queries + N - 1) / N);
             left -= here;
             const char* s = scores + b * a.s_batch * ElemBytes<ST>::value;
+            const int64_t before = b * a.s_batch + h * a.s_head;         // of the scores' memory; room: from here to its end
             const int64_t room = (a.batch - 1 - b) * a.s_batch + (a.heads - 1 - h) * a.s_head + (a.queries - 1) * a.s_query + a.keys;
             for (; g < end; ++g) {
                 const int64_t i = g * N;
                 const int c = static_cast<int>(g + t0 + lane) * N;
                 const unsigned at = static_cast<unsigned>(c) * ElemBytes<ST>::value;
-                if (c < 0 || c >= keys) continue;
+                if (c < 0 || c >= keys || lane > a.last - t0) continue;
                 // (what follows a row's keys is read with them, as far as the tensor reaches, and not used)
                 if ((i + N - 1) * a.s_query + c + N <= room) {
                     Parts<ST, N> v[N];
@@ -257,15 +277,28 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a) {
                         for (int k = 0; k < N; ++k) acc[k - x + N - 1] += e[k];
                     }
                 } else {
-                    // element by element in the tensor's last rows: the sums go round instead of the rows being unrolled
+                    // in the tensor's last rows a vector that would reach over its end is moved back to end with it, and its elements down
+                    // again; the sums go round instead of the rows being unrolled
                     const int have = static_cast<int>(min(keys - c, int64_t(N)));
+                    const bool whole = before + room >= N;
+                    auto place = [&](int x) { return (i + x) * a.s_query + c; };
+                    auto row = [&](int x) { return load_parts<ST, N>(s + min(place(x), room - N) * ElemBytes<ST>::value); };
+                    Parts<ST, N> next = {};
+                    if (whole) next = row(0);
 #pragma unroll 1
                     for (int x = 0; x < 2 * N - 1; ++x) {
-                        if (x < N && i + x < queries) {
+                        if (x < N) {
+                            Parts<ST, N> v = next;
                             float e[N];
-                            load_some<ST, N>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at, have, e);
+                            if (whole) {
+                                next = row(min(x + 1, N - 1));
+                                shift_down(v, static_cast<int>(max(min(place(x) - room + N, int64_t(N - 1)), int64_t(0))) * ElemBytes<ST>::value);
+                                widen<ST, N>(v, e);
+                            } else {
+                                load_some<ST, N>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at, i + x < queries ? have : 0, e);
+                            }
 #pragma unroll
-                            for (int k = 0; k < N; ++k) acc[k + N - 1] += e[k];
+                            for (int k = 0; k < N; ++k) acc[k + N - 1] += k < have && i + x < queries ? e[k] : 0.0f;
                         }
                         const float last = acc[2 * N - 2];
 #pragma unroll
@@ -569,6 +602,7 @@ int32_t ddp_position_bias_grad(ddp_position_bias* h, int64_t batch, int64_t quer
         int64_t last = (keys + n - 1) / n - 1;
         if (causal) last = std::min(last, offset + n - 1 >= 0 ? (offset + n - 1) / n : -((-offset) / n));
         a.band0 = 1 - groups;
+        a.last = last;
         a.strips = (last - a.band0 + 1 + 63) / 64;
         if (a.strips > 0) {
             a.center = std::max<int64_t>(0, std::min(a.strips - 1, (((keys + n - 1) / n - groups) / 2 - a.band0) / 64));
