@@ -81,6 +81,13 @@ inline void layer_release(LayerHandle* h) {
 
 #if defined(__HIPCC__)
 
+// The t-th tile of n in an order in which the blocks of an XCD (every eighth) have neighbouring tiles: each of the eight writes a stretch of
+// memory of its own.  A grid that goes round more than once is a multiple of eight.
+__device__ __forceinline__ int64_t tile_of_xcd(int64_t t, int64_t n) {
+    const int64_t x = t & 7, more = n & 7;
+    return x * (n >> 3) + (x < more ? x : more) + (t >> 3);
+}
+
 // Sums over the LANES (4, 8, 16, 32 or 64) neighbours of a lane, the same bits in all of them: neighbours within 16 by the VALU's lane
 // moves, further ones by swaps of rows.  (A shuffle is an LDS access: six of them one after the other take some 0.4 us of a wave.)
 template <int CTRL>

@@ -7,7 +7,7 @@
 //   grad[k][h]       = scale (sum of dscores[b, h, i, j] over the visible places of bucket k)  (+ what is there)
 //
 // A bias depends on the diagonal alone: forward is a fill, backward a sum along diagonals.  Both are bound by memory: 16 x 4096 x 4096 causal
-// bfloat16 scores (537 MB) are filled in 98 us where many calls follow each other, 5.4 TB/s, and 88 where a few do (a plain fill of as many bytes 78); the gradient of 2 x 16 x 4096 x 4096 (537 MB visible)
+// bfloat16 scores (537 MB) are filled in 91 us, 5.9 TB/s (a plain fill of as many bytes 78); the gradient of 2 x 16 x 4096 x 4096 (537 MB visible)
 // takes 98, of which 93 read 590 MB at 6.3 TB/s; 8 x 16 x 512 x 512 binary32 of ragged lengths 21.8, the join 4 of them.
 #include "layer_host.h"
 
@@ -77,7 +77,7 @@ struct BiasArgs {
     int64_t batch, queries, keys, offset, table_stride, s_batch, s_head, s_query;
     int64_t band0, last, strips, center;         // of the gradient: the first lane of the first strip, the last that is visible
     int64_t tiles, plane_tiles, col_tiles;       // of the bias
-    int32_t heads, buckets, sides, both, causal, strip_blocks, shares, rows, cols, log2_cols;
+    int32_t heads, buckets, sides, both, causal, strip_blocks, shares, rows, cols, log2_cols, regions;
     float scale, masked;
 };
 
@@ -116,7 +116,8 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
     for (int k = threadIdx.x; k < a.sides; k += kThreads) first[k] = a.first[k];
     const int x = threadIdx.x & (a.cols - 1), y = threadIdx.x >> a.log2_cols;
     const int high = (kThreads >> a.log2_cols) * a.rows, wide = a.cols * N;
-    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+    for (int64_t turn = blockIdx.x; turn < a.tiles; turn += gridDim.x) {
+        const int64_t tile = !ADD && a.regions ? tile_of_xcd(turn, a.tiles) : turn;
         const int64_t in_plane = tile % a.plane_tiles, plane = tile / a.plane_tiles, h = plane % a.heads, b = plane / a.heads;
         const int64_t c0 = in_plane % a.col_tiles * wide, i0 = in_plane / a.col_tiles * high;
         const int rows_here = static_cast<int>(min(a.queries - i0, int64_t(high))), cols_here = static_cast<int>(min(a.keys - c0, int64_t(wide)));
@@ -419,6 +420,9 @@ hipError_t launch_apply(ddp_position_bias* h, BiasArgs a, bool add) {
     const int64_t high = static_cast<int64_t>(a.rows) * down;
     a.plane_tiles = a.col_tiles * ((a.queries + high - 1) / high);
     a.tiles = planes * a.plane_tiles;
+    // A fill that no cache holds goes to a stretch of memory for each XCD (16 x 4096 x 4096 bfloat16 91 us, neighbouring tiles in different XCDs
+    // 100; in rows that are three elements further apart 110 and 128; 16 x 2048 x 2048 28 and 26); what is read too does not (165 us, that way 186).
+    a.regions = planes * a.queries * a.keys * ElemBytes<OT>::value >= kStreamBytes;
     const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(a.tiles, kMaxTiles));
     if (add) hipLaunchKernelGGL((apply_kernel<TT, OT, true>), dim3(blocks), dim3(kThreads), 0, h->stream, a);
     else hipLaunchKernelGGL((apply_kernel<TT, OT, false>), dim3(blocks), dim3(kThreads), 0, h->stream, a);

@@ -359,3 +359,25 @@ def test_strides_of_single_entries_may_be_anything():
     want = np.bincount(places, weights=out_of.double().numpy(), minlength=32)
     assert np.allclose(grad[:, 0].double().cpu().numpy(), want, rtol=1e-6, atol=1e-6)
     d.ddp_position_bias_destroy(h)
+
+
+@pytest.mark.parametrize("heads,queries,keys,offset,gap,dt", [(5, 4099, 3331, 0, 0, FP32), (3, 6007, 8009, 2002, 3, BF16)])
+def test_apply_beyond_the_caches(heads, queries, keys, offset, gap, dt):
+    """More than 256 MiB, tiles of no multiple of eight: every place is written, and none between the rows."""
+    torch, d = lib()
+    kind = (32, 8, 700, True)
+    out = torch.full((heads, queries, keys + gap), GUARD, dtype=torch_type(dt), device="cuda")
+    table = torch.randn((32, heads), generator=torch.Generator("cuda").manual_seed(keys), device="cuda")
+    h = d.ddp_position_bias_create(0, 0, heads, *kind)
+    first = torch.from_numpy(d.ddp_position_bias_buckets(h)).cuda().long()
+    torch.cuda.synchronize()
+    d.ddp_position_bias_apply(h, 1, queries, keys, offset, table.data_ptr(), FP32, heads, 0.5, 0, True, -7.0, False, out.data_ptr(), dt, 0,
+                              out.stride(0), out.stride(1))
+    torch.cuda.synchronize()
+    r = torch.arange(keys, device="cuda")[None] - torch.arange(queries, device="cuda")[:, None] - offset
+    bucket = torch.bucketize(r.abs(), first, right=True) - 1 + (r > 0) * 16
+    for n in range(heads):
+        want = torch.where(r > 0, torch.full((), -7.0, device="cuda"), (table[:, n] * 0.5)[bucket]).to(out.dtype)
+        assert torch.equal(out[n, :, :keys], want)
+    assert (out[:, :, keys:] == GUARD).all()
+    d.ddp_position_bias_destroy(h)
