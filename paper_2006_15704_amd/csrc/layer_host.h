@@ -88,6 +88,43 @@ __device__ __forceinline__ int64_t tile_of_xcd(int64_t t, int64_t n) {
     return x * (n >> 3) + (x < more ? x : more) + (t >> 3);
 }
 
+// Partial sums that the last block of a short launch joins, in place of another launch: stored and read with relaxed device-scope atomics, which go
+// through the caches, and waited for before a block arrives (a release would write back whole caches).  Called by all threads of all
+// `blocks` blocks; true in the block that arrives last, which leaves the counter at zero.
+__device__ __forceinline__ void put_part(float* p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get_part(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ bool arrives_last(uint32_t* counter, unsigned blocks) {
+    __shared__ bool last;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // this wave's parts are there
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == blocks - 1;
+        if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return last;
+}
+// The sum of `parts` parts that lie `stride` apart.
+__device__ __forceinline__ double parts_sum(const float* from, int parts, int64_t stride) {
+    constexpr int DEEP = 8;
+    double sum = 0.0;
+    for (int k = 0; k < parts; k += DEEP) {
+        float x[DEEP];                               // (no condition on a load: it would be waited for before the next)
+#pragma unroll
+        for (int u = 0; u < DEEP; ++u) x[u] = get_part(from + min(k + u, parts - 1) * stride);
+#pragma unroll
+        for (int u = 0; u < DEEP; ++u) sum += k + u < parts ? x[u] : 0.0f;
+    }
+    return sum;
+}
+// A gradient of any type, added to what is there or in its place.
+__device__ __forceinline__ void put_grad(char* p, int type, int64_t at, int add, double x) {
+    char* to = p + at * (type == DDP_FP32 ? 4 : 2);
+    if (type == DDP_FP32) store_one<DDP_FP32>(to, static_cast<float>(add ? x + load_one<DDP_FP32>(to) : x));
+    else if (type == DDP_FP16) store_one<DDP_FP16>(to, static_cast<float>(add ? x + load_one<DDP_FP16>(to) : x));
+    else store_one<DDP_BF16>(to, static_cast<float>(add ? x + load_one<DDP_BF16>(to) : x));
+}
+
 // Sums over the LANES (4, 8, 16, 32 or 64) neighbours of a lane, the same bits in all of them: neighbours within 16 by the VALU's lane
 // moves, further ones by swaps of rows.  (A shuffle is an LDS access: six of them one after the other take some 0.4 us of a wave.)
 template <int CTRL>

@@ -13,6 +13,7 @@ struct ddp_layernorm : ddp::LayerHandle {
     int64_t width = 0;
     int32_t chunks = 0;                          // row chunks that the workspace holds sums of
     float* partial = nullptr;                    // [chunks][2][width]
+    uint32_t* counter = nullptr;
 };
 
 namespace {
@@ -38,8 +39,10 @@ struct BackwardArgs {
     const float *mean, *rstd;
     char *dx;
     float* partial;
+    uint32_t* counter;                               // of the blocks that have arrived, where the last one joins
+    char *dgamma, *dbeta;
     int64_t rows, dy_stride, x_stride, dsum_stride, dx_stride, rows_per_chunk;
-    int32_t width, param, chunks, stream;
+    int32_t width, param, chunks, stream, grad, add;
 };
 
 // gamma or beta: `none` where there is none.
@@ -379,10 +382,28 @@ __global__ __launch_bounds__(T::THREADS) void backward_team_kernel(BackwardArgs 
         }
         __syncthreads();
     }
-    if (threadIdx.x >= T::SIZE) return;
-    char* to = reinterpret_cast<char*>(a.partial + static_cast<int64_t>(blockIdx.x) * 2 * a.width);
-    team.template store<DDP_FP32>(to, true, dgamma);
-    team.template store<DDP_FP32>(to + static_cast<int64_t>(a.width) * 4, true, dbeta);
+    float* to = a.partial + static_cast<int64_t>(blockIdx.x) * 2 * a.width;
+    if (a.counter == nullptr) {
+        if (threadIdx.x >= T::SIZE) return;
+        team.template store<DDP_FP32>(reinterpret_cast<char*>(to), true, dgamma);
+        team.template store<DDP_FP32>(reinterpret_cast<char*>(to + a.width), true, dbeta);
+        return;
+    }
+    if (threadIdx.x < T::SIZE) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i >= team.own[v]) {
+                    put_part(to + team.at[v] + i, dgamma[v][i]);
+                    put_part(to + a.width + team.at[v] + i, dbeta[v][i]);
+                }
+    }
+    if (!arrives_last(a.counter, gridDim.x)) return;
+    for (int c = threadIdx.x; c < 2 * a.width; c += T::THREADS) {
+        char* grad = c < a.width ? a.dgamma : a.dbeta;
+        if (grad != nullptr) put_grad(grad, a.grad, c < a.width ? c : c - a.width, a.add, parts_sum(a.partial + c, gridDim.x, 2 * static_cast<int64_t>(a.width)));
+    }
 }
 
 // ---- other rows ----
@@ -543,15 +564,15 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(JoinArgs a) {
     if (wave != 0 || c >= a.width) return;
 #pragma unroll
     for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
-    char* to = out + static_cast<int64_t>(c) * (a.grad == DDP_FP32 ? 4 : 2);
-    if (a.grad == DDP_FP32) store_one<DDP_FP32>(to, static_cast<float>(a.add ? sum + load_one<DDP_FP32>(to) : sum));
-    else if (a.grad == DDP_FP16) store_one<DDP_FP16>(to, static_cast<float>(a.add ? sum + load_one<DDP_FP16>(to) : sum));
-    else store_one<DDP_BF16>(to, static_cast<float>(a.add ? sum + load_one<DDP_BF16>(to) : sum));
+    put_grad(out, a.grad, c, a.add, sum);
 }
 
 // ---- host ----
 
 constexpr int kRowBlocks = 1 << 16;
+// Parts and columns that the last block joins, in place of another launch: 8 x 256 5.7 us, 30 x 500 7.3, both 8.2 in two launches; one row of 4096, which
+// is 16 columns a thread one after the other, 18.6.
+constexpr int64_t kJoinParts = 4096, kJoinColumns = 512;
 
 // Forward: a block for every row group (16384 x 1024 21.1 us, 1536 blocks that go on 22.4); teams of eight waves and more go on, which keeps
 // their parameters in registers (4096 x 8192 48.7 us, a block a row 51.9).  Elements a lane: forward 16 (without residual 12.4 us, 8: 14.4), backward 8, which
@@ -587,16 +608,17 @@ hipError_t launch_forward(ddp_layernorm* h, const ForwardArgs& a) {
         hipLaunchKernelGGL((forward_kernel<XT, YT>), dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kRowBlocks))), dim3(kThreads), 0, h->stream, a);
     return hipGetLastError();
 }
-// Returns the row chunks that sums are left of.
+// Returns the row chunks that sums are left of, -1 where they are joined already.
 template <int XT, int YT>
 int32_t launch_backward(ddp_layernorm* h, BackwardArgs a) {
     int32_t chunks = a.chunks;
     const bool team = with_team<XT, YT, kBackwardThreads, kBackwardEach>(a.width, [&](auto t) {
         typedef decltype(t) T;
         chunks = static_cast<int32_t>(std::min<int64_t>((a.rows + T::TEAMS - 1) / T::TEAMS, h->chunks));
+        if (a.partial != nullptr && a.width <= kJoinColumns && static_cast<int64_t>(chunks) * 2 * a.width <= kJoinParts) a.counter = h->counter;
         hipLaunchKernelGGL((backward_team_kernel<XT, YT, T>), dim3(static_cast<unsigned>(chunks)), dim3(T::THREADS), 0, h->stream, a);
     });
-    if (team) return chunks;
+    if (team) return a.counter != nullptr ? -1 : chunks;
     if (a.dx != nullptr)
         hipLaunchKernelGGL((backward_rows_kernel<XT, YT>), dim3(static_cast<unsigned>(std::min<int64_t>(a.rows, kRowBlocks))), dim3(kThreads), 0, h->stream, a);
     if (a.partial != nullptr)
@@ -645,12 +667,20 @@ int32_t ddp_layernorm_create(ddp_layernorm** out, int32_t device, void* stream, 
     // two blocks a compute unit, one of the widest teams (32768 x 4096: 512 chunks 195 us, 256 213; 2048 x 12000: 256 53.6, 512 70.7)
     h->chunks = static_cast<int32_t>(std::max<int64_t>(16, std::min<int64_t>(width <= 8 * 1024 ? 512 : 256, (int64_t(1) << 22) / width)));
     if (device != DDP_DEVICE_NONE) {
-        const hipError_t err = layer_alloc(h, static_cast<int64_t>(h->chunks) * 2 * width * 4);
+        const int64_t sums = static_cast<int64_t>(h->chunks) * 2 * width * 4;
+        hipError_t err = layer_alloc(h, sums + 256);
+        if (err == hipSuccess) {
+            OnDevice on(device);
+            const uint32_t none = 0;
+            err = taken(hipMemcpy(h->mem + sums, &none, sizeof none, hipMemcpyHostToDevice));
+            if (err != hipSuccess) (void)taken(hipFree(h->mem));
+        }
         if (err != hipSuccess) {
             delete h;
             return layer_fail(nullptr, DDP_ERR_HIP, hipGetErrorString(err));
         }
         h->partial = reinterpret_cast<float*>(h->mem);
+        h->counter = reinterpret_cast<uint32_t*>(h->mem + sums);
     }
     *out = h;
     return DDP_OK;
@@ -733,6 +763,10 @@ int32_t ddp_layernorm_backward(ddp_layernorm* h, int64_t rows, const void* dy, i
     a.rstd = rstd;
     a.dx = static_cast<char*>(dx);
     a.partial = params ? h->partial : nullptr;
+    a.dgamma = static_cast<char*>(dgamma);
+    a.dbeta = static_cast<char*>(dbeta);
+    a.grad = grad_dtype;
+    a.add = accumulate != 0;
     a.rows = rows;
     a.dy_stride = dy_stride;
     a.x_stride = x_stride;
@@ -748,7 +782,7 @@ int32_t ddp_layernorm_backward(ddp_layernorm* h, int64_t rows, const void* dy, i
         chunks = with_types(x_dtype, dy_dtype, [&](auto xt, auto yt) { return launch_backward<xt.value, yt.value>(h, a); });
         LAYER_HIP(h, hipGetLastError());
     }
-    if (!params) return DDP_OK;
+    if (!params || chunks < 0) return DDP_OK;
     JoinArgs j{h->partial, static_cast<char*>(dgamma), static_cast<char*>(dbeta), a.width, chunks, grad_dtype, accumulate != 0};
     hipLaunchKernelGGL(join_kernel, dim3(static_cast<unsigned>((a.width + 63) / 64), 2), dim3(64 * kJoinWaves), 0, h->stream, j);
     LAYER_HIP(h, hipGetLastError());

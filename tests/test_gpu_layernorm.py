@@ -406,3 +406,49 @@ def test_in_place(width, dt):
     for a, b in zip(backward(along, along), want):
         assert torch.equal(a, b)
     d.ddp_layernorm_destroy(h)
+
+
+@pytest.mark.parametrize("rows,width", [(1, 64), (8, 256), (30, 500), (33, 512), (33, 513), (200, 128), (2000, 24), (129, 17)])
+def test_backward_of_few_rows_again_and_again(rows, width):
+    """Where the last block joins the sums: whole numbers, so that every order of them has the same sum; other sizes on the same handle and replays of
+    a graph in between, and what is added to."""
+    torch, d = lib()
+    gen = torch.Generator("cuda").manual_seed(width)
+    stream = torch.cuda.Stream()
+    h = d.ddp_layernorm_create(0, stream.cuda_stream, width)
+    many = 40000
+    dy = torch.randint(-2, 3, (many, width), generator=gen, device="cuda").float()
+    x = torch.randint(-2, 3, (many, width), generator=gen, device="cuda").float()
+    mean, rstd, dx = torch.zeros(many, device="cuda"), torch.ones(many, device="cuda"), torch.empty_like(x)
+    dgamma, dbeta = torch.zeros(width, device="cuda"), torch.zeros(width, device="cuda")
+    torch.cuda.synchronize()
+
+    def call(n, add):
+        d.ddp_layernorm_backward(h, n, dy.data_ptr(), FP32, width, x.data_ptr(), FP32, width, mean.data_ptr(), rstd.data_ptr(), 0, FP32, 0, 0, dx.data_ptr(),
+                                 width, add, dgamma.data_ptr(), dbeta.data_ptr(), FP32)
+
+    def want(n):
+        return (dy[:n].double() * x[:n].double()).sum(0).float(), dy[:n].double().sum(0).float()
+
+    few, one, all_of_them = want(rows), want(1), want(many)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        call(rows, False)
+        stream.synchronize()
+        graph.capture_begin()
+        call(rows, True)
+        graph.capture_end()
+        for turn in range(50):
+            call(rows, False)
+            assert torch.equal(dgamma, few[0]) and torch.equal(dbeta, few[1]), turn
+            call(1, True)
+            assert torch.equal(dgamma, few[0] + one[0]) and torch.equal(dbeta, few[1] + one[1]), turn
+            graph.replay()
+            assert torch.equal(dgamma, 2 * few[0] + one[0]) and torch.equal(dbeta, 2 * few[1] + one[1]), turn
+            if turn % 10 == 0:
+                call(many, False)
+                assert torch.equal(dgamma, all_of_them[0]) and torch.equal(dbeta, all_of_them[1]), turn
+        stream.synchronize()
+    torch.cuda.synchronize()
+    d.ddp_layernorm_destroy(h)
