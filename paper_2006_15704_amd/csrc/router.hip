@@ -272,6 +272,8 @@ constexpr float kNearSoftmax = 0x1p-18f, kNearKey = 0x1p-20f;
 // Chosen scores whose sum is below this (biases have chosen them, or every logit of a sigmoid is far below 0) are near binary32's end, their
 // quotients not: a wave takes the weights in binary64.
 constexpr float kTiny = 0x1p-100f;
+// Below this a lifted key and the sum of a group's two largest are finite, above -inf and below inf.
+constexpr float kGroupLift = 0x1p126f;
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t lane_moved(uint32_t x) {
@@ -436,7 +438,8 @@ __global__ __launch_bounds__(kThreads, !HERE && (LANES == 2 || LANES == 6) ? 6 :
             }
             const float worst = -team_max(log2_lanes, before < a.kept && group < a.groups ? -rank : kMasked);
             const float next = team_max(log2_lanes, before >= a.kept && group < a.groups ? rank : kMasked);
-            again = (next > kMasked && !(worst - next > 2.0f * apart)) || !(lift < __builtin_huge_valf());
+            // (a finite bias of 2^126 and more takes a lifted key, or a group's two keys together, out of binary32: binary64)
+            again = (next > kMasked && !(worst - next > 2.0f * apart)) || !(lift < kGroupLift);
             if (before >= a.kept) {
 #pragma unroll
                 for (int i = 0; i < EACH; ++i) w[i] = 0;
