@@ -107,9 +107,10 @@ class Layer:
 
     def step(self, p: Dict[str, torch.Tensor], grad: Dict[str, torch.Tensor], balance: torch.Tensor, now: torch.Tensor, then: torch.Tensor,
              lengths: torch.Tensor, counts: torch.Tensor) -> Tuple[torch.Tensor, Sequence[int]]:
-        """One replica's forward and backward pass: writes its gradients and counts (int32 [experts]); experts that no token
-        chose have theirs left as they are.  now, then: int64 [sequences, length]; lengths: int32 [sequences], behind which tokens are -1.
-        Returns (mean loss, the counts on the host)."""
+        """One replica's forward and backward pass: writes its gradients and counts (int32 [experts]: the tokens of each expert).
+        now, then: int64 [sequences, length]; lengths: int32 [sequences], behind which tokens are -1.  Returns (mean loss, the rows that the
+        router gave each expert, those behind a sequence's end among them).  Gradients of experts without a row are left as they are; where all
+        their rows are behind an end they are zeros, and their count is 0."""
         s, T, D, H = self.sizes, self.tokens, self.sizes.width, self.sizes.heads
         S, L, scale = s.sequences, s.length, math.sqrt(s.width)
         head = D // H
@@ -127,14 +128,18 @@ class Layer:
         gate = b @ p["router"].t()
         chosen = torch.empty((T, s.chosen), dtype=torch.int32, device=now.device)
         weights = torch.empty((T, s.chosen), device=now.device)
+        rows = torch.empty(s.experts, dtype=torch.int32, device=now.device)
         B.ddp_router_route(self.router, T, gate.data_ptr(), B.DDP_FP32, s.experts, balance.data_ptr(), chosen.data_ptr(), weights.data_ptr(),
-                           B.DDP_FP32, counts.data_ptr())
+                           B.DDP_FP32, rows.data_ptr())
+        # rows behind a sequence's end are routed with the rest, and that is all: no expert has them, no count and no gradient
+        picked = chosen.masked_fill((now.view(-1) < 0)[:, None], -1)
+        counts.copy_((picked.view(-1, 1) == torch.arange(s.experts, device=now.device)).sum(0))
         mixed, kept = torch.zeros((T, D), device=now.device), {}
-        load = counts.tolist()
+        load = rows.tolist()
         for e in range(s.experts):
             if load[e] == 0:
                 continue
-            t, n = (chosen == e).nonzero(as_tuple=True)
+            t, n = (picked == e).nonzero(as_tuple=True)
             up = b[t] @ p[f"up{e}"].t()
             down = torch.relu(up) @ p[f"down{e}"].t()
             mixed.index_add_(0, t, weights[t, n][:, None] * down)
@@ -160,7 +165,7 @@ class Layer:
             grad[f"up{e}"].copy_(dup.t() @ b[t])
             db.index_add_(0, t, dup @ p[f"up{e}"])
         dgate = torch.empty_like(gate)
-        B.ddp_router_grad(self.router, T, gate.data_ptr(), B.DDP_FP32, s.experts, chosen.data_ptr(), dweights.data_ptr(), B.DDP_FP32, dgate.data_ptr(),
+        B.ddp_router_grad(self.router, T, gate.data_ptr(), B.DDP_FP32, s.experts, picked.data_ptr(), dweights.data_ptr(), B.DDP_FP32, dgate.data_ptr(),
                           s.experts)
         grad["router"].copy_(dgate.t() @ b)
         db += dgate @ p["router"]

@@ -157,9 +157,9 @@ def run_layer(replicas: int = 2, steps: int = 40, bits: int = 32, sizes: layer.S
                 total, load = torch.zeros((), device=device), []
                 for r in range(replicas):
                     batch = [x.to(device) for x in sequences(task, sizes, (seed * 100003 + step) * 64 + r)]
-                    loss, counted = model.step(params, grad[r], balance, *batch, counts[r])
+                    loss, _ = model.step(params, grad[r], balance, *batch, counts[r])
                     total += loss / replicas
-                    load.append(counted)
+                    load.append(counts[r].tolist())
                 for i in reversed(range(n)):
                     expert = layer.expert_of(keys[i])
                     if expert >= 0:                                  # takes part where tokens have reached it
