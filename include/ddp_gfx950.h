@@ -698,8 +698,10 @@ int32_t ddp_position_bias_apply(ddp_position_bias* bias, int64_t batch, int64_t 
 
 /* grad[k][h] = scale * sum of dscores[b, h, i, j] over the visible places of bucket k (zeros where there are none; accumulate != 0:
  * added to what grad holds).  Places are visible as above, and only queries i < query_lengths[b] (NULL: all) take part.  Strides of dscores
- * may be anything from 0 on (0: the same scores for all); what lies between its rows is memory that can be read.  Sums in binary32 along a diagonal and binary64 across, in an order that depends on the sizes
- * alone (repeated calls give the same bits), rounded once. */
+ * may be anything from 0 on (0: the same scores for all); what lies between its rows is memory that can be read.  A diagonal's
+ * places are summed in binary32 in runs of up to 512 (256 of binary32 scores), four of them at a time, and everything else in binary64, in an order that
+ * depends on the sizes alone (repeated calls give the same bits); each block's part of a bucket is rounded to binary32 before the parts are joined,
+ * and the result to the type of grad. */
 int32_t ddp_position_bias_grad(ddp_position_bias* bias, int64_t batch, int64_t queries, int64_t keys, int64_t offset, const void* dscores,
                                int32_t dtype, int64_t batch_stride, int64_t head_stride, int64_t query_stride, float scale,
                                const int32_t* key_lengths, const int32_t* query_lengths, int32_t causal, int32_t accumulate, void* grad,

@@ -183,8 +183,10 @@ __global__ __launch_bounds__(kThreads) void apply_kernel(BiasArgs a) {
 // a lane holds them in registers, loads whole aligned vectors, and adds every element once.  Lane t of the band has columns N (g + t) in the
 // rows N g ... N g + N - 1; neighbours in a wave are neighbours in memory.
 //
-// A block has the 64 lanes' band (64 N diagonals) of one head and a share of its row groups of all sequences, which go round its waves.  Then
-// diagonals are put together in LDS, and buckets, which are ranges of diagonals, summed in binary64.
+// A block has the 64 lanes' band (64 N diagonals) of one head and a share of its row groups of all sequences, in equal parts for its waves.  Every
+// kRun row groups, at most 64 N additions of a diagonal in binary32, the waves' diagonals are put together in LDS, and buckets, which are ranges of
+// diagonals, summed in binary64 (one chain over 134 sequences of 4096 equal scores was off by 2^-9).
+constexpr int64_t kRun = 64;
 
 template <int N> struct Band {
     static constexpr int diagonals = 64 * N + N - 1, low = N - 1;    // element e of row x of lane t: N t + e - x + low
@@ -250,115 +252,124 @@ __global__ __launch_bounds__(kThreads) void diagonal_kernel(BiasArgs a, JoinArgs
         const int64_t g_from = max(int64_t(0), -min(t0 + 63, a.last)), steps = max(min(groups, vectors - t0) - g_from, int64_t(0));
         const int64_t units = steps * a.batch, turns = static_cast<int64_t>(a.shares) * kWaves;
         const int64_t each = (units + turns - 1) / turns, mine = (static_cast<int64_t>(share) * kWaves + wave) * each;
-        int64_t left = min(each, units - mine);
-        float acc[2 * N - 1] = {};
-        for (int64_t b = left > 0 ? mine / steps : 0, g = g_from + (left > 0 ? mine % steps : 0); left > 0; ++b, g = g_from) {
-            const int64_t keys = length_of(a.key_lengths, b, a.keys), queries = length_of(a.query_lengths, b, a.queries);
-            const int64_t here = min(left, g_from + steps - g), end = min(g + here, (queries + N - 1) / N);
-            left -= here;
-            const char* s = scores + b * a.s_batch * ElemBytes<ST>::value;
-            const int64_t before = b * a.s_batch + h * a.s_head;         // of the scores' memory; room: from here to its end
-            const int64_t room = (a.batch - 1 - b) * a.s_batch + (a.heads - 1 - h) * a.s_head + (a.queries - 1) * a.s_query + a.keys;
-            for (; g < end; ++g) {
-                const int64_t i = g * N;
-                const int c = static_cast<int>(g + t0 + lane) * N;
-                const unsigned at = static_cast<unsigned>(c) * ElemBytes<ST>::value;
-                if (c < 0 || c >= keys || lane > a.last - t0) continue;
-                // (what follows a row's keys is read with them, as far as the tensor reaches, and not used)
-                if ((i + N - 1) * a.s_query + c + N <= room) {
-                    Parts<ST, N> v[N];
+        int64_t rest = min(each, units - mine), b = rest > 0 ? mine / steps : 0, g = g_from + (rest > 0 ? mine % steps : 0);
+        for (int64_t runs = (each + kRun - 1) / kRun; runs > 0; --runs) {
+            float acc[2 * N - 1] = {};
+            int64_t left = min(rest, kRun);
+            rest -= left;
+            while (left > 0) {
+                const int64_t keys = length_of(a.key_lengths, b, a.keys), queries = length_of(a.query_lengths, b, a.queries);
+                const int64_t here = min(left, g_from + steps - g), stop = g + here, end = min(stop, (queries + N - 1) / N);
+                left -= here;
+                const char* s = scores + b * a.s_batch * ElemBytes<ST>::value;
+                const int64_t before = b * a.s_batch + h * a.s_head;         // of the scores' memory; room: from here to its end
+                const int64_t room = (a.batch - 1 - b) * a.s_batch + (a.heads - 1 - h) * a.s_head + (a.queries - 1) * a.s_query + a.keys;
+                for (; g < end; ++g) {
+                    const int64_t i = g * N;
+                    const int c = static_cast<int>(g + t0 + lane) * N;
+                    const unsigned at = static_cast<unsigned>(c) * ElemBytes<ST>::value;
+                    if (c < 0 || c >= keys || lane > a.last - t0) continue;
+                    // (what follows a row's keys is read with them, as far as the tensor reaches, and not used)
+                    if ((i + N - 1) * a.s_query + c + N <= room) {
+                        Parts<ST, N> v[N];
 #pragma unroll
-                    for (int x = 0; x < N; ++x) v[x] = load_parts<ST, N, NT>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at);
-                    const bool partial = c + N > keys || i + N > queries;
-                    const int have = static_cast<int>(min(keys - c, int64_t(N))), rows = static_cast<int>(min(queries - i, int64_t(N)));
-                    if (__ballot(partial) != 0) {
+                        for (int x = 0; x < N; ++x) v[x] = load_parts<ST, N, NT>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at);
+                        const bool partial = c + N > keys || i + N > queries;
+                        const int have = static_cast<int>(min(keys - c, int64_t(N))), rows = static_cast<int>(min(queries - i, int64_t(N)));
+                        if (__ballot(partial) != 0) {
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const int in = have * ElemBytes<ST>::value - 4 * w;          // bytes of this word
-                            const uint32_t keep = in >= 4 ? ~0u : in == 2 ? 0xFFFFu : 0u;
+                            for (int w = 0; w < 4; ++w) {
+                                const int in = have * ElemBytes<ST>::value - 4 * w;          // bytes of this word
+                                const uint32_t keep = in >= 4 ? ~0u : in == 2 ? 0xFFFFu : 0u;
 #pragma unroll
-                            for (int x = 0; x < N; ++x) v[x].part[0].w[w] &= x < rows ? keep : 0u;
-                        }
-                    }
-#pragma unroll
-                    for (int x = 0; x < N; ++x) {
-                        float e[N];
-                        widen<ST, N>(v[x], e);
-#pragma unroll
-                        for (int k = 0; k < N; ++k) acc[k - x + N - 1] += e[k];
-                    }
-                } else {
-                    // in the tensor's last rows a vector that would reach over its end is moved back to end with it, and its elements down
-                    // again; the sums go round instead of the rows being unrolled
-                    const int have = static_cast<int>(min(keys - c, int64_t(N)));
-                    const bool whole = before + room >= N;
-                    auto place = [&](int x) { return (i + x) * a.s_query + c; };
-                    auto row = [&](int x) { return load_parts<ST, N>(s + min(place(x), room - N) * ElemBytes<ST>::value); };
-                    Parts<ST, N> next = {};
-                    if (whole) next = row(0);
-#pragma unroll 1
-                    for (int x = 0; x < 2 * N - 1; ++x) {
-                        if (x < N) {
-                            Parts<ST, N> v = next;
-                            float e[N];
-                            if (whole) {
-                                next = row(min(x + 1, N - 1));
-                                shift_down(v, static_cast<int>(max(min(place(x) - room + N, int64_t(N - 1)), int64_t(0))) * ElemBytes<ST>::value);
-                                widen<ST, N>(v, e);
-                            } else {
-                                load_some<ST, N>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at, i + x < queries ? have : 0, e);
+                                for (int x = 0; x < N; ++x) v[x].part[0].w[w] &= x < rows ? keep : 0u;
                             }
-#pragma unroll
-                            for (int k = 0; k < N; ++k) acc[k + N - 1] += k < have && i + x < queries ? e[k] : 0.0f;
                         }
-                        const float last = acc[2 * N - 2];
 #pragma unroll
-                        for (int k = 2 * N - 2; k > 0; --k) acc[k] = acc[k - 1];
-                        acc[0] = last;
+                        for (int x = 0; x < N; ++x) {
+                            float e[N];
+                            widen<ST, N>(v[x], e);
+#pragma unroll
+                            for (int k = 0; k < N; ++k) acc[k - x + N - 1] += e[k];
+                        }
+                    } else {
+                        // in the tensor's last rows a vector that would reach over its end is moved back to end with it, and its elements down
+                        // again; the sums go round instead of the rows being unrolled
+                        const int have = static_cast<int>(min(keys - c, int64_t(N)));
+                        const bool whole = before + room >= N;
+                        auto place = [&](int x) { return (i + x) * a.s_query + c; };
+                        auto row = [&](int x) { return load_parts<ST, N>(s + min(place(x), room - N) * ElemBytes<ST>::value); };
+                        Parts<ST, N> next = {};
+                        if (whole) next = row(0);
+#pragma unroll 1
+                        for (int x = 0; x < 2 * N - 1; ++x) {
+                            if (x < N) {
+                                Parts<ST, N> v = next;
+                                float e[N];
+                                if (whole) {
+                                    next = row(min(x + 1, N - 1));
+                                    shift_down(v, static_cast<int>(max(min(place(x) - room + N, int64_t(N - 1)), int64_t(0))) * ElemBytes<ST>::value);
+                                    widen<ST, N>(v, e);
+                                } else {
+                                    load_some<ST, N>(s + (i + x) * a.s_query * ElemBytes<ST>::value + at, i + x < queries ? have : 0, e);
+                                }
+#pragma unroll
+                                for (int k = 0; k < N; ++k) acc[k + N - 1] += k < have && i + x < queries ? e[k] : 0.0f;
+                            }
+                            const float last = acc[2 * N - 2];
+#pragma unroll
+                            for (int k = 2 * N - 2; k > 0; --k) acc[k] = acc[k - 1];
+                            acc[0] = last;
+                        }
                     }
                 }
+                g = stop;
+                if (g == g_from + steps) {
+                    ++b;
+                    g = g_from;
+                }
             }
-        }
-        // diagonals of two neighbouring lanes: first each lane's upper ones (and the lowest lane's lower ones), then the others'
-        __syncthreads();
+            // diagonals of two neighbouring lanes: first each lane's upper ones (and the lowest lane's lower ones), then the others'
+            __syncthreads();
 #pragma unroll
-        for (int k = 0; k < N; ++k) diagonal[wave][N * lane + k + N - 1] = acc[k + N - 1];
-        if (lane == 0) {
+            for (int k = 0; k < N; ++k) diagonal[wave][N * lane + k + N - 1] = acc[k + N - 1];
+            if (lane == 0) {
 #pragma unroll
-            for (int k = 0; k < N - 1; ++k) diagonal[wave][k] = acc[k];
-        }
-        __syncthreads();
-        if (lane > 0) {
-#pragma unroll
-            for (int k = 0; k < N - 1; ++k) diagonal[wave][N * lane + k] += acc[k];
-        }
-        __syncthreads();
-        for (int d = threadIdx.x; d < DIAGONALS; d += kThreads) {
-            float sum = diagonal[0][d];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) sum += diagonal[w][d];
-            diagonal[0][d] = sum;
-        }
-        __syncthreads();
-        // buckets go round the threads; those of many diagonals take a wave each
-        const int64_t r0 = t0 * N - Band<N>::low - a.offset;         // of diagonal[0][0]
-        const int64_t top = a.causal ? min(int64_t(0), r0 + DIAGONALS - 1) : r0 + DIAGONALS - 1;
-        for (int k0 = wave * 64; k0 < a.buckets; k0 += kThreads) {
-            int64_t lo = 0, hi = -1;
-            if (k0 + lane < a.buckets) range_of(first, a, k0 + lane, lo, hi);
-            const int d0 = static_cast<int>(max(lo, r0) - r0), n = static_cast<int>(max(min(hi, top) - max(lo, r0) + 1, int64_t(0)));
-            if (n > 0 && n <= 16) {
-                double sum = 0.0;
-                for (int d = 0; d < n; ++d) sum += diagonal[0][d0 + d];
-                sums[k0 + lane] += sum;
+                for (int k = 0; k < N - 1; ++k) diagonal[wave][k] = acc[k];
             }
-            for (uint64_t many = __ballot(n > 16); many != 0; many &= many - 1) {
-                const int l = __ffsll(static_cast<unsigned long long>(many)) - 1, from = __shfl(d0, l), count = __shfl(n, l);
-                double sum = 0.0;
-                for (int d = lane; d < count; d += 64) sum += diagonal[0][from + d];
+            __syncthreads();
+            if (lane > 0) {
 #pragma unroll
-                for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
-                if (lane == l) sums[k0 + l] += sum;
+                for (int k = 0; k < N - 1; ++k) diagonal[wave][N * lane + k] += acc[k];
+            }
+            __syncthreads();
+            for (int d = threadIdx.x; d < DIAGONALS; d += kThreads) {
+                float sum = diagonal[0][d];
+#pragma unroll
+                for (int w = 1; w < kWaves; ++w) sum += diagonal[w][d];
+                diagonal[0][d] = sum;
+            }
+            __syncthreads();
+            // buckets go round the threads; those of many diagonals take a wave each
+            const int64_t r0 = t0 * N - Band<N>::low - a.offset;         // of diagonal[0][0]
+            const int64_t top = a.causal ? min(int64_t(0), r0 + DIAGONALS - 1) : r0 + DIAGONALS - 1;
+            for (int k0 = wave * 64; k0 < a.buckets; k0 += kThreads) {
+                int64_t lo = 0, hi = -1;
+                if (k0 + lane < a.buckets) range_of(first, a, k0 + lane, lo, hi);
+                const int d0 = static_cast<int>(max(lo, r0) - r0), n = static_cast<int>(max(min(hi, top) - max(lo, r0) + 1, int64_t(0)));
+                if (n > 0 && n <= 16) {
+                    double sum = 0.0;
+                    for (int d = 0; d < n; ++d) sum += diagonal[0][d0 + d];
+                    sums[k0 + lane] += sum;
+                }
+                for (uint64_t many = __ballot(n > 16); many != 0; many &= many - 1) {
+                    const int l = __ffsll(static_cast<unsigned long long>(many)) - 1, from = __shfl(d0, l), count = __shfl(n, l);
+                    double sum = 0.0;
+                    for (int d = lane; d < count; d += 64) sum += diagonal[0][from + d];
+#pragma unroll
+                    for (int x = 32; x > 0; x >>= 1) sum += __shfl_xor(sum, x);
+                    if (lane == l) sums[k0 + l] += sum;
+                }
             }
         }
     }
