@@ -9,6 +9,7 @@
 // A bias depends on the diagonal alone: forward is a fill, backward a sum along diagonals.  Both are bound by memory: 16 x 4096 x 4096 causal
 // bfloat16 scores (537 MB) are filled in 91 us, 5.9 TB/s (a plain fill of as many bytes 78); the gradient of 2 x 16 x 4096 x 4096 (537 MB visible)
 // takes 98, of which 93 read 590 MB at 6.3 TB/s; 8 x 16 x 512 x 512 binary32 of ragged lengths 21.8, the join 4 of them.
+#include "extent.h"
 #include "layer_host.h"
 
 #include <cmath>
@@ -636,7 +637,7 @@ int32_t ddp_position_bias_grad(ddp_position_bias* h, int64_t batch, int64_t quer
             const dim3 grid(static_cast<unsigned>(parts * h->heads));
             j.parts = static_cast<int32_t>(parts);
             const size_t bytes = static_cast<size_t>(a.buckets) * 8;
-            const bool stream = batch * h->heads * queries * keys * elem_bytes(dtype) >= kStreamBytes;
+            const bool stream = product_reaches(kStreamBytes, {batch, h->heads, queries, keys, elem_bytes(dtype)});
             auto launch = [&](auto st, auto nt) { hipLaunchKernelGGL((diagonal_kernel<st.value, nt.value>), grid, dim3(kThreads), bytes, h->stream, a, j); };
             auto typed = [&](auto nt) {
                 if (dtype == DDP_FP32) launch(std::integral_constant<int, DDP_FP32>(), nt);
