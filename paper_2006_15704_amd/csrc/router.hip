@@ -530,12 +530,12 @@ __global__ __launch_bounds__(kThreads, !HERE && (LANES == 2 || LANES == 6) ? 6 :
                 wave_meets();
                 again = at[0] != -1;                 // some are chosen
             }
-            const float factor = !a.renormalise ? a.scale : all > 0.0f ? a.scale / all : 0.0f;
+            const float factor = !a.renormalise ? 1.0f : all > 0.0f ? 1.0f / all : 0.0f;      // (scale / all may leave binary32)
             for (int n = l; n < a.listed; n += lanes) {
                 if (again || at[n] < 0) continue;
                 const int e = at[n] & 0xFFFF, rank = at[n] >> 16;
                 a.experts_out[t * a.chosen + rank] = e;
-                store_weight(a.weights, a.weights_type, t * a.chosen + rank, as_float(word[n]) * factor);
+                store_weight(a.weights, a.weights_type, t * a.chosen + rank, as_float(word[n]) * factor * a.scale);
                 if (a.counts != nullptr) atomicAdd(&counts[e], 1);
             }
         }
