@@ -558,8 +558,8 @@ __global__ __launch_bounds__(64) void count_kernel(int32_t* copies, int32_t* cou
     if (e < experts) counts[e] = take_copies(copies, experts, e) + (accumulate ? counts[e] : 0);
 }
 
-// Below this a sigmoid is 0 in binary64 too, and the weights are.
-constexpr float kNoScore = -745.0f;
+// The largest number of binary32 whose sigmoid is 0 in binary64 too (exp(-x) is beyond it), as its weight is.
+constexpr float kNoScore = -709.78271484375f;
 
 // A token's gradient by a team of lanes with EACH experts each, in vectors of 16 bytes side by side.  What the chosen experts get is put together in a row in LDS, which is zeros
 // otherwise, and everyone reads what is theirs.  Only a softmax that is not renormalised reads the other logits: renormalised, it is that of the
@@ -644,16 +644,16 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(RouteGradArgs a) {
             of[n] = g;
             score[n] = x;
         }
-        float shift = WHOLE ? largest : 0.0f, factor = WHOLE ? part : 1.0f;
+        const float factor = WHOLE ? part : 1.0f, none = sigmoid ? kNoScore : kMasked;
+        float shift = WHOLE ? largest : 0.0f;
         if (renormalise) {
             most = team_max(a.log2_lanes, most);
             shift = sigmoid ? fminf(most, 0.0f) : most;
-            if (sigmoid && most < kNoScore) factor = 0.0f;
         }
         for (int n = l; n < a.chosen; n += lanes) {
             const float x = score[n];
             float w = 0.0f;
-            if (x != kMasked) w = sigmoid && x > 0.0f ? 1.0f / (1.0f + expf(-x)) : expf(x - shift) * (sigmoid ? factor / (1.0f + expf(x)) : factor);
+            if (!(x <= none)) w = sigmoid && x > 0.0f ? 1.0f / (1.0f + expf(-x)) : expf(x - shift) * (sigmoid ? factor / (1.0f + expf(x)) : factor);
             all += w;
             dot += of[n] * w;
             score[n] = w;
