@@ -676,7 +676,8 @@ typedef struct ddp_position_bias ddp_position_bias;
  *   f(d) = d below `exact`, then min(n - 1, exact + floor((n - exact) * log(d / exact) / log(max_distance / exact)))
  * both == 0: n = buckets, the bucket of r is f(max(-r, 0)) (keys behind the query share bucket 0); both != 0: n = buckets / 2,
  * f(|r|), + n for r > 0.  exact == n: every distance below n - 1 has its own, no logarithm.  The steps of the logarithm are
- * settled in whole numbers.  Up to 4096 heads, 1024 buckets, a distance of 2^20. */
+ * settled in whole numbers.  Up to 4096 heads, 1024 buckets, a distance of 2^20.  The workspace takes up to 16 MiB, above 2^16 heads x buckets 256 bytes
+ * for each of them (1 GiB at most). */
 int32_t ddp_position_bias_create(ddp_position_bias** out, int32_t device, void* stream, int32_t heads, int32_t buckets, int32_t exact,
                                  int64_t max_distance, int32_t both);
 int32_t ddp_position_bias_destroy(ddp_position_bias* bias);   /* waits for the handle's outstanding work */
@@ -725,7 +726,11 @@ const char* ddp_router_last_error(const ddp_router* router);
  * index; weights[t, :] (of weights_dtype, [tokens][chosen]): theirs.  bias: binary32 [experts], NULL: zeros.  An expert whose logit is -inf or whose
  * key is -inf or NaN is never chosen (nor does it count in its group; a softmax over a NaN or +inf gives NaN to all); places left over get index -1 and
  * weight 0, and so does a sum of 0.  counts (int32 [experts], may be NULL): tokens that chose each expert; accumulate != 0: added to what is
- * there.  A count of 0 on a replica is a 0 in ddp_mark_ready_local's flags for that expert's parameters. */
+ * there.  A count of 0 on a replica is a 0 in ddp_mark_ready_local's flags for that expert's parameters.  A row that is to count for nothing (padding)
+ * has logits of -inf.
+ * The time depends on the keys: tokens for which binary32 leaves the choice open, by errors relative to the largest score and the largest finite
+ * |bias|, are settled in binary64, which takes several times as long.  Sharp logits, a large finite bias as a mask (-inf costs nothing) and equal keys of more
+ * than chosen + 1 experts make them many. */
 int32_t ddp_router_route(ddp_router* router, int64_t tokens, const void* logits, int32_t dtype, int64_t stride, const float* bias,
                          int32_t* experts_out, void* weights, int32_t weights_dtype, int32_t* counts, int32_t accumulate);
 

@@ -261,7 +261,10 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
 // in the lane for their last four bits; a lane sorts its own, and the team takes the largest head, as often as there are candidates: one more than
 // are chosen.  Where the candidates' keys are all further apart than the error of a binary32 key, their order is that of binary64.
 // Where not, the candidates are ordered again by whole binary32 keys, equal logits with equal biases by their index.  Where that too leaves it open, or the
-// groups' scores come near each other, a wave does the token over in binary64: of 256 normal logits in eight groups, one token in 400.
+// groups' scores come near each other, a wave does the token over in binary64: of 256 normal logits of deviation 1.5 in eight groups, one token in 400.
+// The errors are taken from the largest score and bias of all experts, so that small keys count as near each other too: with logits of deviation 5
+// most tokens are done over (65536 x 256, softmax with small biases: 43 us at 1.5, 76 at 3, 203 at 5, 255 at 8), with a finite mask in the bias
+// all of them (252), and so are those whose logits are all equal, which take the longest (653).
 
 constexpr int kEach = 16, kSpare = 1;                // (two spare candidates: 65536 x 256 48.7 us against 47.7, 86976 x 143 66.7 against 64.3)
 // A key's error in parts of 2^-24 of the largest score and bias: exp, sum and quotient of a softmax over 1024 under 30, the key's
@@ -270,7 +273,7 @@ constexpr float kApart = 0x1p-16f;
 // The same of whole keys: 30 of the largest score and 3 of score and bias each of a softmax, 5 of a sigmoid.
 constexpr float kNearSoftmax = 0x1p-18f, kNearKey = 0x1p-20f;
 // Chosen scores whose sum is below this (biases have chosen them, or every logit of a sigmoid is far below 0) are near binary32's end, their
-// quotients not: a wave takes the weights in binary64.
+// quotients not: a wave takes the weights in binary64.  (Next to a larger sum a chosen score below 2^-126 loses its bits: less than 2^-26 of that.)
 constexpr float kTiny = 0x1p-100f;
 // Below this a lifted key and the sum of a group's two largest are finite, above -inf and below inf.
 constexpr float kGroupLift = 0x1p126f;
@@ -320,7 +323,7 @@ __device__ __forceinline__ int first_lane(uint64_t mask, int log2_lanes, int of_
 // A key as a word: positive floats sort as their bits do, so `lift` makes the key positive; 0: no key.
 __device__ __forceinline__ float key_of(uint32_t word, float lift) { return as_float(word & ~15u) - lift; }
 
-// Descending, by odd-even merges.
+// Descending, by Batcher's odd-even merges.
 template <int N>
 __device__ __forceinline__ void sort_words(uint32_t (&w)[N]) {
 #pragma unroll
@@ -723,7 +726,8 @@ __global__ __launch_bounds__(kMaxExperts) void balance_kernel(const int32_t* cou
 // Gradients of this size and more are stored past the caches (65536 x 256 16.3 us against 17.8).
 constexpr int64_t kStreamBytes = int64_t(4) << 20;
 // kBlocks: six waves a SIMD, all resident.  Up to kFewBlocks blocks do tokens over where they meet them: a second launch would cost more (one
-// token 6.1 us against 8.6, 1270 tokens 10.9 against 11.7), but more of them would run at four waves a SIMD (65536 x 256 48.6 us against 79).
+// token 6.1 us against 8.6, 1270 tokens 10.9 against 11.7), but more of them would run at four waves a SIMD (65536 x 256 47.5 us against 77).
+// The gradient takes kBlocks over (65536 x 256 16 us, with more blocks than that 18); other limits have not been measured.
 // kFewLanes: of all teams, where tokens are few (65536: 4096 tokens 24.4 us; 262144: 27.3; 16384: 3948 tokens of 30 experts 16.6 against 14.1).
 constexpr int64_t kBlocks = 1536, kFewLanes = 65536, kFewBlocks = 512;
 
